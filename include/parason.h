@@ -54,12 +54,12 @@ extern "C" {
 /* ---- status codes ------------------------------------------------------- */
 #define PARASON_OK 0
 #define PARASON_ERR_NULL (-1)      /* a required pointer argument is NULL */
-#define PARASON_ERR_SIZE (-2)      /* negative or too large n_traj / total_tokens */
+#define PARASON_ERR_SIZE (-2)      /* a negative or too large size */
 #define PARASON_ERR_GROUP (-3)     /* group_size < 1 or n_traj % group_size != 0 */
-#define PARASON_ERR_WORKSPACE (-4) /* workspace smaller than parason_workspace_size */
+#define PARASON_ERR_WORKSPACE (-4) /* workspace smaller than the call's workspace size */
 #define PARASON_ERR_TAGS (-5)      /* a tag id is negative or two tag ids are equal */
-#define PARASON_ERR_PARAM (-6)     /* a reward parameter is not finite */
-#define PARASON_ERR_ALIGN (-7)     /* tokens not 4-byte aligned or workspace not 256-byte aligned */
+#define PARASON_ERR_PARAM (-6)     /* a parameter is not finite, or a type or flag is not one that the call takes */
+#define PARASON_ERR_ALIGN (-7)     /* a pointer or stride not aligned as the call needs (workspace: 256 bytes) */
 #define PARASON_ERR_HIP (-8)       /* a HIP call or kernel launch failed */
 #define PARASON_ERR_DEVICE (-9)    /* the current device is not gfx950 or cannot be queried (checked by
                                       every call that launches, before its first launch) */
@@ -438,6 +438,178 @@ int parason_join_sized(const parason_handle *h, const int32_t *tokens, const int
                        int64_t n_rows, const int64_t *worker_off, const int32_t *wtokens, const int64_t *wstarts,
                        const int32_t *wlengths, int64_t n_workers, uint32_t flags, const parason_join_outputs *out,
                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- key/value cache of rollouts in progress -----------------------------
+ * The keys and values of the positions that rollouts have behind them, kept in
+ * pages of page_size slots: position p of row i is slot p % page_size of page
+ * pages[i * pages_stride + p / page_size].  Pages belong to a row, or to
+ * several (a shared prefix), in any order.
+ *
+ * 16-bit caches hold the values (float32 ones rounded to nearest even).  8-bit
+ * caches hold codes, and one float scale per slot and head for each of keys
+ * and values:
+ *   scale = max(amax * (1 / Q), 2^-126), amax = the largest |x| of the head's
+ *           head_dim values, Q = 448 (FP8) or 127 (INT8);
+ *   code  = x / scale rounded to nearest even; read back as code * scale
+ * (1 / Q, the product, the quotient and the product read back each rounded to
+ * float once).
+ * A head that holds a NaN or an infinity gets scale NaN, so that all of it
+ * reads back as NaN (16-bit caches keep such values as they are). */
+#define PARASON_DTYPE_FP8 3  /* 8 bits: sign, 4 exponent bits, 3 fraction bits, no infinities (OCP E4M3) */
+#define PARASON_DTYPE_INT8 4 /* -127 .. 127 */
+
+#define PARASON_KV_MAX_DIM 256
+#define PARASON_KV_MAX_HEADS 1024
+
+/* Device memory of the caller; the struct itself is host memory.  Value d of
+ * head h in slot t of page p is element
+ *   p * stride_page + t * stride_slot + h * stride_head + d
+ * of k or v, and its scale element
+ *   p * scale_stride_page + t * scale_stride_slot + h * scale_stride_head
+ * of k_scale or v_scale.  k and v are 16-byte aligned and their strides
+ * multiples of 16 bytes, so that a head's values are read 16 bytes at a time. */
+typedef struct parason_kv_cache {
+    void *k, *v;
+    float *k_scale, *v_scale; /* 8-bit caches; NULL for 16-bit ones */
+    int64_t n_pages;
+    int64_t stride_page, stride_slot, stride_head;
+    int64_t scale_stride_page, scale_stride_slot, scale_stride_head;
+    int32_t page_size, n_heads;
+    int32_t head_dim;         /* a multiple of 16, at most PARASON_KV_MAX_DIM */
+    int32_t dtype;            /* PARASON_DTYPE_BF16, _F16, _FP8 or _INT8 */
+} parason_kv_cache;
+
+/* The rows of a call (device arrays, host struct).  Row i has lengths[i] tokens
+ * at starts[i] of the call's token arrays (queries, or keys and values), and
+ * kv_lens[i] positions in the cache.  max_length and max_kv_len are bounds
+ * that the caller knows on the host; the launches are sized by them. */
+typedef struct parason_kv_rows {
+    int64_t n_rows;
+    int64_t n_tokens;         /* tokens of the call's token arrays */
+    const int64_t *starts;    /* [n_rows] */
+    const int32_t *lengths;   /* [n_rows] */
+    const int32_t *kv_lens;   /* [n_rows] */
+    const int32_t *pages;     /* row i: pages[i * pages_stride ..], max_pages entries; those that no position of the
+                                 row needs are not read */
+    int64_t pages_stride;
+    int32_t max_pages;
+    int32_t max_length;       /* >= every lengths[i] */
+    int32_t max_kv_len;       /* >= every kv_lens[i] */
+} parason_kv_rows;
+
+/* Bits that the calls below OR into row_status[i] (uint32[n_rows] that the
+ * caller has cleared, so that one array may serve several calls; NULL: not
+ * reported). */
+#define PARASON_KV_BAD_ROW (1u << 0)  /* a negative or too large length, tokens outside [0, n_tokens), more positions
+                                         than max_kv_len or max_pages allow, fewer than the call needs, or more tree
+                                         positions than the mask holds */
+#define PARASON_KV_BAD_PAGE (1u << 1) /* a page outside [0, n_pages) in a place that the row needs */
+
+/* Write the keys and values of the rows' tokens into the cache, asynchronously
+ * on `stream`: token j of row i goes to position kv_lens[i] - lengths[i] + j,
+ * so kv_lens counts the positions with the new ones.  k and v hold n_tokens
+ * tokens of cache->n_heads heads: value d of head h of token t is element
+ * t * stride_token + h * stride_head + d, of type `dtype` (PARASON_DTYPE_F32,
+ * _BF16 or _F16; a 16-bit cache takes its own type or F32), at any alignment
+ * of the type.  Bad rows are not written, nor are positions whose page is bad.
+ * Two tokens that fall on one slot leave either of them. */
+int parason_kv_write(const parason_kv_cache *cache, const parason_kv_rows *rows, const void *k, const void *v,
+                     int32_t dtype, int64_t stride_token, int64_t stride_head, uint32_t *row_status, void *stream);
+
+/* The reverse: read the last lengths[i] of the first kv_lens[i] positions of
+ * every row into k and v (code * scale, rounded to `dtype`: F32, BF16 or F16).
+ * Positions whose page is bad read as NaN; bad rows are not written. */
+int parason_kv_read(const parason_kv_cache *cache, const parason_kv_rows *rows, void *k, void *v, int32_t dtype,
+                    int64_t stride_token, int64_t stride_head, uint32_t *row_status, void *stream);
+
+/* ---- attention for a tree of tokens over the cache -----------------------
+ * Several tokens of a row at once, each of which sees the row's prefix and its
+ * own path: the threads of a <Parallel> region (Sec. 3.4), draft tokens, the
+ * beams of a prompt.  The last tree_lens[i] of the row's kv_lens[i] positions
+ * are its tree, the others its prefix.  Token j of row i sees every position
+ * of the prefix, and position kv_lens[i] - tree_lens[i] + b of the tree when
+ * bit b % 64 of mask word (starts[i] + j) * mask_stride + b / 64 is set.
+ * Without a mask, token j sees positions 0 .. kv_lens[i] - lengths[i] + j: a
+ * single token, or a chain of them.  Query head h reads cache head
+ * h / (n_q_heads / n_heads):
+ *   s_p = scale * q . k_p,   out = sum_p exp(s_p) v_p / sum_p exp(s_p),
+ *   lse = ln sum_p exp(s_p)   over the positions p that the token sees.
+ * A token that sees nothing (or whose scores are all -inf) gets out = 0 and
+ * lse = -inf.  What a token does not see changes nothing for it, whatever it
+ * holds.  Scores, maxima, sums and the accumulation are float32; the weights
+ * exp(s_p - max) are rounded to 16 bits for the matrix product with v.
+ * Rows that are bad, or need a bad page, get NaN (nothing, where starts[i] and
+ * lengths[i] themselves are bad). */
+typedef struct parason_tree_args {
+    const void *q;            /* value d of head h of token t: element t * q_stride_token + h * q_stride_head + d */
+    void *out;                /* the same with its own strides */
+    float *lse;               /* optional: [n_tokens * n_q_heads] */
+    int64_t q_stride_token, q_stride_head, out_stride_token, out_stride_head;
+    const uint64_t *mask;     /* NULL: a chain */
+    int64_t mask_stride;      /* words between the mask words of a token and the next */
+    const int32_t *tree_lens; /* [n_rows]; NULL: lengths.  Only with a mask */
+    int32_t mask_words;       /* words of a token; tree_lens[i] <= 64 * mask_words */
+    int32_t n_q_heads;        /* a multiple of the cache's heads */
+    int32_t dtype;            /* of q and out: BF16 or F16, that of a 16-bit cache */
+    float scale;
+} parason_tree_args;
+
+/* Bytes of device workspace parason_tree_attention needs (host arithmetic on
+ * the sizes and bounds alone: the same for every call that has them). */
+int parason_tree_attention_workspace_size(const parason_kv_cache *cache, const parason_kv_rows *rows,
+                                          int32_t n_q_heads, size_t *bytes);
+
+/* The attention, asynchronously on `stream`.  Host-side argument errors return
+ * a negative status before any launch. */
+int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows *rows, const parason_tree_args *args,
+                           uint32_t *row_status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- beams ---------------------------------------------------------------
+ * n_groups prompts of `beams` beams each; beam b of group g is row
+ * g * beams + b.  A row's candidates are its tokens t, each with
+ *   score + logits[t] - ln sum_u exp(logits[u]),
+ * (logits of -inf, as parason_decode_step leaves them for forbidden tokens, are
+ * no candidates), or, when its decode state says PARASON_DECODE_DONE, the row
+ * as it is (token -1) with its score alone.  The new beams of a group are its
+ * `beams` best candidates, best first, ties to the lowest row and token.
+ * Candidates are compared in double precision, from a float32 sum of
+ * exponentials.
+ *
+ * Not a candidate: a row whose score is not finite (the empty beams of a prompt
+ * that has just begun have -inf), whose state says PARASON_DECODE_ERROR, or
+ * whose sum is not finite (a NaN or +inf among its logits).  Where a group has
+ * fewer candidates than beams the last beams are empty: score -inf, token -1,
+ * parent the beam's own row. */
+#define PARASON_BEAM_MAX 64
+
+/* Bytes of device workspace parason_beam_select needs. */
+int parason_beam_workspace_size(int64_t n_groups, int32_t beams, int64_t vocab, size_t *bytes);
+
+/* The selection, asynchronously on `stream`.  logits: row i at logits +
+ * i * row_stride elements, `vocab` of type `dtype` (F32, BF16, F16), aligned to
+ * the element; scores float[rows]; states parason_decode_state[rows] or NULL
+ * (no row is finished).  Outputs [rows]: new_scores (may be scores itself),
+ * parents (the row that a beam continues) and tokens, as parason_decode_step
+ * takes them once the states are in the new order. */
+int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, int32_t dtype, const float *scores,
+                        const parason_decode_state *states, int64_t n_groups, int32_t beams, float *new_scores,
+                        int32_t *parents, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream);
+
+/* What belongs to a beam, in the new order: row i of every array's dst becomes
+ * row parents[i] of its src, byte for byte (decode states, token histories,
+ * mask rows of the tree attention, page tables, ...).  A parent outside
+ * [0, n_rows) leaves the row of dst as it is.  src and dst do not overlap; up
+ * to PARASON_BEAM_ARRAYS arrays, in one launch, asynchronously on `stream`. */
+#define PARASON_BEAM_ARRAYS 8
+typedef struct parason_beam_array {
+    const void *src;
+    void *dst;
+    int64_t row_bytes;
+    int64_t src_stride, dst_stride; /* bytes between rows, >= row_bytes */
+} parason_beam_array;
+
+int parason_beam_reorder(const int32_t *parents, int64_t n_rows, const parason_beam_array *arrays, int32_t n_arrays,
+                         void *stream);
 
 /* Static description of a status code. */
 const char *parason_strerror(int status);

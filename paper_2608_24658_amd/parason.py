@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from typing import Any, NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libparason.so")
@@ -45,7 +46,9 @@ MAX_OPEN_ENTRIES = 1 << 24
 EXPORTED = ("parason_create", "parason_workspace_size", "parason_run", "parason_run_timed", "parason_destroy",
             "parason_strerror", "parason_pg_workspace_size", "parason_pg_run", "parason_decode_init",
             "parason_decode_step", "parason_fork_workspace_size", "parason_join_workspace_size", "parason_fork",
-            "parason_join", "parason_read_probe", "parason_run_noalloc", "parason_fork_sized", "parason_join_sized")
+            "parason_join", "parason_read_probe", "parason_run_noalloc", "parason_fork_sized", "parason_join_sized",
+            "parason_kv_write", "parason_kv_read", "parason_tree_attention_workspace_size", "parason_tree_attention",
+            "parason_beam_workspace_size", "parason_beam_select", "parason_beam_reorder")
 
 FORK_SEED_ENTRY = 1 << 0
 JOIN_CLOSE_PARALLEL = 1 << 0
@@ -59,8 +62,15 @@ PACK_BAD_ROW = 1 << 5
 
 DECODE_ERROR = 1 << 0
 DECODE_DONE = 1 << 1
-DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_FP8, DTYPE_INT8 = range(5)
 DECODE_STATE_BYTES = 16
+
+KV_BAD_ROW = 1 << 0
+KV_BAD_PAGE = 1 << 1
+KV_MAX_DIM = 256
+KV_MAX_HEADS = 1024
+BEAM_MAX = 64
+BEAM_ARRAYS = 8
 
 PG_STATS = ("loss", "tokens", "clip_high", "clip_low")
 
@@ -126,6 +136,70 @@ class JoinOutputs(ctypes.Structure):
         ("lengths", ctypes.c_void_p),
         ("row_status", ctypes.c_void_p),
         ("totals", ctypes.c_void_p),
+    ]
+
+
+class KvCacheArgs(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int64),
+        ("stride_page", ctypes.c_int64),
+        ("stride_slot", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("scale_stride_page", ctypes.c_int64),
+        ("scale_stride_slot", ctypes.c_int64),
+        ("scale_stride_head", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("n_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
+class KvRowsArgs(ctypes.Structure):
+    _fields_ = [
+        ("n_rows", ctypes.c_int64),
+        ("n_tokens", ctypes.c_int64),
+        ("starts", ctypes.c_void_p),
+        ("lengths", ctypes.c_void_p),
+        ("kv_lens", ctypes.c_void_p),
+        ("pages", ctypes.c_void_p),
+        ("pages_stride", ctypes.c_int64),
+        ("max_pages", ctypes.c_int32),
+        ("max_length", ctypes.c_int32),
+        ("max_kv_len", ctypes.c_int32),
+    ]
+
+
+class TreeArgs(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("lse", ctypes.c_void_p),
+        ("q_stride_token", ctypes.c_int64),
+        ("q_stride_head", ctypes.c_int64),
+        ("out_stride_token", ctypes.c_int64),
+        ("out_stride_head", ctypes.c_int64),
+        ("mask", ctypes.c_void_p),
+        ("mask_stride", ctypes.c_int64),
+        ("tree_lens", ctypes.c_void_p),
+        ("mask_words", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class BeamArray(ctypes.Structure):
+    _fields_ = [
+        ("src", ctypes.c_void_p),
+        ("dst", ctypes.c_void_p),
+        ("row_bytes", ctypes.c_int64),
+        ("src_stride", ctypes.c_int64),
+        ("dst_stride", ctypes.c_int64),
     ]
 
 
@@ -220,6 +294,19 @@ def lib():
         L.parason_read_probe.restype = ctypes.c_int
         L.parason_read_probe.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_int64,
                                          ctypes.c_void_p]
+        cache, rows, void, i64 = ctypes.POINTER(KvCacheArgs), ctypes.POINTER(KvRowsArgs), ctypes.c_void_p, ctypes.c_int64
+        for name, args in (
+            ("parason_kv_write", [cache, rows, void, void, ctypes.c_int32, i64, i64, void, void]),
+            ("parason_kv_read", [cache, rows, void, void, ctypes.c_int32, i64, i64, void, void]),
+            ("parason_tree_attention_workspace_size", [cache, rows, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]),
+            ("parason_tree_attention", [cache, rows, ctypes.POINTER(TreeArgs), void, void, ctypes.c_size_t, void]),
+            ("parason_beam_workspace_size", [i64, ctypes.c_int32, i64, ctypes.POINTER(ctypes.c_size_t)]),
+            ("parason_beam_select", [void, i64, i64, ctypes.c_int32, void, void, i64, ctypes.c_int32, void, void, void,
+                                     void, ctypes.c_size_t, void]),
+            ("parason_beam_reorder", [void, i64, ctypes.POINTER(BeamArray), ctypes.c_int32, void]),
+        ):
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = args
         L.parason_strerror.restype = ctypes.c_char_p
         L.parason_strerror.argtypes = [ctypes.c_int]
         _lib = L
@@ -547,3 +634,321 @@ def pg_run(reward, logp, logp_old, starts, lengths, group_size=8, clip_low=0.2, 
     if rc != OK:
         raise ParasonError(rc, "parason_pg_run")
     return dict(advantage=adv, grad=grad, stats=stats)
+
+
+# ---- the cache of rollouts in progress, tree attention, beams ----------------
+
+
+class KVCache(NamedTuple):
+    """Paged keys and values (device tensors).  k and v are [pages, page_size,
+    heads, head_dim] in any layout whose last stride is 1, of one type (bfloat16,
+    float16, float8_e4m3fn or int8) and with the same strides; k_scale and
+    v_scale (8-bit types only) float32 [pages, page_size, heads], with the same
+    strides."""
+
+    k: Any
+    v: Any
+    k_scale: Any = None
+    v_scale: Any = None
+
+
+class KVRows(NamedTuple):
+    """The rows of a call (device tensors): row i has lengths[i] tokens at
+    starts[i] of the call's token arrays and kv_lens[i] positions in the cache,
+    on the pages pages[i].  starts int64, lengths and kv_lens int32, pages int32
+    [rows, max_pages] with unit stride along a row.  max_length and max_kv_len
+    are bounds of lengths and kv_lens that the program knows."""
+
+    starts: Any
+    lengths: Any
+    kv_lens: Any
+    pages: Any
+    max_length: int
+    max_kv_len: int
+
+
+def kv_alloc(n_pages: int, page_size: int, heads: int, head_dim: int, dtype, device) -> KVCache:
+    """A cache of zeros, each head's slots of a page next to each other."""
+    import torch
+
+    code = _kv_types().get(dtype)
+    if code is None:
+        raise TypeError("a cache holds bfloat16, float16, float8_e4m3fn or int8 values")
+    shape = (int(n_pages), int(heads), int(page_size), int(head_dim))
+    kv = [torch.zeros(shape, dtype=torch.uint8 if code >= DTYPE_FP8 else dtype, device=device).view(dtype)
+          .permute(0, 2, 1, 3) for _ in "kv"]
+    if code >= DTYPE_FP8:
+        kv += [torch.zeros(shape[:3], dtype=torch.float32, device=device).permute(0, 2, 1) for _ in "kv"]
+    return KVCache(*kv)
+
+
+@functools.lru_cache(maxsize=None)
+def _kv_types():
+    import torch
+
+    return {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_FP8, torch.int8: DTYPE_INT8}
+
+
+@functools.lru_cache(maxsize=None)
+def _float_types():
+    import torch
+
+    return {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+
+
+def _cache_args(cache: KVCache) -> KvCacheArgs:
+    import torch
+
+    k, v, ks, vs = cache
+    code = _kv_types().get(k.dtype)
+    if code is None or v.dtype is not k.dtype or k.dim() != 4 or not k.is_cuda or not v.is_cuda:
+        raise TypeError("k and v must be [pages, page_size, heads, head_dim] bfloat16/float16/float8_e4m3fn/int8 "
+                        "device tensors of one type")
+    shape, st = k.shape, k.stride()
+    if v.shape != shape or v.stride() != st or (st[3] != 1 and shape[3] > 1):
+        raise ValueError("k and v must have the same shape and strides, and unit stride along a head")
+    if code < DTYPE_FP8:
+        if ks is not None or vs is not None:
+            raise TypeError("a 16-bit cache has no scales")
+        return KvCacheArgs(k.data_ptr(), v.data_ptr(), None, None, shape[0], st[0], st[1], st[2], 0, 0, 0, shape[1],
+                           shape[2], shape[3], code)
+    if ks is None or vs is None or ks.dtype is not torch.float32 or vs.dtype is not torch.float32 \
+            or not ks.is_cuda or not vs.is_cuda:
+        raise TypeError("an 8-bit cache needs float32 device tensors k_scale and v_scale")
+    sst = ks.stride()
+    if ks.shape != shape[:3] or vs.shape != shape[:3] or vs.stride() != sst:
+        raise ValueError("k_scale and v_scale must be [pages, page_size, heads], with the same strides")
+    return KvCacheArgs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), shape[0], st[0], st[1], st[2], sst[0],
+                       sst[1], sst[2], shape[1], shape[2], shape[3], code)
+
+
+def _rows_args(rows: KVRows, n_tokens: int) -> KvRowsArgs:
+    import torch
+
+    starts, lengths, kv_lens, pages, max_length, max_kv_len = rows
+    n = starts.numel()
+    for t, dt in ((starts, torch.int64), (lengths, torch.int32), (kv_lens, torch.int32)):
+        if t.dtype is not dt or not t.is_cuda or not t.is_contiguous():
+            raise TypeError("expected contiguous %s device tensors" % dt)
+    if pages.dtype is not torch.int32 or not pages.is_cuda or pages.dim() != 2 \
+            or (pages.stride(1) != 1 and pages.shape[1] > 1):
+        raise TypeError("pages must be an int32 [rows, max_pages] device tensor, unit stride along a row")
+    if lengths.numel() != n or kv_lens.numel() != n or pages.shape[0] != n:
+        raise ValueError("starts, lengths, kv_lens and pages must have the same number of rows")
+    return KvRowsArgs(n, n_tokens, starts.data_ptr(), lengths.data_ptr(), kv_lens.data_ptr(), pages.data_ptr(),
+                      pages.stride(0), pages.shape[1], int(max_length), int(max_kv_len))
+
+
+def _status_ptr(status, n):
+    import torch
+
+    if status is None:
+        return None
+    if status.dtype is not torch.int32 or status.numel() != n or not status.is_contiguous() or not status.is_cuda:
+        raise TypeError("status must be a contiguous int32 device tensor of one entry per row")
+    return status.data_ptr()
+
+
+def _token_arrays(k, v, cache: KVCache):
+    """Type, token stride and head stride of two [tokens, heads, head_dim] tensors."""
+    code = _float_types().get(k.dtype)
+    if code is None or v.dtype is not k.dtype or k.dim() != 3 or not k.is_cuda or not v.is_cuda:
+        raise TypeError("k and v must be [tokens, heads, head_dim] float32/bfloat16/float16 device tensors of one type")
+    if k.shape != v.shape or k.stride() != v.stride() or k.shape[1:] != cache.k.shape[2:] \
+            or (k.stride(2) != 1 and k.shape[2] > 1):
+        raise ValueError("k and v must have the cache's heads, the same shape and strides, and unit stride along a head")
+    return code, k.stride(0), k.stride(1)
+
+
+def kv_write(k, v, cache: KVCache, rows: KVRows, status=None) -> None:
+    """Write the keys and values of the rows' tokens ([tokens, heads, head_dim]
+    tensors) into the cache, at the last lengths[i] of row i's kv_lens[i]
+    positions (asynchronous on the current stream).  8-bit caches are quantised
+    per slot and head.  status: int32[rows] that KV_BAD_* bits are added to."""
+    ca, ra = _cache_args(cache), _rows_args(rows, k.shape[0])
+    code, st, sh = _token_arrays(k, v, cache)
+    rc = (_lib or lib()).parason_kv_write(ca, ra, k.data_ptr(), v.data_ptr(), code, st, sh,
+                                          _status_ptr(status, ra.n_rows), _stream(k.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_kv_write")
+
+
+def kv_read(cache: KVCache, rows: KVRows, n_tokens: int, dtype, out=None, status=None):
+    """(k, v): the last lengths[i] of row i's kv_lens[i] positions as
+    [n_tokens, heads, head_dim] tensors of `dtype` (asynchronous on the current
+    stream; `out`: a pair of tensors to write into)."""
+    import torch
+
+    if out is None:
+        shape = (int(n_tokens),) + tuple(cache.k.shape[2:])
+        out = tuple(torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in "kv")
+    k, v = out
+    if k.shape[0] != n_tokens or k.dtype is not dtype:
+        raise ValueError("out must hold n_tokens tokens of dtype")
+    ca, ra = _cache_args(cache), _rows_args(rows, int(n_tokens))
+    code, st, sh = _token_arrays(k, v, cache)
+    rc = (_lib or lib()).parason_kv_read(ca, ra, k.data_ptr(), v.data_ptr(), code, st, sh,
+                                         _status_ptr(status, ra.n_rows), _stream(k.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_kv_read")
+    return out
+
+
+def tree_attention_workspace_size(cache: KVCache, rows: KVRows, n_tokens: int, q_heads: int) -> int:
+    return _tree_workspace(_cache_args(cache), _rows_args(rows, int(n_tokens)), int(q_heads))
+
+
+def _tree_workspace(ca, ra, q_heads: int) -> int:
+    b = ctypes.c_size_t()
+    rc = (_lib or lib()).parason_tree_attention_workspace_size(ca, ra, q_heads, b)
+    if rc != OK:
+        raise ParasonError(rc, "parason_tree_attention_workspace_size")
+    return b.value
+
+
+def tree_attention(q, cache: KVCache, rows: KVRows, mask=None, tree_lens=None, scale=None, out=None, lse=False,
+                   workspace=None, status=None):
+    """Attention of the rows' tokens over the cache (asynchronous on the current
+    stream); returns out, or (out, lse).
+
+    q       [tokens, q_heads, head_dim] bfloat16 or float16 (a 16-bit cache's
+            own type), any strides with unit stride along a head
+    mask    int64 [tokens, words]: the positions of its row's tree that a token
+            sees, bit b of word w the position 64 * w + b; None: a chain, where
+            every token sees all positions up to its own
+    tree_lens  int32 [rows]: the last positions of each row that form its tree
+            (default: the row's tokens)
+    scale   of the scores (default head_dim ** -0.5)
+    lse     True (or a float32 [tokens, q_heads] tensor): also the logarithm of
+            each token's and head's sum of exponentials
+    """
+    import torch
+
+    code = _float_types().get(q.dtype)
+    if code is None or code == DTYPE_F32 or q.dim() != 3 or not q.is_cuda or (q.stride(2) != 1 and q.shape[2] > 1):
+        raise TypeError("q must be a [tokens, q_heads, head_dim] bfloat16/float16 device tensor, unit stride along a head")
+    n_tokens, q_heads, dim = q.shape
+    if dim != cache.k.shape[3]:
+        raise ValueError("q must have the cache's head_dim")
+    ca, ra = _cache_args(cache), _rows_args(rows, n_tokens)
+    if out is None:
+        out = torch.empty((n_tokens, q_heads, dim), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_cuda or (out.stride(2) != 1 and dim > 1):
+        raise TypeError("out must be a device tensor of q's shape and type, unit stride along a head")
+    if lse is True:
+        lse = torch.empty((n_tokens, q_heads), dtype=torch.float32, device=q.device)
+    elif lse is False:
+        lse = None
+    elif lse.dtype is not torch.float32 or lse.shape != (n_tokens, q_heads) or not lse.is_contiguous() or not lse.is_cuda:
+        raise TypeError("lse must be a contiguous float32 [tokens, q_heads] device tensor")
+    words = stride = 0
+    if mask is not None:
+        if mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != n_tokens or not mask.is_cuda \
+                or (mask.stride(1) != 1 and mask.shape[1] > 1):
+            raise TypeError("mask must be an int64 [tokens, words] device tensor, unit stride along a token")
+        words, stride = mask.shape[1], mask.stride(0)
+    if tree_lens is not None and (tree_lens.dtype is not torch.int32 or tree_lens.numel() != ra.n_rows
+                                  or not tree_lens.is_contiguous() or not tree_lens.is_cuda):
+        raise TypeError("tree_lens must be a contiguous int32 device tensor of one entry per row")
+    if workspace is None:
+        workspace = torch.empty(_tree_workspace(ca, ra, q_heads), dtype=torch.uint8, device=q.device)
+    ta = TreeArgs(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q.stride(0), q.stride(1),
+                  out.stride(0), out.stride(1), mask.data_ptr() if mask is not None else None, stride,
+                  tree_lens.data_ptr() if tree_lens is not None else None, words, q_heads, code,
+                  dim ** -0.5 if scale is None else float(scale))
+    rc = (_lib or lib()).parason_tree_attention(ca, ra, ta, _status_ptr(status, ra.n_rows), workspace.data_ptr(),
+                                                workspace.numel(), _stream(q.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_tree_attention")
+    return out if lse is None else (out, lse)
+
+
+@functools.lru_cache(maxsize=256)
+def beam_workspace_size(n_groups: int, beams: int, vocab: int) -> int:
+    b = ctypes.c_size_t()
+    rc = lib().parason_beam_workspace_size(n_groups, beams, vocab, b)
+    if rc != OK:
+        raise ParasonError(rc, "parason_beam_workspace_size")
+    return b.value
+
+
+def beam_select(logits, scores, beams: int, states=None, workspace=None) -> dict:
+    """The `beams` best continuations of every group of `beams` rows
+    (asynchronous on the current stream): dict of score (float32), parent (the
+    row continued) and token (-1: the row is finished, or the beam empty), int32.
+
+    logits  [rows, vocab] float32/bfloat16/float16, unit stride along the
+            vocabulary; -inf forbids a token
+    scores  float32 [rows]; -inf: an empty beam
+    states  decode states (uint8[rows * 16]) or None: finished rows stay as they
+            are, rows with an error are dropped"""
+    import torch
+
+    code = _float_types().get(logits.dtype)
+    if code is None or logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise TypeError("logits must be a [rows, vocab] float32/bfloat16/float16 device tensor, unit stride")
+    rows, vocab = logits.shape
+    beams = int(beams)
+    if beams < 1 or rows % beams:
+        raise ValueError("the rows must be whole groups of beams")
+    if scores.dtype is not torch.float32 or scores.numel() != rows or not scores.is_contiguous() or not scores.is_cuda:
+        raise TypeError("scores must be a contiguous float32 device tensor of one entry per row")
+    if states is not None and (states.dtype is not torch.uint8 or states.numel() != rows * DECODE_STATE_BYTES
+                               or not states.is_contiguous() or not states.is_cuda):
+        raise TypeError("states must be a contiguous uint8 device tensor of rows * 16 bytes")
+    if workspace is None:
+        workspace = torch.empty(beam_workspace_size(rows // beams, beams, vocab), dtype=torch.uint8, device=logits.device)
+    score = torch.empty_like(scores)
+    parent, token = torch.empty((2, rows), dtype=torch.int32, device=logits.device)
+    rc = (_lib or lib()).parason_beam_select(
+        logits.data_ptr(), vocab, logits.stride(0) if rows > 1 else vocab, code, scores.data_ptr(),
+        states.data_ptr() if states is not None else None, rows // beams, beams, score.data_ptr(), parent.data_ptr(),
+        token.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(logits.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_beam_select")
+    return dict(score=score, parent=parent, token=token)
+
+
+def beam_reorder(parent, arrays, out=None) -> list:
+    """What belongs to the beams, in their new order: row i of every result is
+    row parent[i] of the array (asynchronous on the current stream).  arrays: up
+    to BEAM_ARRAYS device tensors, each [rows, ...] with contiguous rows, or a
+    flat one of rows equal parts; out: tensors to write into, other than these."""
+    import torch
+
+    rows = parent.numel()
+    if parent.dtype is not torch.int32 or not parent.is_contiguous() or not parent.is_cuda:
+        raise TypeError("parent must be a contiguous int32 device tensor")
+    if len(arrays) > BEAM_ARRAYS:
+        raise ValueError("at most %d arrays in one call" % BEAM_ARRAYS)
+    if out is None:
+        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in arrays]
+    if len(out) != len(arrays):
+        raise ValueError("as many results as arrays")
+    args = (BeamArray * max(1, len(arrays)))()
+    for a, x, y in zip(args, arrays, out):
+        if x.dtype is not y.dtype or x.shape != y.shape or not x.is_cuda or not y.is_cuda:
+            raise TypeError("a result must be a device tensor of its array's shape and type")
+        a.src, a.dst = x.data_ptr(), y.data_ptr()
+        a.row_bytes, a.src_stride = _row_bytes(x, rows)
+        a.dst_stride = _row_bytes(y, rows)[1]
+    rc = (_lib or lib()).parason_beam_reorder(parent.data_ptr(), rows, args, len(arrays), _stream(parent.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_beam_reorder")
+    return out
+
+
+def _row_bytes(x, rows: int):
+    """Bytes of a row of x, and from one row to the next."""
+    size = x.element_size()
+    if x.is_contiguous():
+        n = x.numel()
+        if rows == 0 or n % rows:
+            if rows == n == 0:
+                return 0, 0
+            raise ValueError("an array must have rows equal parts")
+        return n // rows * size, n // rows * size
+    if x.shape[0] != rows or (rows and not x[0].is_contiguous()) or x.stride(0) < 0:
+        raise ValueError("an array must be [rows, ...] with contiguous rows")
+    n = x[0].numel() if rows else 0
+    return n * size, x.stride(0) * size

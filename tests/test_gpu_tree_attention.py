@@ -1,0 +1,290 @@
+"""The attention of a tree of tokens over the paged cache on the GPU against the oracle in 64 bits, within the error
+bound that the oracle derives for every output from its own inputs."""
+import numpy as np
+import pytest
+
+from decoding_cases import Paged, torch_type, tree_seen, words
+from gpu_util import log
+from oracle import decoding_oracle as D
+from paper_2608_24658_amd import parason as PX
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch.device("cuda:0")
+
+
+def given_of(kind, seed):
+    return kind if kind in ("bf16", "fp16") else ("bf16", "fp16")[seed % 2]
+
+
+def check(P, q, out, lse, seens, starts, lengths, scale, given):
+    bits_of = {"bf16": 7, "fp16": 10}
+    # weights: 16 bits of the cache's own type, bfloat16 where it holds 8 bits
+    weight = bits_of[P.kind] if P.kind in bits_of else 7
+    worst = 0.0
+    out, lse, qh = out.detach().cpu().double().numpy(), lse.cpu().double().numpy(), q.detach().cpu().double().numpy()
+    for i, n in enumerate(lengths):
+        if n == 0:
+            continue
+        k, v = P.held[i]
+        at = slice(starts[i], starts[i] + n)
+        o, z, ot, zt = D.attention(qh[at], k, v, seens[i], scale, weight, bits_of[given])
+        fine = np.isfinite(o)
+        assert np.array_equal(np.isnan(o), np.isnan(out[at])), ("NaN", i)
+        with np.errstate(invalid="ignore"):
+            far = np.where(fine, np.abs(out[at] - o) / np.where(fine, ot + 1e-300, 1), np.where(out[at] == o, 0, np.inf))
+            far = np.where(np.isnan(o), 0, far)
+            farz = np.where(np.isfinite(z), np.abs(lse[at] - z) / np.where(np.isfinite(z), zt + 1e-300, 1),
+                            np.where((lse[at] == z) | (np.isnan(z) & np.isnan(lse[at])), 0, np.inf))
+        worst = max(worst, float(far.max()), float(farz.max()))
+        assert far.max() <= 1, ("out", i, np.unravel_index(far.argmax(), far.shape), far.max())
+        assert farz.max() <= 1, ("lse", i, np.unravel_index(farz.argmax(), farz.shape), farz.max())
+    return worst
+
+
+def run_case(dev, kind, page, heads, group, dim, kv_lens, lengths, shape=None, tree_lens=None, seed=0, layout="heads", pad=0, values=None,
+             odd=False, scale=None, given=None, spoil=None):
+    """A case through the binding and the oracle.  shape: None (a chain) or a tree of decoding_cases.tree_seen."""
+    given = given or given_of(kind, seed)
+    rng = np.random.default_rng(seed)
+    P = Paged(dev, kv_lens, page, heads, dim, kind, seed, layout=layout, pad=pad)
+    P.fill(values or (lambda i, n: rng.standard_normal((2, n, heads, dim)) * np.exp(rng.uniform(-2, 2, (2, n, heads, 1)))))
+    rows, total, starts = P.rows(lengths, gap=1)
+    q = torch.as_tensor(rng.standard_normal((total, heads * group, dim)).astype(np.float32)).to(torch_type(given))
+    if odd:  # neither tight nor aligned to 16 bytes
+        wide = torch.zeros(total, heads * group, dim + 3, dtype=q.dtype, device=dev)
+        wide[..., 1: dim + 1] = q.to(dev)
+        qd, out = wide[..., 1: dim + 1], torch.full_like(wide, 9.0)[..., 1: dim + 1]
+    else:
+        qd, out = q.to(dev), torch.full(q.shape, 9.0, dtype=q.dtype, device=dev)
+    mask = trees = None
+    if shape is None:
+        seens = [D.visible(int(kv), int(n)) for kv, n in zip(kv_lens, lengths)]
+    else:
+        t = np.asarray(lengths if tree_lens is None else tree_lens)
+        n_words = max(1, -(-int(t.max()) // 64)) + seed % 2
+        m = np.full((total, n_words), 0xFFFFFFFFFFFFFFFF, np.uint64)
+        seens = []
+        for i, n in enumerate(lengths):
+            s = tree_seen(rng, int(t[i]), shape)[int(t[i]) - int(n):] if n else np.zeros((0, int(t[i])), bool)
+            w = words(s, n_words)
+            # bits behind the tree mean nothing
+            w |= ~words(np.ones((int(n), int(t[i])), bool), n_words)
+            m[starts[i]: starts[i] + n] = w
+            seens.append(D.visible(int(kv_lens[i]), int(n), int(t[i]), w))
+        mask = torch.as_tensor(m.view(np.int64)).to(dev)
+        trees = torch.as_tensor(t).to(device=dev, dtype=torch.int32) if tree_lens is not None else None
+    if spoil is not None:
+        spoil(P, seens)
+    status = torch.zeros(len(lengths), dtype=torch.int32, device=dev)
+    scale = dim ** -0.5 if scale is None else scale
+    got, lse = PX.tree_attention(qd, P.cache, rows, mask=mask, tree_lens=trees, scale=scale, out=out, lse=True, status=status)
+    assert status.cpu().tolist() == [0] * len(lengths)
+    worst = check(P, q, got, lse, seens, starts, lengths, scale, given)
+    owned = np.zeros(total, bool)
+    for s, n in zip(starts, lengths):
+        owned[s: s + n] = True
+    assert torch.all(got.cpu()[torch.from_numpy(~owned)] == 9.0)
+    log("  within %.3f of the bound" % worst)
+    return got, lse
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp8", "int8"])
+@pytest.mark.parametrize("dim", [16, 64, 80, 128, 192, 256])
+def test_single_tokens(dev, kind, dim):
+    log("case single tokens %s dim %d" % (kind, dim))
+    kv = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300]
+    run_case(dev, kind, 16, 2, 4, dim, kv, [1] * len(kv), seed=dim)
+
+
+@pytest.mark.parametrize("heads,group", [(1, 1), (8, 1), (1, 16), (4, 7), (1, 48), (2, 40), (1, 130)])
+def test_head_layouts(dev, heads, group):
+    log("case heads %d group %d" % (heads, group))
+    run_case(dev, "bf16", 32, heads, group, 64, [5, 70, 200], [1, 3, 2], seed=group)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("page", [1, 3, 8, 24, 64, 100, 256])
+def test_pages(dev, kind, page):
+    """Pages that end inside every kind of tile."""
+    log("case pages of %d, %s" % (page, kind))
+    run_case(dev, kind, page, 2, 2, 64, [1, page, page + 1, 3 * page - 1, 333], [1, 1, 1, min(3, 3 * page - 1), 40], seed=page,
+             layout="slots" if page % 2 else "heads", pad=16 if page == 24 else 0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp8", "int8"])
+@pytest.mark.parametrize("lengths,before", [([100], [0]), ([257, 1, 64], [0, 30, 500]), ([33, 0, 129], [1000, 50, 1]), ([65], [63])])
+def test_chains(dev, kind, lengths, before):
+    """Prompts and parts of prompts."""
+    log("case chain %s %s behind %s" % (kind, lengths, before))
+    run_case(dev, kind, 16, 2, 4, 64, np.array(lengths) + before, lengths, seed=len(lengths))
+
+
+@pytest.mark.parametrize("dim", [96, 128, 256])
+def test_chains_of_wide_heads(dev, dim):
+    log("case chain dim %d" % dim)
+    run_case(dev, "bf16", 64, 1, 3, dim, [210, 90], [150, 90], seed=dim)
+    run_case(dev, "int8", 24, 1, 5, dim, [210, 90], [150, 90], seed=dim + 1)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "int8"])
+@pytest.mark.parametrize("shape", ["chain", "star", "threads", "tree", "random", "empty"])
+def test_trees(dev, kind, shape):
+    log("case tree %s %s" % (shape, kind))
+    # trees behind prefixes of every kind, one without a prefix, one that is longer than a mask word
+    run_case(dev, kind, 16, 2, 3, 64, [8, 40, 100, 267, 1], [8, 13, 70, 3, 1], shape=shape, seed=5)
+    run_case(dev, kind, 24, 1, 4, 128, [300, 150], [150, 150], shape=shape, seed=6)
+
+
+@pytest.mark.parametrize("kind", ["fp16", "fp8"])
+def test_newest_nodes_of_a_larger_tree(dev, kind):
+    """Beams: the queries are the last nodes of a tree that has grown for many steps; a row without any prefix."""
+    log("case beams %s" % kind)
+    run_case(dev, kind, 16, 2, 4, 64, [700, 90, 64], [4, 8, 1], shape="tree", tree_lens=[640, 90, 64], seed=8)
+    run_case(dev, kind, 16, 1, 2, 128, [2000], [40], shape="threads", tree_lens=[1999], seed=9)
+
+
+def test_tokens_without_positions(dev):
+    """No position at all: an empty row, a chain whose cache is shorter than the chain, a tree of nobody."""
+    log("case empty rows")
+    out, lse = run_case(dev, "bf16", 16, 2, 2, 64, [0, 3, 0], [2, 5, 0], seed=1)
+    assert torch.all(out[1:3] == 0) and torch.all(lse[1:3] == -float("inf"))
+    out, lse = run_case(dev, "int8", 16, 2, 2, 64, [6, 0], [6, 0], shape="empty", seed=2)
+    assert torch.all(out[1:7:2] == 0) and torch.all(lse[1:7:2] == -float("inf"))
+
+
+def test_odd_strides(dev):
+    log("case odd strides")
+    for kind in ("bf16", "fp16", "fp8"):
+        run_case(dev, kind, 16, 2, 3, 64, [70, 300], [3, 200], odd=True, seed=3)
+        run_case(dev, kind, 16, 2, 3, 80, [70, 300], [1, 1], odd=True, seed=4)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp8", "int8"])
+@pytest.mark.parametrize("lengths", [[4, 9], [90, 130]])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_not_seen_changes_nothing(dev, kind, lengths, bad):
+    """NaN and infinities in keys and values of positions that some tokens see and others do not: the tokens that do not
+    see them get what they would get without them (and the cache behind every row holds NaN anyway)."""
+    log("case masked %s %s %s" % (kind, lengths, bad))
+    rng = np.random.default_rng(1)
+
+    def values(i, n):
+        x = rng.standard_normal((2, n, 2, 64))
+        at = n - 1 - rng.integers(0, min(n, lengths[i]), 3)
+        x[1, at[0], :, 3] = bad       # one value of a head
+        x[1, at[1], 1, :] = -bad      # a whole head
+        if np.isnan(bad):
+            x[0, at[2], 0, 7] = bad   # a key
+        return x
+
+    for shape in (None, "tree", "empty"):
+        run_case(dev, kind, 16, 2, 4, 64, [lengths[0] + 37, lengths[1]], lengths, shape=shape, seed=11, values=values, given="bf16" if kind != "fp16" else None)
+
+
+def test_large_and_small_scores(dev):
+    """Scores far from zero (weights that all but one position lose) and a scale of zero (equal weights)."""
+    log("case scores")
+    big = lambda i, n: np.random.default_rng(i).standard_normal((2, n, 1, 64)) * np.array([30.0, 1.0])[:, None, None, None]  # noqa: E731
+    run_case(dev, "bf16", 16, 1, 4, 64, [200, 90], [1, 60], values=big, scale=1.0, seed=2)
+    run_case(dev, "fp8", 16, 1, 4, 64, [200, 90], [1, 60], values=big, scale=-0.5, seed=2)
+    run_case(dev, "fp16", 16, 1, 4, 64, [200, 90], [1, 60], scale=0.0, seed=2)
+
+
+def test_long_rows_of_few_tokens(dev):
+    """Long caches are taken in parts that are joined afterwards."""
+    log("case long rows")
+    run_case(dev, "fp8", 64, 2, 2, 64, [9000, 4001, 17], [1, 1, 1], seed=4)
+    run_case(dev, "bf16", 16, 1, 4, 128, [6000], [5], shape="tree", seed=5)
+    run_case(dev, "int8", 16, 1, 16, 64, [5000, 100], [9, 7], seed=6)
+
+
+def test_rows_and_pages_that_are_bad(dev):
+    log("case bad rows")
+    P = Paged(dev, [40] * 6, 8, 2, 64, "bf16", seed=3)
+    rng = np.random.default_rng(0)
+    P.fill(lambda i, n: rng.standard_normal((2, n, 2, 64)))
+    rows, total, starts = P.rows([2] * 6)
+    lengths, kv, st, pages = (t.clone() for t in (rows.lengths, rows.kv_lens, rows.starts, rows.pages))
+    lengths[1] = 3             # more than the bound
+    kv[2] = 41                 # more positions than the bound
+    st[3] = -1
+    pages[4, 3] = P.n_pages    # behind the pool
+    rows = rows._replace(lengths=lengths, kv_lens=kv, starts=st, pages=pages)
+    q = torch.randn(total, 4, 64, device=dev, dtype=torch.bfloat16)
+    status = torch.zeros(6, dtype=torch.int32, device=dev)
+    out = torch.full_like(q, 3.0)
+    _, lse = PX.tree_attention(q, P.cache, rows, out=out, lse=True, status=status)
+    assert status.cpu().tolist() == [0, PX.KV_BAD_ROW, PX.KV_BAD_ROW, PX.KV_BAD_ROW, PX.KV_BAD_PAGE, 0]
+    got = out.cpu().float()
+    assert torch.all(got[2:4] == 3.0) and torch.all(got[6:8] == 3.0)  # whose tokens are not known
+    assert torch.isnan(got[4:6]).all() and torch.isnan(got[8:10]).all() and torch.isnan(lse[8:10]).all()
+    for i in (0, 5):
+        o, z, ot, zt = D.attention(q[2 * i: 2 * i + 2].cpu().double().numpy(), *P.held[i], D.visible(40, 2), 0.125, 7, 7)
+        assert np.all(np.abs(got[2 * i: 2 * i + 2].numpy() - o) <= ot)
+    # a tree longer than its mask
+    mask = torch.full((total, 1), -1, dtype=torch.int64, device=dev)
+    rows, total, starts = P.rows([2] * 6)
+    trees = torch.tensor([2, 40, 65, -1, 41, 0], dtype=torch.int32, device=dev)
+    status.zero_()
+    PX.tree_attention(q, P.cache, rows, mask=mask, tree_lens=trees, status=status)
+    b = PX.KV_BAD_ROW
+    assert status.cpu().tolist() == [0, 0, b, b, b, 0]
+
+
+def test_offsets_beyond_32_bits(dev):
+    """Pages whose elements lie behind 2^32 of the pool's first, for one token and for a chain."""
+    log("case long offsets")
+    n_pages, page, heads, dim = 270_000, 16, 4, 256
+    cache = PX.kv_alloc(n_pages, page, heads, dim, torch.float16, dev)
+    far = cache.k.numel() > 1 << 32
+    assert far
+    table = [n_pages - 1, 0, n_pages - 2, 7, n_pages - 9]
+    rng = np.random.default_rng(0)
+    kv = 75
+    held = torch.as_tensor(rng.standard_normal((2, kv, heads, dim))).to(torch.float16)
+    for p in range(kv):
+        cache.k[table[p // page], p % page], cache.v[table[p // page], p % page] = held[0, p].to(dev), held[1, p].to(dev)
+    one = lambda v, dt: torch.tensor(v, dtype=dt, device=dev)  # noqa: E731
+    for n in (1, 70):
+        rows = PX.KVRows(one([0], torch.int64), one([n], torch.int32), one([kv], torch.int32), one([table], torch.int32), n, kv)
+        q = torch.as_tensor(rng.standard_normal((n, 8, dim))).to(torch.float16)
+        got = PX.tree_attention(q.to(dev), cache, rows).cpu().double().numpy()
+        o, _, tol, _ = D.attention(q.double().numpy(), held[0].double().numpy(), held[1].double().numpy(), D.visible(kv, n), dim ** -0.5, 10, 10)
+        far = np.abs(got - o) / tol
+        assert far.max() <= 1
+
+
+def test_on_another_stream_and_in_a_graph(dev):
+    """A side stream, and a graph replayed with other work between the replays."""
+    log("case streams and graphs")
+    P = Paged(dev, [3000, 500], 16, 2, 64, "fp8", seed=3)
+    rng = np.random.default_rng(0)
+    P.fill(lambda i, n: rng.standard_normal((2, n, 2, 64)))
+    rows, total, _ = P.rows([3, 4])
+    q = torch.randn(total, 8, 64, device=dev, dtype=torch.bfloat16)
+    want, lse = PX.tree_attention(q, P.cache, rows, lse=True)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = PX.tree_attention(q, P.cache, rows)
+    s.synchronize()
+    assert torch.equal(got, want)
+    ws = torch.empty(PX.tree_attention_workspace_size(P.cache, rows, total, 8), dtype=torch.uint8, device=dev)
+    out, z = torch.empty_like(q), torch.empty_like(lse)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        PX.tree_attention(q, P.cache, rows, out=out, lse=z, workspace=ws)
+    for _ in range(3):
+        out.zero_()
+        ws.fill_(0xFF)
+        (torch.randn(1000, device=dev) * 2).sum().item()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(z, lse)
