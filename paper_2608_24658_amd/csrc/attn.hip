@@ -8,6 +8,69 @@
 using abi::aligned;
 using abi::cu_count;
 
+namespace {
+
+typedef void (*TreeKernel)(pk::TreeArgs);
+
+template <int DP, int WQ>
+TreeKernel pick_kind(bool f16, int kind)
+{
+    switch (kind) {
+    case pk::KV_BF16: return pk::tree_attention<DP, WQ, false, pk::KV_BF16>;
+    case pk::KV_F16: return pk::tree_attention<DP, WQ, true, pk::KV_F16>;
+    case pk::KV_FP8: return f16 ? pk::tree_attention<DP, WQ, true, pk::KV_FP8> : pk::tree_attention<DP, WQ, false, pk::KV_FP8>;
+    default: return f16 ? pk::tree_attention<DP, WQ, true, pk::KV_INT8> : pk::tree_attention<DP, WQ, false, pk::KV_INT8>;
+    }
+}
+
+TreeKernel pick(int dim, int cols, bool f16, int kind)
+{
+    if (dim <= 64) return cols == 32 ? pick_kind<64, 1>(f16, kind) : pick_kind<64, 4>(f16, kind);
+    if (dim <= 128) return cols == 32 ? pick_kind<128, 1>(f16, kind) : pick_kind<128, 4>(f16, kind);
+    return cols == 32 ? pick_kind<256, 1>(f16, kind) : pick_kind<256, 4>(f16, kind);
+}
+
+/* How a call is cut into blocks: by its sizes and bounds alone, so that the
+ * workspace can be sized without a GPU. */
+struct TreePlan {
+    int32_t cols, q_blocks, parts, part_len;
+    int64_t units, blocks;
+    bool by_xcd;
+    size_t ml, end; /* workspace: the parts' vectors at 0, their maxima and sums at ml */
+};
+
+constexpr int64_t PART_BLOCKS = 2048;            /* blocks that a call is cut into */
+constexpr size_t PART_BYTES = (size_t)1 << 29;   /* of the parts' vectors */
+
+int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads, TreePlan *p)
+{
+    const int64_t group = n_q_heads / c->n_heads, cols = (int64_t)r->max_length * group;
+    if (cols > INT32_MAX) return PARASON_ERR_SIZE;
+    p->cols = cols <= 32 ? 32 : 128;
+    p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
+    const int64_t base = r->n_rows * c->n_heads * p->q_blocks;
+    const int64_t tile = p->cols == 32 ? 128 : 64;
+    int64_t len = 4096;
+    while (len > 2 * tile && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
+    const size_t per_part = (size_t)r->n_tokens * n_q_heads * c->head_dim * 4;
+    int64_t parts = (r->max_kv_len + len - 1) / len;
+    if (parts < 1 || base >= PART_BLOCKS) parts = 1;
+    if (per_part > 0 && (size_t)parts > PART_BYTES / per_part) parts = PART_BYTES / per_part > 1 ? (int64_t)(PART_BYTES / per_part) : 1;
+    len = (r->max_kv_len + parts - 1) / parts;
+    p->part_len = (int32_t)((len + tile - 1) / tile * tile < INT32_MAX ? (len + tile - 1) / tile * tile : len);
+    if (p->part_len < tile) p->part_len = (int32_t)tile;
+    p->parts = (int32_t)parts;
+    p->units = r->n_rows * c->n_heads * parts;
+    p->by_xcd = p->q_blocks > 1 && p->units >= 8;
+    p->blocks = (p->by_xcd ? (p->units + 7) / 8 * 8 : p->units) * p->q_blocks;
+    if (p->blocks > INT32_MAX) return PARASON_ERR_SIZE;
+    p->ml = parts > 1 ? abi::align_up(per_part * parts) : 0;
+    p->end = parts > 1 ? p->ml + abi::align_up((size_t)r->n_tokens * n_q_heads * 8 * parts) : abi::ALIGN;
+    return PARASON_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 int parason_tree_attention_workspace_size(const parason_kv_cache *cache, const parason_kv_rows *rows,
@@ -21,8 +84,10 @@ int parason_tree_attention_workspace_size(const parason_kv_cache *cache, const p
     rc = abi::check_row_sizes(rows);
     if (rc != PARASON_OK) return rc;
     if (n_q_heads < 1 || n_q_heads > PARASON_KV_MAX_HEADS || n_q_heads % cache->n_heads != 0) return PARASON_ERR_SIZE;
-    *bytes = abi::ALIGN;
-    return PARASON_OK;
+    TreePlan p;
+    rc = plan(cache, rows, n_q_heads, &p);
+    if (rc == PARASON_OK) *bytes = p.end;
+    return rc;
 }
 
 int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows *rows, const parason_tree_args *args,
@@ -30,41 +95,59 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
 {
     if (!args) return PARASON_ERR_NULL;
     pk::TreeArgs a;
-    int rc = abi::check_cache(cache, &a.c, &a.kind);
+    int kind;
+    int rc = abi::check_cache(cache, &a.c, &kind);
     if (rc != PARASON_OK) return rc;
     rc = abi::check_rows(rows, row_status, &a.r);
     if (rc != PARASON_OK) return rc;
     if (args->dtype != PARASON_DTYPE_BF16 && args->dtype != PARASON_DTYPE_F16) return PARASON_ERR_PARAM;
-    if ((a.kind == pk::KV_BF16 && args->dtype != PARASON_DTYPE_BF16) ||
-        (a.kind == pk::KV_F16 && args->dtype != PARASON_DTYPE_F16) || !std::isfinite(args->scale) ||
+    if ((kind == pk::KV_BF16 && args->dtype != PARASON_DTYPE_BF16) ||
+        (kind == pk::KV_F16 && args->dtype != PARASON_DTYPE_F16) || !std::isfinite(args->scale) ||
         (!args->mask && args->tree_lens))
         return PARASON_ERR_PARAM;
-    size_t need;
-    rc = parason_tree_attention_workspace_size(cache, rows, args->n_q_heads, &need);
-    if (rc != PARASON_OK) return rc;
-    if (!abi::stride_fits(args->q_stride_token, rows->n_tokens) || !abi::stride_fits(args->q_stride_head, args->n_q_heads) ||
-        !abi::stride_fits(args->out_stride_token, rows->n_tokens) || !abi::stride_fits(args->out_stride_head, args->n_q_heads) ||
+    const int32_t heads = args->n_q_heads;
+    if (heads < 1 || heads > PARASON_KV_MAX_HEADS || heads % cache->n_heads != 0) return PARASON_ERR_SIZE;
+    if (!abi::stride_fits(args->q_stride_token, rows->n_tokens) || !abi::stride_fits(args->q_stride_head, heads) ||
+        !abi::stride_fits(args->out_stride_token, rows->n_tokens) || !abi::stride_fits(args->out_stride_head, heads) ||
         (args->mask && (args->mask_words < 0 || !abi::stride_fits(args->mask_stride, rows->n_tokens))))
         return PARASON_ERR_SIZE;
+    TreePlan p;
+    rc = plan(cache, rows, heads, &p);
+    if (rc != PARASON_OK) return rc;
     if (rows->n_rows == 0 || rows->n_tokens == 0 || rows->max_length == 0) return PARASON_OK;
     if (!args->q || !args->out || !workspace) return PARASON_ERR_NULL;
     if (!aligned(args->q, 2) || !aligned(args->out, 2) || !aligned(args->lse, 4) || !aligned(args->mask, 8) ||
         !aligned(args->tree_lens, 4) || !aligned(workspace, abi::ALIGN))
         return PARASON_ERR_ALIGN;
-    if (workspace_bytes < need) return PARASON_ERR_WORKSPACE;
+    if (workspace_bytes < p.end) return PARASON_ERR_WORKSPACE;
     if (cu_count() <= 0) return PARASON_ERR_DEVICE;
 
     a.q = (const char *)args->q, a.out = (char *)args->out, a.lse = args->lse;
     a.q_stride_token = args->q_stride_token, a.q_stride_head = args->q_stride_head;
     a.out_stride_token = args->out_stride_token, a.out_stride_head = args->out_stride_head;
+    a.q_wide = aligned(args->q, 16) && args->q_stride_token % 8 == 0 && args->q_stride_head % 8 == 0;
+    a.out_wide = aligned(args->out, 8) && args->out_stride_token % 4 == 0 && args->out_stride_head % 4 == 0;
     a.mask = args->mask, a.mask_stride = args->mask_stride, a.mask_words = args->mask_words;
     a.tree_lens = args->tree_lens;
-    a.n_q_heads = args->n_q_heads;
-    a.scale = args->scale;
-    a.f16 = args->dtype == PARASON_DTYPE_F16;
-    if (rows->n_rows > INT32_MAX / rows->max_length) return PARASON_ERR_SIZE;
-    hipLaunchKernelGGL(pk::tree_attention_simple, dim3((unsigned)(rows->n_rows * rows->max_length), (unsigned)args->n_q_heads), dim3(256),
-                       0, (hipStream_t)stream_ptr, a);
+    a.n_q_heads = heads;
+    a.group = heads / cache->n_heads;
+    a.group_div = pk::fast_div((uint32_t)a.group);
+    a.negate = args->scale < 0.0f;
+    const float c2 = (float)(std::fabs((double)args->scale) * 1.4426950408889634);
+    a.c2 = c2 > 0x1p-126f ? c2 : 0x1p-126f;
+    a.q_blocks = p.q_blocks, a.parts = p.parts, a.part_len = p.part_len, a.units = p.units, a.by_xcd = p.by_xcd;
+    a.part_out = (float *)workspace;
+    a.part_ml = (float2 *)((char *)workspace + p.ml);
+    const bool f16 = args->dtype == PARASON_DTYPE_F16;
+    hipStream_t stream = (hipStream_t)stream_ptr;
+    hipLaunchKernelGGL(pick(cache->head_dim, p.cols, f16, kind), dim3((unsigned)p.blocks), dim3(pk::TREE_THREADS), 0, stream, a);
+    if (p.parts > 1) {
+        constexpr int64_t per_block = pk::TREE_THREADS / 64;
+        const int64_t waves = rows->n_rows * rows->max_length * heads;
+        if (waves / per_block >= INT32_MAX) return PARASON_ERR_SIZE;
+        hipLaunchKernelGGL(f16 ? pk::tree_join<true> : pk::tree_join<false>, dim3((unsigned)((waves + per_block - 1) / per_block)),
+                           dim3(pk::TREE_THREADS), 0, stream, a, p.cols);
+    }
     return hipGetLastError() == hipSuccess ? PARASON_OK : PARASON_ERR_HIP;
 }
 

@@ -1,6 +1,23 @@
 /*
  * attn_kernels.h -- attention of a tree of tokens over the paged cache for
  * gfx950.
+ *
+ * A block takes the query heads that share a cache head, of neighbouring tokens
+ * of one row, as the columns of its products, and runs over tiles of positions:
+ *   S^T = K Q^T,   P^T = exp2(c S^T - max),   O^T += V^T P^T.
+ * In S^T a lane of the 32x32 product holds 16 positions of one query, so the
+ * maximum and the sum of a softmax are within the lane but for one exchange
+ * with the lane 32 away, and P^T is already the right operand of the second
+ * product: the 8 positions that a lane holds of each 16 are not consecutive
+ * (0-3 and 8-11, or 4-7 and 12-15), which the rows of V^T are read to match.
+ * V stays row by row in LDS; its transposed reads come from the LDS itself.
+ *
+ * Two shapes.  Few queries (up to 32 columns: single tokens, beams, short
+ * drafts): the four waves take a quarter of each tile's positions each and are
+ * joined at the end; what bounds it is reading the cache once.  More queries:
+ * the waves take 32 columns each and share the tile; bound by the products and
+ * the exponentials.  Long rows are cut into parts, whose results
+ * tree_join puts together.
  */
 #pragma once
 #include "kv_common.h"
@@ -13,112 +30,637 @@ struct TreeArgs {
     const char *q;
     char *out;
     float *lse;
-    int64_t q_stride_token, q_stride_head, out_stride_token, out_stride_head;
+    int64_t q_stride_token, q_stride_head, out_stride_token, out_stride_head; /* elements */
     const uint64_t *mask;
     int64_t mask_stride;
     const int32_t *tree_lens;
-    int32_t mask_words, n_q_heads;
-    float scale;
-    bool f16;
-    int kind;
+    int32_t mask_words, n_q_heads, group;
+    FastDiv group_div;
+    float c2;            /* |scale| * log2(e), at least 2^-126 */
+    bool negate;         /* scale < 0: the queries change their sign instead */
+    bool q_wide, out_wide; /* queries in 16-byte, outputs in 8-byte pieces */
+    int32_t q_blocks;    /* blocks of columns of a row and head */
+    int32_t parts;       /* parts of a row's positions, part_len each (the last block of a row: the rest) */
+    int32_t part_len;
+    int64_t units;       /* rows * cache heads * parts */
+    bool by_xcd;
+    float *part_out;     /* [n_tokens * n_q_heads][parts][head_dim] */
+    float2 *part_ml;     /* [n_tokens * n_q_heads][parts]: exponent of the maximum, sum */
 };
 
-__device__ __forceinline__ float to_f32(const char *p, bool f16)
+typedef short frag8 __attribute__((ext_vector_type(8)));
+typedef short frag4 __attribute__((ext_vector_type(4)));
+typedef float acc16 __attribute__((ext_vector_type(16)));
+
+template <bool F16>
+__device__ __forceinline__ acc16 mma(frag8 a, frag8 b, acc16 c)
 {
-    const uint32_t h = *reinterpret_cast<const uint16_t *>(p);
-    return f16 ? f16_to_f32(h) : bf16_to_f32(h);
+    typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+    if (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
 }
 
-__device__ __forceinline__ float cached(const char *base, int64_t at, int kind)
+/* Two floats to two 16-bit values, rounded to nearest even. */
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float x, float y)
 {
-    if (kind == KV_BF16 || kind == KV_F16) return to_f32(base + at * 2, kind == KV_F16);
-    float x[4];
-    const uint32_t w = (uint8_t)base[at];
-    if (kind == KV_FP8) fp8x4_to_f32(w, x);
-    else int8x4_to_f32(w, x);
-    return x[0];
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    if (F16) return __builtin_bit_cast(uint32_t, h2{(_Float16)x, (_Float16)y});
+    return __builtin_bit_cast(uint32_t, b2{(__bf16)x, (__bf16)y});
 }
 
-/* One block per (token, query head): 256 positions at a time, a thread for
- * each; then a thread for each value of the head. */
-__global__ void __launch_bounds__(256) tree_attention_simple(TreeArgs a)
+/* Four codes to four 16-bit values: exact in either type. */
+template <bool F16, int KIND>
+__device__ __forceinline__ uint2 widen4(uint32_t w)
 {
-    __shared__ float qs[PARASON_KV_MAX_DIM], ps[256], red[8];
-    __shared__ int64_t at_v[256];
-    const int64_t row = blockIdx.x / (uint32_t)a.r.max_length;
-    const int32_t j = (int32_t)(blockIdx.x % (uint32_t)a.r.max_length);
-    const int head = (int)blockIdx.y, kv_head = head / (a.n_q_heads / a.c.n_heads);
-    const int tid = (int)threadIdx.x, D = a.c.head_dim;
-    const KvRow w = load_row(a.r, a.c, row, false);
-    if (!w.out_ok) {
-        if (tid == 0) report(a.r, row, PARASON_KV_BAD_ROW);
-        return;
+    if (KIND == KV_FP8) {
+        if (F16)
+            return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)),
+                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)));
+        return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
     }
-    if (j >= w.length) return;
-    const int64_t t = w.start + j;
-    const int32_t tree = a.mask ? (a.tree_lens ? a.tree_lens[row] : w.length) : 0;
-    const bool ok = w.ok && (!a.mask || (tree >= 0 && tree <= w.kv_len && (tree + 63) / 64 <= a.mask_words));
-    if (!ok && tid == 0) report(a.r, row, PARASON_KV_BAD_ROW);
-    const int32_t base = w.kv_len - tree;
-    const int32_t end = !ok ? 0 : (a.mask ? w.kv_len : min(w.kv_len, w.kv_len - w.length + j + 1));
-    bool bad = !ok;
-    if (tid < D) qs[tid] = to_f32(a.q + (t * a.q_stride_token + head * a.q_stride_head + tid) * 2, a.f16);
-    float m = -INFINITY, l = 0.0f, o = 0.0f;
-    for (int32_t p0 = 0; p0 < end; p0 += 256) {
-        const int32_t p = p0 + tid;
-        bool seen = p < end;
-        if (seen && p >= base && a.mask)
-            seen = (a.mask[t * a.mask_stride + (p - base) / 64] >> ((p - base) & 63)) & 1;
-        float s = -INFINITY, vs = 1.0f;
-        int64_t av = 0;
-        __syncthreads();
-        if (seen) {
-            int32_t slot;
-            const int32_t page = page_of(a.r, a.c, row, p, &slot);
-            if (page < 0) {
-                report(a.r, row, PARASON_KV_BAD_PAGE);
-                s = __uint_as_float(0x7FC00000u);
-            } else {
-                av = (int64_t)page * a.c.stride_page + (int64_t)slot * a.c.stride_slot + kv_head * a.c.stride_head;
-                s = 0.0f;
-                for (int d = 0; d < D; ++d) s += qs[d] * cached(a.c.k, av + d, a.kind);
-                if (a.c.k_scale) {
-                    const int64_t as = (int64_t)page * a.c.scale_stride_page + (int64_t)slot * a.c.scale_stride_slot +
-                                       kv_head * a.c.scale_stride_head;
-                    s *= a.c.k_scale[as];
-                    vs = a.c.v_scale[as];
+    float x[4];
+    int8x4_to_f32(w, x);
+    return make_uint2(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]));
+}
+
+/* Whether one of two 16-bit values is an infinity or NaN. */
+template <bool F16>
+__device__ __forceinline__ bool not_finite2(uint32_t w)
+{
+    const uint32_t e = F16 ? 0x7C00u : 0x7F80u;
+    return (w & e) == e || ((w >> 16) & e) == e;
+}
+
+template <bool F16>
+__device__ __forceinline__ float widen1(uint16_t h) { return F16 ? f16_to_f32(h) : bf16_to_f32(h); }
+
+constexpr int TREE_THREADS = 256;
+constexpr int TREE_SKIP_WORDS = 64; /* of the list of a tree's tiles that nobody in the block sees: 2,048 tiles */
+
+template <int DP, int WQ>
+struct TreeShape {
+    static constexpr int TK = WQ == 1 ? 128 : 64;     /* positions of a tile */
+    static constexpr int KW = WQ == 1 ? 32 : 64;      /* of it, those of one wave */
+    static constexpr int SUBS = KW / 32;
+    static constexpr int COLS = 32 * WQ;              /* queries of a block */
+    /* rows of 16-bit values in LDS: 16 bytes more than a multiple of 128 spread the
+     * 16-byte reads of K over the banks, 64 bytes more the transposed reads of V */
+    static constexpr int KS = DP + 8, VS = DP + 32;
+    static constexpr int KBYTES = TK * KS * 2, VBYTES = TK * VS * 2;
+    static constexpr int OS = DP + 4;                 /* floats of a row of the waves' results when they are joined */
+    static constexpr int JOIN = WQ == 1 ? 4 * 32 * OS * 4 : 0;
+    static constexpr int TILE = KBYTES + VBYTES > JOIN ? KBYTES + VBYTES : JOIN;
+};
+
+/* What a block's columns can see of their row, the same for the main kernel and the join. */
+struct TreeSpan {
+    int32_t tree, base;  /* tree positions, and the first of them */
+    int32_t end;         /* positions that some column may see: [0, end) */
+    int32_t tok0, tok1;  /* tokens of the columns: [tok0, tok1) */
+    bool ok;
+};
+
+__device__ __forceinline__ TreeSpan tree_span(const TreeArgs &a, const KvRow &w, int64_t row, int32_t q_block, int cols)
+{
+    TreeSpan s;
+    s.tree = a.mask ? (a.tree_lens ? a.tree_lens[row] : w.length) : 0;
+    s.ok = w.ok && (!a.mask || (s.tree >= 0 && s.tree <= w.kv_len && ((int64_t)s.tree + 63) / 64 <= a.mask_words));
+    s.base = w.kv_len - s.tree;
+    const int64_t col0 = (int64_t)q_block * cols, n = (int64_t)w.length * a.group;
+    const int64_t col1 = col0 + cols < n ? col0 + cols : n;
+    s.tok0 = col0 < n ? (int32_t)div_by((uint32_t)col0, a.group_div) : w.length;
+    s.tok1 = col0 < n ? (int32_t)div_by((uint32_t)(col1 - 1), a.group_div) + 1 : w.length;
+    s.end = !s.ok ? 0 : a.mask ? w.kv_len : w.kv_len - w.length + s.tok1;
+    if (s.end < 0) s.end = 0;
+    return s;
+}
+
+__device__ __forceinline__ int32_t parts_of(const TreeArgs &a, int32_t end)
+{
+    const int32_t n = (int32_t)(((int64_t)end + a.part_len - 1) / a.part_len);
+    return n < 1 ? 1 : n < a.parts ? n : a.parts;
+}
+
+template <int DP, int WQ, bool F16, int KIND>
+__global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention(TreeArgs a)
+{
+    typedef TreeShape<DP, WQ> Sh;
+    constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
+    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
+    constexpr bool PF16 = KIND == KV_F16;   /* type of the weights and of V: bfloat16 for codes, whose scales are in the weights */
+    constexpr int VE = CODES ? 16 : 8;      /* values of a 16-byte piece of the cache */
+    constexpr int VPR = DP / VE, RPP = TREE_THREADS / VPR, NP = TK / RPP;
+    constexpr int ES = CODES ? 1 : 2;
+    constexpr int NK = DP / 16, ND = DP / 32;
+    static_assert(NP >= 1 && NP * RPP == TK, "the block's loads cover a tile");
+
+    __shared__ __attribute__((aligned(16))) char tile[Sh::TILE];
+    __shared__ __attribute__((aligned(16))) float k_sc[CODES ? TK : 4], v_sc[CODES ? TK : 4];
+    __shared__ int64_t place[TK];
+    __shared__ int32_t v_stamp[TK];
+    __shared__ uint32_t skip[TREE_SKIP_WORDS];
+    __shared__ int32_t flags[2];            /* a bad page; the last tile with a value of V that is not finite */
+    __shared__ float join_ml[2][4][32];
+    uint16_t *const Ks = reinterpret_cast<uint16_t *>(tile), *const Vs = Ks + TK * KS;
+
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = lane & 31, h = lane >> 5;
+    const int wq = WQ == 1 ? 0 : wave, wk = WQ == 1 ? wave : 0;
+
+    /* ---- which row, cache head, part and columns */
+    int64_t unit;
+    int32_t q_block;
+    if (a.by_xcd) {
+        /* blocks that read the same keys on one XCD's L2 */
+        const uint32_t x = blockIdx.x & 7u, y = blockIdx.x >> 3;
+        unit = (int64_t)(y / (uint32_t)a.q_blocks) * 8 + x;
+        q_block = (int32_t)(y % (uint32_t)a.q_blocks);
+    } else {
+        unit = blockIdx.x / (uint32_t)a.q_blocks;
+        q_block = (int32_t)(blockIdx.x % (uint32_t)a.q_blocks);
+    }
+    if (unit >= a.units) return;
+    q_block = a.q_blocks - 1 - q_block;     /* the longest of a chain first */
+    const int32_t part = (int32_t)(unit % a.parts);
+    const int32_t head = (int32_t)(unit / a.parts % a.c.n_heads);
+    const int64_t row = unit / a.parts / a.c.n_heads;
+    const KvRow w = load_row(a.r, a.c, row, false);
+    const TreeSpan sp = tree_span(a, w, row, q_block, Sh::COLS);
+    if (!sp.ok && part == 0 && head == 0 && q_block == 0 && tid == 0) report(a.r, row, PARASON_KV_BAD_ROW);
+    if (!w.out_ok || sp.tok0 >= w.length) return;
+    const int32_t my_parts = parts_of(a, sp.end);
+    if (part >= my_parts) return;
+    const int32_t k_begin = part * a.part_len;
+    const int32_t k_end = part == my_parts - 1 ? sp.end : k_begin + a.part_len;
+
+    /* ---- this lane's query */
+    const int32_t col = q_block * Sh::COLS + wq * 32 + n;
+    const int32_t tok = (int32_t)div_by((uint32_t)col, a.group_div);
+    const bool live = tok < w.length;
+    const int32_t q_head = head * a.group + (col - tok * a.group);
+    const int64_t t = w.start + (live ? tok : 0);
+    frag8 qf[NK];
+    {
+        const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + t * a.q_stride_token + (live ? q_head : 0) * a.q_stride_head;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const int d = k * 16 + h * 8;
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (live && d < a.c.head_dim) {
+                if (a.q_wide) {
+                    x = *reinterpret_cast<const uint4 *>(q + d);
+                } else {
+                    uint32_t e[8];
+                    for (int i = 0; i < 8; ++i) e[i] = q[d + i];
+                    x = make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16), e[6] | (e[7] << 16));
                 }
-                s *= a.scale;
+                if (a.negate) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
+            }
+            qf[k] = __builtin_bit_cast(frag8, x);
+        }
+    }
+    /* positions below `open` are seen by every column of the block */
+    const int32_t open = a.mask ? sp.base : w.kv_len - w.length + sp.tok0 + 1;
+    /* and this lane's own bound in a chain */
+    const int32_t my_end = a.mask ? w.kv_len : (live ? w.kv_len - w.length + tok + 1 : 0);
+    const uint64_t *const my_mask = a.mask ? a.mask + t * a.mask_stride : nullptr;
+    const int32_t tree_words = (sp.tree + 63) >> 6;
+
+    if (tid < 2) flags[tid] = -1;
+    if (tid < TREE_SKIP_WORDS) skip[tid] = 0u;
+    for (int i = tid; i < TK; i += TREE_THREADS) v_stamp[i] = -1;
+    __syncthreads();
+
+    /* ---- the tree's tiles that some column sees: bit (tile - first tile of the tree) of `skip` */
+    const int32_t tile0 = sp.base / TK;
+    if (a.mask && k_end > sp.base) {
+        const int32_t lo = k_begin > sp.base ? (k_begin - sp.base) >> 6 : 0;
+        const int32_t words = ((k_end - sp.base + 63) >> 6) - lo;
+        const int64_t total = (int64_t)words * (sp.tok1 - sp.tok0);
+        if (total > (1 << 24)) {             /* (a list of 2,048 tiles would help such a tree little) */
+            if (tid < TREE_SKIP_WORDS) skip[tid] = 0xFFFFFFFFu;
+        } else for (uint32_t i = (uint32_t)tid; i < (uint32_t)total; i += TREE_THREADS) {
+            const uint32_t j = i / (uint32_t)words;
+            const int32_t x = lo + (int32_t)(i - j * (uint32_t)words);
+            uint64_t m = a.mask[(w.start + sp.tok0 + j) * a.mask_stride + x];
+            const int32_t rest = sp.tree - x * 64;
+            if (rest < 64) m &= ~0ull >> (64 - rest);
+            if (m == 0) continue;
+            const int32_t p = sp.base + x * 64;
+            const uint32_t first = (uint32_t)((p + __builtin_ctzll(m)) / TK - tile0);
+            const uint32_t last = (uint32_t)((p + 63 - __builtin_clzll(m)) / TK - tile0);
+            if (first < TREE_SKIP_WORDS * 32) atomicOr(&skip[first >> 5], 1u << (first & 31));
+            if (last < TREE_SKIP_WORDS * 32) atomicOr(&skip[last >> 5], 1u << (last & 31));
+        }
+        __syncthreads();
+    }
+    const int32_t t_end = (k_end + TK - 1) / TK;
+    auto next_tile = [&](int32_t x) {
+        if (!a.mask) return x;
+        while (x < t_end) {
+            const uint32_t at = (uint32_t)(x - tile0);
+            /* tiles with some of the prefix, and those behind the list, count as seen */
+            if (x * TK < sp.base || at >= TREE_SKIP_WORDS * 32 || ((skip[at >> 5] >> (at & 31)) & 1u)) break;
+            ++x;
+        }
+        return x;
+    };
+
+    /* ---- loads: a position's page a tile ahead of its keys and values, these a tile ahead of their use */
+    const int32_t my_piece = tid % VPR, my_row = tid / VPR;
+    const bool piece_live = my_piece * VE < a.c.head_dim;
+    const char *const kb = a.c.k + ((int64_t)head * a.c.stride_head + my_piece * VE) * ES;
+    const char *const vb = a.c.v + ((int64_t)head * a.c.stride_head + my_piece * VE) * ES;
+    int32_t pg = -1, pg_slot = 0;            /* of position tid of a tile */
+    auto load_page = [&](int32_t x) {
+        const int32_t p = x * TK + tid;
+        pg = -1;
+        if (tid < TK && p < k_end) {
+            const uint32_t nth = div_by((uint32_t)p, a.c.page_div);
+            pg_slot = p - (int32_t)(nth * (uint32_t)a.c.page_size);
+            pg = a.r.pages[row * a.r.pages_stride + nth];
+            if (pg < 0 || pg >= a.c.n_pages) pg = -2;
+        }
+    };
+    float ks_next = 0.0f, vs_next = 0.0f;
+    auto put_place = [&]() {
+        if (tid < TK) {
+            if (pg == -2) flags[0] = 0;
+            place[tid] = pg < 0 ? -1 : (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
+            if (CODES) {
+                ks_next = vs_next = 0.0f;
+                if (pg >= 0) {
+                    const int64_t at = (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
+                                       (int64_t)head * a.c.scale_stride_head;
+                    ks_next = a.c.k_scale[at];
+                    vs_next = a.c.v_scale[at];
+                }
             }
         }
-        float top = s;
-        for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-        if ((tid & 63) == 0) red[tid >> 6] = top;
-        at_v[tid] = seen ? av : -1;
+    };
+    uint4 kr[NP], vr[NP];
+    auto load_tile = [&]() {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int64_t at = place[my_row + p * RPP];
+            kr[p] = vr[p] = make_uint4(0u, 0u, 0u, 0u);
+            if (at >= 0 && piece_live) {
+                kr[p] = *reinterpret_cast<const uint4 *>(kb + at * ES);
+                vr[p] = *reinterpret_cast<const uint4 *>(vb + at * ES);
+            }
+        }
+    };
+    uint64_t m_lo = 0, m_hi = 0;             /* mask words of a tile's positions of this wave */
+    auto load_mask = [&](int32_t x) {
+        const int32_t b = x * TK + wk * 32 - sp.base;
+        m_lo = m_hi = 0;
+        if (a.mask && live && b + Sh::KW > 0) {
+            const int32_t i = b < 0 ? 0 : b >> 6;
+            if (i < tree_words) m_lo = my_mask[i];
+            if (b >= 0 && i + 1 < tree_words) m_hi = my_mask[i + 1];
+        }
+    };
+
+    acc16 o[ND] = {};
+    float mc = -INFINITY, l = 0.0f;          /* c2 * maximum; this lane's share of the sum */
+
+    int32_t x = next_tile(k_begin / TK);
+    if (x < t_end) {
+        load_page(x);
+        put_place();
         __syncthreads();
-        const float m_new = fmaxf(fmaxf(fmaxf(m, red[0]), red[1]), fmaxf(red[2], red[3]));
-        const float ref = m_new == -INFINITY ? 0.0f : m_new;
-        const float e = seen ? __expf(s - ref) : 0.0f;
-        ps[tid] = e * vs;
-        float sum = e;
-        for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-        if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
+        load_tile();
+        load_mask(x);
         __syncthreads();
-        const float corr = m == -INFINITY ? 0.0f : __expf(m - ref);
-        l = l * corr + red[4] + red[5] + red[6] + red[7];
-        o *= corr;
-        m = m_new;
-        if (tid < D)
-            for (int k = 0; k < min(256, end - p0); ++k)
-                if (at_v[k] >= 0) o += ps[k] * cached(a.c.v, at_v[k] + tid, a.kind);
     }
-    if (bad) o = l = __uint_as_float(0x7FC00000u);
-    const float r = l == 0.0f ? 0.0f : o / l;
-    if (tid < D) {
-        uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + t * a.out_stride_token + head * a.out_stride_head + tid;
-        *dst = (uint16_t)(a.f16 ? f32_to_f16(r) : f32_to_bf16(r));
+    int32_t x1 = x < t_end ? next_tile(x + 1) : t_end;
+    float ks_now = ks_next, vs_now = vs_next;
+    if (x1 < t_end) load_page(x1);
+    while (x < t_end) {
+        const int32_t kp = x * TK;
+        const bool masked = kp + TK > open || kp + TK > k_end; /* some column does not see all of the tile */
+        /* ---- the tile goes to LDS */
+        if (x1 < t_end) put_place();         /* (nobody reads the tile's places any more) */
+        if (CODES && tid < TK) k_sc[tid] = ks_now, v_sc[tid] = vs_now;
+        ks_now = ks_next, vs_now = vs_next;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int r = my_row + p * RPP;
+            if (CODES) {
+                const uint32_t kw[4] = {kr[p].x, kr[p].y, kr[p].z, kr[p].w}, vw[4] = {vr[p].x, vr[p].y, vr[p].z, vr[p].w};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint2 k0 = widen4<F16, KIND>(kw[2 * i]), k1 = widen4<F16, KIND>(kw[2 * i + 1]);
+                    *reinterpret_cast<uint4 *>(Ks + r * KS + my_piece * VE + 8 * i) = make_uint4(k0.x, k0.y, k1.x, k1.y);
+                    const uint2 v0 = widen4<PF16, KIND>(vw[2 * i]), v1 = widen4<PF16, KIND>(vw[2 * i + 1]);
+                    *reinterpret_cast<uint4 *>(Vs + r * VS + my_piece * VE + 8 * i) = make_uint4(v0.x, v0.y, v1.x, v1.y);
+                    if (KIND == KV_FP8 && masked &&
+                        (not_finite2<PF16>(v0.x) || not_finite2<PF16>(v0.y) || not_finite2<PF16>(v1.x) || not_finite2<PF16>(v1.y)))
+                        v_stamp[r] = flags[1] = x;
+                }
+            } else {
+                *reinterpret_cast<uint4 *>(Ks + r * KS + my_piece * VE) = kr[p];
+                *reinterpret_cast<uint4 *>(Vs + r * VS + my_piece * VE) = vr[p];
+                if (masked && (not_finite2<PF16>(vr[p].x) || not_finite2<PF16>(vr[p].y) || not_finite2<PF16>(vr[p].z) ||
+                               not_finite2<PF16>(vr[p].w)))
+                    v_stamp[r] = flags[1] = x;
+            }
+        }
+        const uint64_t lo = m_lo, hi = m_hi;
+        __syncthreads();
+        /* ---- the next tile is on its way */
+        const int32_t x2 = x1 < t_end ? next_tile(x1 + 1) : t_end;
+        if (x1 < t_end) {
+            load_tile();
+            load_mask(x1);
+            if (x2 < t_end) load_page(x2);
+        }
+        /* ---- S^T */
+        acc16 s[SUBS];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+            s[u] = acc16{};
+            const uint16_t *ka = Ks + (wk * 32 + u * 32 + n) * KS + h * 8;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) s[u] = mma<F16>(*reinterpret_cast<const frag8 *>(ka + k * 16), qf[k], s[u]);
+            if (CODES) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 f = *reinterpret_cast<const float4 *>(&k_sc[wk * 32 + u * 32 + 8 * i + 4 * h]);
+                    s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
+                }
+            }
+        }
+        /* ---- what this lane's query sees of the wave's positions, from bit 0 on */
+        uint32_t see[SUBS];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) see[u] = 0xFFFFFFFFu;
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                const int32_t p0 = kp + wk * 32 + u * 32;
+                const int32_t left = (my_end < k_end ? my_end : k_end) - p0;
+                uint32_t m = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
+                if (a.mask) {
+                    const int32_t b = p0 - sp.base;         /* of the wave's first word: u * 32 less */
+                    const int32_t b0 = b - u * 32;
+                    uint32_t tm;
+                    if (b <= -32) {
+                        tm = 0xFFFFFFFFu;
+                    } else if (b < 0) {
+                        tm = ((uint32_t)lo << -b) | ((1u << -b) - 1u);
+                    } else {
+                        /* lo holds word b0 / 64 (word 0 where the wave's positions begin in the prefix) */
+                        const int32_t sh = b0 < 0 ? b : (b0 & 63) + u * 32;
+                        tm = sh < 64 ? (uint32_t)(lo >> sh) | (sh > 32 ? (uint32_t)(hi << (64 - sh)) : 0u)
+                                     : (uint32_t)(hi >> (sh - 64));
+                    }
+                    m &= tm;
+                }
+                see[u] = m;
+                const uint32_t mine = m >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!((mine >> (8 * (r / 4) + (r & 3))) & 1u)) s[u][r] = -INFINITY;
+            }
+        }
+        /* ---- maximum, weights, sum */
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mc_new = fmaxf(mc, top * a.c2);
+        const float ref = mc_new == -INFINITY ? 0.0f : mc_new;
+        if (__ballot(mc_new > mc)) {
+            const float corr = __builtin_amdgcn_exp2f(mc - ref);
+            l *= corr;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= corr;
+            mc = mc_new;
+        }
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c2, -ref));
+                l += s[u][r];
+            }
+        if (CODES) {
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                const uint32_t mine = see[u] >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 f = *reinterpret_cast<const float4 *>(&v_sc[wk * 32 + u * 32 + 8 * i + 4 * h]);
+                    s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
+                }
+                if (masked) {                /* no scale, whatever it is, makes a weight where nothing is seen */
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!((mine >> (8 * (r / 4) + (r & 3))) & 1u)) s[u][r] = 0.0f;
+                }
+            }
+        }
+        /* ---- O^T */
+        const bool odd_values = masked && flags[1] == x;
+        const uint16_t *va = Vs + (wk * 32 + 4 * h + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t pw[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pw[i] = pack2<PF16>(s[u][8 * k + 2 * i], s[u][8 * k + 2 * i + 1]);
+                const frag8 pf = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    typedef __attribute__((address_space(3))) frag4 lds4;
+                    const uint16_t *v0 = va + (u * 32 + k * 16) * VS + d * 32;
+                    const frag4 f0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)v0);
+                    const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + 8 * VS));
+                    frag8 vf = __builtin_shufflevector(f0, f1, 0, 1, 2, 3, 4, 5, 6, 7);
+                    if (odd_values) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (not_finite2<PF16>((uint16_t)vf[i])) vf[i] = 0;
+                    }
+                    o[d] = mma<PF16>(vf, pf, o[d]);
+                }
+            }
+        }
+        if (odd_values) {
+            /* infinities and NaN of V reach only the queries that see them: a product by zero would not do.  They
+             * were left out above and are added one position at a time. */
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                for (int kk = 0; kk < 32; ++kk) {
+                    const int r = wk * 32 + u * 32 + kk;
+                    if (v_stamp[r] != x) continue;
+                    float p = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p = ((kk >> 3) * 4 + (kk & 3)) == i ? s[u][i] : p;
+                    p = __shfl(p, n + 32 * ((kk >> 2) & 1));
+                    if (!((see[u] >> kk) & 1u)) continue;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint16_t v = Vs[r * VS + d * 32 + 8 * (i / 4) + 4 * h + (i & 3)];
+                            if (not_finite2<PF16>(v)) o[d][i] += p * widen1<PF16>(v);
+                        }
+                }
+            }
+        }
+        __syncthreads();
+        x = x1;
+        x1 = x2;
     }
-    if (tid == 0 && a.lse) a.lse[t * a.n_q_heads + head] = l == 0.0f ? -INFINITY : m + logf(l);
+    __syncthreads();
+    const bool bad = !sp.ok || flags[0] == 0;
+    if (flags[0] == 0 && tid == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
+
+    /* ---- results */
+    l += __shfl_xor(l, 32);
+    const float nan = __uint_as_float(0x7FC00000u);
+    if (WQ == 1) {
+        /* join the waves: every column's maximum and sum over the four, then their shares of O */
+        float *const Os = reinterpret_cast<float *>(tile);
+        if (h == 0) join_ml[0][wave][n] = mc, join_ml[1][wave][n] = l;
+        __syncthreads();
+        float m4 = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m4 = fmaxf(m4, join_ml[0][i][n]);
+        const float ref = m4 == -INFINITY ? 0.0f : m4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += join_ml[1][i][n] * __builtin_amdgcn_exp2f(join_ml[0][i][n] - ref);
+        const float f = __builtin_amdgcn_exp2f(mc - ref);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4 *>(&Os[(wave * 32 + n) * Sh::OS + d * 32 + 8 * i + 4 * h]) =
+                    make_float4(o[d][4 * i] * f, o[d][4 * i + 1] * f, o[d][4 * i + 2] * f, o[d][4 * i + 3] * f);
+        if (bad) sum = nan;
+        __syncthreads();
+        if (wave == 0 && h == 0) join_ml[0][0][n] = m4, join_ml[1][0][n] = sum;
+        __syncthreads();
+        const int D4 = a.c.head_dim / 4, cols = (sp.tok1 - sp.tok0) * a.group;
+        for (int i = tid; i < cols * D4; i += TREE_THREADS) {
+            const int c = i / D4, d = (i - c * D4) * 4;
+            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 z = *reinterpret_cast<const float4 *>(&Os[(k * 32 + c) * Sh::OS + d]);
+                y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
+            }
+            const float m_c = join_ml[0][0][c], s_c = join_ml[1][0][c];
+            const int32_t tk = (int32_t)div_by((uint32_t)(q_block * Sh::COLS + c), a.group_div);
+            const int32_t qh = head * a.group + (q_block * Sh::COLS + c - tk * a.group);
+            const int64_t un = (w.start + tk) * a.n_q_heads + qh;
+            if (my_parts > 1) {
+                *reinterpret_cast<float4 *>(a.part_out + (un * a.parts + part) * a.c.head_dim + d) = y;
+                if (d == 0) a.part_ml[un * a.parts + part] = make_float2(m_c, s_c);
+                continue;
+            }
+            const float inv = s_c == 0.0f ? 0.0f : 1.0f / s_c;
+            uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + (w.start + tk) * a.out_stride_token + qh * a.out_stride_head + d;
+            y.x *= inv, y.y *= inv, y.z *= inv, y.w *= inv;
+            const uint2 p = make_uint2(pack2<F16>(y.x, y.y), pack2<F16>(y.z, y.w));
+            if (a.out_wide) *reinterpret_cast<uint2 *>(dst) = p;
+            else dst[0] = (uint16_t)p.x, dst[1] = (uint16_t)(p.x >> 16), dst[2] = (uint16_t)p.y, dst[3] = (uint16_t)(p.y >> 16);
+            if (d == 0 && a.lse) a.lse[un] = s_c == 0.0f ? -INFINITY : (m_c + __builtin_amdgcn_logf(s_c)) * 0.6931471805599453f;
+        }
+        return;
+    }
+    if (!live) return;
+    if (bad) l = nan;
+    const int64_t un = t * a.n_q_heads + q_head;
+    if (my_parts > 1) {
+        float *dst = a.part_out + (un * a.parts + part) * a.c.head_dim;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = d * 32 + 8 * i + 4 * h;
+                if (at < a.c.head_dim)
+                    *reinterpret_cast<float4 *>(dst + at) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+            }
+        if (h == 0) a.part_ml[un * a.parts + part] = make_float2(mc, l);
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *const dst = reinterpret_cast<uint16_t *>(a.out) + t * a.out_stride_token + q_head * a.out_stride_head;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = d * 32 + 8 * i + 4 * h;
+            if (at >= a.c.head_dim) continue;
+            const uint2 p = make_uint2(pack2<F16>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
+                                       pack2<F16>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
+            if (a.out_wide) *reinterpret_cast<uint2 *>(dst + at) = p;
+            else dst[at] = (uint16_t)p.x, dst[at + 1] = (uint16_t)(p.x >> 16), dst[at + 2] = (uint16_t)p.y, dst[at + 3] = (uint16_t)(p.y >> 16);
+        }
+    if (h == 0 && a.lse) a.lse[un] = l == 0.0f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+/* A wave per (token, query head) joins the parts of its row: the parts' maxima
+ * give their factors, the sums and the vectors are added in the order of the
+ * parts. */
+template <bool F16>
+__global__ void __launch_bounds__(TREE_THREADS) tree_join(TreeArgs a, int cols)
+{
+    const int lane = (int)threadIdx.x & 63;
+    const int64_t per_row = (int64_t)a.r.max_length * a.n_q_heads;
+    const int64_t i = (int64_t)blockIdx.x * (TREE_THREADS / 64) + (threadIdx.x >> 6);
+    const int64_t row = i / per_row;
+    if (row >= a.r.n_rows) return;
+    const int32_t tok = (int32_t)(i % per_row / a.n_q_heads), q_head = (int32_t)(i % a.n_q_heads);
+    const KvRow w = load_row(a.r, a.c, row, false);
+    if (!w.out_ok || tok >= w.length) return;
+    const int32_t col = tok * a.group + q_head % a.group;
+    const TreeSpan sp = tree_span(a, w, row, col / cols, cols);
+    const int32_t parts = parts_of(a, sp.end);
+    if (parts == 1) return;
+    const int64_t un = (w.start + tok) * a.n_q_heads + q_head;
+    const float2 *ml = a.part_ml + un * a.parts;
+    float m = -INFINITY;
+    for (int32_t p = lane; p < parts; p += 64) m = fmaxf(m, ml[p].x);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float y[4] = {}, sum = 0.0f;
+    for (int32_t p0 = 0; p0 < parts; p0 += 64) {
+        float f = 0.0f, fl = 0.0f;
+        if (p0 + lane < parts) {
+            const float2 v = ml[p0 + lane];
+            f = __builtin_amdgcn_exp2f(v.x - ref);
+            fl = v.y * f;
+        }
+        const int here = parts - p0 < 64 ? parts - p0 : 64;
+        for (int k = 0; k < here; ++k) {
+            const float g = __shfl(f, k);
+            sum += __shfl(fl, k);
+            const float *src = a.part_out + (un * a.parts + p0 + k) * a.c.head_dim;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e * 64 + lane < a.c.head_dim) y[e] += g * src[e * 64 + lane];
+        }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + (w.start + tok) * a.out_stride_token + q_head * a.out_stride_head;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e * 64 + lane < a.c.head_dim) dst[e * 64 + lane] = (uint16_t)(F16 ? f32_to_f16(y[e] * inv) : f32_to_bf16(y[e] * inv));
+    if (lane == 0 && a.lse) a.lse[un] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace pk
