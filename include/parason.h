@@ -536,10 +536,12 @@ int parason_kv_read(const parason_kv_cache *cache, const parason_kv_rows *rows, 
  *   lse = ln sum_p exp(s_p)   over the positions p that the token sees.
  * A token that sees nothing (or whose scores are all -inf) gets out = 0 and
  * lse = -inf.  What a token does not see changes nothing for it, whatever it
- * holds.  Scores, maxima, sums and the accumulation are float32; the weights
- * exp(s_p - max) are rounded to 16 bits for the matrix product with v.
- * Rows that are bad, or need a bad page, get NaN (nothing, where starts[i] and
- * lengths[i] themselves are bad). */
+ * holds.  Scores, maxima, sums and the accumulation are float32; for the matrix
+ * product with v the weights exp(s_p - max), an 8-bit cache's scales of v
+ * among them, are rounded to 16 bits (float16 over an F16 cache, else bfloat16;
+ * F16 results over an 8-bit cache: to two bfloat16 terms).  Bad rows get NaN (nothing, where starts[i] and lengths[i] themselves
+ * are bad), and so do tokens that see a position on a bad page (others of their
+ * row may). */
 typedef struct parason_tree_args {
     const void *q;            /* value d of head h of token t: element t * q_stride_token + h * q_stride_head + d */
     void *out;                /* the same with its own strides */

@@ -152,6 +152,12 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
     constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
     constexpr bool PF16 = KIND == KV_F16;   /* type of the weights and of V: bfloat16 for codes, whose scales are in the weights */
+    /* float16 results over codes: the weights go in as two bfloat16 terms, so that they are not the coarsest step of
+     * the whole.  (float16 weights would lose all precision where the positions with nearly all of the weight hold a
+     * code of zero.) */
+    constexpr bool SPLIT = CODES && F16;
+    /* The largest weight is 2^LIFT: of float16's 30 binades of full precision 29 are then below it. */
+    constexpr int LIFT = PF16 ? 15 : 0;
     constexpr int VE = CODES ? 16 : 8;      /* values of a 16-byte piece of the cache */
     constexpr int VPR = DP / VE, RPP = TREE_THREADS / VPR, NP = TK / RPP;
     constexpr int ES = CODES ? 1 : 2;
@@ -326,7 +332,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     };
 
     acc16 o[ND] = {};
-    float mc = -INFINITY, l = 0.0f;          /* c2 * maximum; this lane's share of the sum */
+    float at = -INFINITY, l = 0.0f;          /* the exponent that o and l are relative to; this lane's share of the sum */
 
     int32_t x = next_tile(k_begin / TK);
     if (x < t_end) {
@@ -435,16 +441,16 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float mc_new = fmaxf(mc, top * a.c2);
-        const float ref = mc_new == -INFINITY ? 0.0f : mc_new;
-        if (__ballot(mc_new > mc)) {
-            const float corr = __builtin_amdgcn_exp2f(mc - ref);
+        const float at_new = fmaxf(at, top * a.c2 - LIFT);
+        const float ref = at_new == -INFINITY ? 0.0f : at_new;
+        if (__ballot(at_new > at)) {
+            const float corr = __builtin_amdgcn_exp2f(at - ref);
             l *= corr;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= corr;
-            mc = mc_new;
+            at = at_new;
         }
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
@@ -480,6 +486,14 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pw[i] = pack2<PF16>(s[u][8 * k + 2 * i], s[u][8 * k + 2 * i + 1]);
                 const frag8 pf = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+                frag8 pf_rest = {};
+                if (SPLIT) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        pw[i] = pack2<PF16>(s[u][8 * k + 2 * i] - __uint_as_float(pw[i] << 16),
+                                            s[u][8 * k + 2 * i + 1] - __uint_as_float(pw[i] & 0xFFFF0000u));
+                    pf_rest = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+                }
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
                     typedef __attribute__((address_space(3))) frag4 lds4;
@@ -493,6 +507,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                             if (not_finite2<PF16>((uint16_t)vf[i])) vf[i] = 0;
                     }
                     o[d] = mma<PF16>(vf, pf, o[d]);
+                    if (SPLIT) o[d] = mma<PF16>(vf, pf_rest, o[d]);
                 }
             }
         }
@@ -533,7 +548,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     if (WQ == 1) {
         /* join the waves: every column's maximum and sum over the four, then their shares of O */
         float *const Os = reinterpret_cast<float *>(tile);
-        if (h == 0) join_ml[0][wave][n] = mc, join_ml[1][wave][n] = l;
+        if (h == 0) join_ml[0][wave][n] = at, join_ml[1][wave][n] = l;
         __syncthreads();
         float m4 = -INFINITY, sum = 0.0f;
 #pragma unroll
@@ -541,7 +556,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
         const float ref = m4 == -INFINITY ? 0.0f : m4;
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum += join_ml[1][i][n] * __builtin_amdgcn_exp2f(join_ml[0][i][n] - ref);
-        const float f = __builtin_amdgcn_exp2f(mc - ref);
+        const float f = __builtin_amdgcn_exp2f(at - ref);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -593,7 +608,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                 if (at < a.c.head_dim)
                     *reinterpret_cast<float4 *>(dst + at) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
             }
-        if (h == 0) a.part_ml[un * a.parts + part] = make_float2(mc, l);
+        if (h == 0) a.part_ml[un * a.parts + part] = make_float2(at, l);
         return;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -609,7 +624,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
             if (a.out_wide) *reinterpret_cast<uint2 *>(dst + at) = p;
             else dst[at] = (uint16_t)p.x, dst[at + 1] = (uint16_t)(p.x >> 16), dst[at + 2] = (uint16_t)p.y, dst[at + 3] = (uint16_t)(p.y >> 16);
         }
-    if (h == 0 && a.lse) a.lse[un] = l == 0.0f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    if (h == 0 && a.lse) a.lse[un] = l == 0.0f ? -INFINITY : (at + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 /* A wave per (token, query head) joins the parts of its row: the parts' maxima

@@ -10,10 +10,20 @@ using abi::cu_count;
 
 namespace {
 
-int check_sizes(int64_t n_groups, int32_t beams, int64_t vocab)
+struct BeamLayout {
+    int64_t chunks;
+    size_t best, end; /* the chunks' sums at 0 */
+};
+
+int layout_for(int64_t n_groups, int32_t beams, int64_t vocab, BeamLayout *L)
 {
     if (n_groups < 0 || beams < 1 || beams > PARASON_BEAM_MAX || n_groups > INT32_MAX / beams || vocab < 1 || vocab > INT32_MAX - 1)
         return PARASON_ERR_SIZE;
+    L->chunks = (vocab + pk::BEAM_CHUNK - 1) / pk::BEAM_CHUNK;
+    const int64_t rows = n_groups * beams;
+    if (rows > INT32_MAX / L->chunks) return PARASON_ERR_SIZE;
+    L->best = abi::align_up((size_t)(rows * L->chunks) * sizeof(float2));
+    L->end = L->best + abi::align_up((size_t)(rows * L->chunks) * beams * sizeof(pk::BeamCandidate) + 1);
     return PARASON_OK;
 }
 
@@ -24,18 +34,18 @@ extern "C" {
 int parason_beam_workspace_size(int64_t n_groups, int32_t beams, int64_t vocab, size_t *bytes)
 {
     if (!bytes) return PARASON_ERR_NULL;
-    const int rc = check_sizes(n_groups, beams, vocab);
-    if (rc != PARASON_OK) return rc;
-    *bytes = abi::align_up((size_t)(n_groups * beams) * 8 + 1);
-    return PARASON_OK;
+    BeamLayout L;
+    const int rc = layout_for(n_groups, beams, vocab, &L);
+    if (rc == PARASON_OK) *bytes = L.end;
+    return rc;
 }
 
 int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, int32_t dtype, const float *scores,
                         const parason_decode_state *states, int64_t n_groups, int32_t beams, float *new_scores,
                         int32_t *parents, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream_ptr)
 {
-    size_t need;
-    const int rc = parason_beam_workspace_size(n_groups, beams, vocab, &need);
+    BeamLayout L;
+    const int rc = layout_for(n_groups, beams, vocab, &L);
     if (rc != PARASON_OK) return rc;
     const int64_t rows = n_groups * beams;
     if (row_stride < vocab || row_stride > INT64_MAX / 8 / (rows > 0 ? rows : 1)) return PARASON_ERR_SIZE;
@@ -46,21 +56,20 @@ int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, i
     if (!aligned(logits, elem) || !aligned(scores, 4) || !aligned(states, 16) || !aligned(new_scores, 4) ||
         !aligned(parents, 4) || !aligned(tokens, 4) || !aligned(workspace, abi::ALIGN))
         return PARASON_ERR_ALIGN;
-    if (workspace_bytes < need) return PARASON_ERR_WORKSPACE;
+    if (workspace_bytes < L.end) return PARASON_ERR_WORKSPACE;
     if (cu_count() <= 0) return PARASON_ERR_DEVICE;
     pk::BeamArgs a;
     a.logits = (const char *)logits;
-    a.vocab = vocab, a.row_bytes = row_stride * elem, a.rows = rows;
-    a.scores = scores, a.states = states, a.beams = beams;
-    a.norm = (double *)workspace;
+    a.vocab = vocab, a.row_bytes = row_stride * elem;
+    a.scores = scores, a.states = states, a.beams = beams, a.chunks = (int32_t)L.chunks;
+    a.sums = (float2 *)workspace;
+    a.best = (pk::BeamCandidate *)((char *)workspace + L.best);
     a.new_scores = new_scores, a.parents = parents, a.tokens = tokens;
     hipStream_t stream = (hipStream_t)stream_ptr;
-    auto norm = dtype == PARASON_DTYPE_F32 ? pk::beam_norm<PARASON_DTYPE_F32>
-                : dtype == PARASON_DTYPE_BF16 ? pk::beam_norm<PARASON_DTYPE_BF16> : pk::beam_norm<PARASON_DTYPE_F16>;
-    auto rounds = dtype == PARASON_DTYPE_F32 ? pk::beam_rounds<PARASON_DTYPE_F32>
-                  : dtype == PARASON_DTYPE_BF16 ? pk::beam_rounds<PARASON_DTYPE_BF16> : pk::beam_rounds<PARASON_DTYPE_F16>;
-    hipLaunchKernelGGL(norm, dim3((unsigned)rows), dim3(pk::BEAM_THREADS), 0, stream, a);
-    hipLaunchKernelGGL(rounds, dim3((unsigned)n_groups), dim3(pk::BEAM_THREADS), 0, stream, a);
+    auto scan = dtype == PARASON_DTYPE_F32 ? pk::beam_scan<PARASON_DTYPE_F32>
+                : dtype == PARASON_DTYPE_BF16 ? pk::beam_scan<PARASON_DTYPE_BF16> : pk::beam_scan<PARASON_DTYPE_F16>;
+    hipLaunchKernelGGL(scan, dim3((unsigned)(rows * L.chunks)), dim3(pk::BEAM_THREADS), 0, stream, a);
+    hipLaunchKernelGGL(pk::beam_choose, dim3((unsigned)n_groups), dim3(pk::BEAM_THREADS), 0, stream, a);
     return hipGetLastError() == hipSuccess ? PARASON_OK : PARASON_ERR_HIP;
 }
 
@@ -72,19 +81,32 @@ int parason_beam_reorder(const int32_t *parents, int64_t n_rows, const parason_b
     if (!parents || !arrays) return PARASON_ERR_NULL;
     pk::ReorderArgs a;
     a.parents = parents, a.n_rows = n_rows, a.n_arrays = 0;
-    for (int k = 0; k < n_arrays; ++k) {
-        const parason_beam_array &x = arrays[k];
-        if (x.row_bytes < 0 || x.src_stride < x.row_bytes || x.dst_stride < x.row_bytes ||
-            !abi::stride_fits(x.src_stride, n_rows) || !abi::stride_fits(x.dst_stride, n_rows))
-            return PARASON_ERR_SIZE;
-        if (x.row_bytes == 0) continue;
-        if (!x.src || !x.dst) return PARASON_ERR_NULL;
-        a.arrays[a.n_arrays++] = x;
+    int64_t blocks = 0;
+    for (int small = 1; small >= 0; --small) {
+        if (!small) {
+            a.n_small = a.n_arrays;
+            blocks = a.n_small > 0; /* block 0 of a row: the small arrays */
+        }
+        for (int k = 0; k < n_arrays; ++k) {
+            const parason_beam_array &x = arrays[k];
+            if (x.row_bytes < 0 || x.src_stride < x.row_bytes || x.dst_stride < x.row_bytes ||
+                !abi::stride_fits(x.src_stride, n_rows) || !abi::stride_fits(x.dst_stride, n_rows))
+                return PARASON_ERR_SIZE;
+            if (x.row_bytes == 0 || (x.row_bytes <= pk::REORDER_SMALL) != (small == 1)) continue;
+            if (!x.src || !x.dst) return PARASON_ERR_NULL;
+            const uintptr_t ends = (uintptr_t)x.src | (uintptr_t)x.dst | (uintptr_t)x.src_stride | (uintptr_t)x.dst_stride;
+            a.width[a.n_arrays] = (ends & 15u) == 0 ? 16 : (ends & 3u) == 0 ? 4 : 1;
+            a.first_block[a.n_arrays] = (int32_t)blocks;
+            a.arrays[a.n_arrays++] = x;
+            if (!small) blocks += (x.row_bytes + pk::REORDER_SEGMENT - 1) / pk::REORDER_SEGMENT;
+            if (blocks > INT32_MAX / n_rows) return PARASON_ERR_SIZE;
+        }
     }
     if (!aligned(parents, 4)) return PARASON_ERR_ALIGN;
     if (a.n_arrays == 0) return PARASON_OK;
     if (cu_count() <= 0) return PARASON_ERR_DEVICE;
-    hipLaunchKernelGGL(pk::beam_reorder, dim3((unsigned)n_rows), dim3(256), 0, (hipStream_t)stream_ptr, a);
+    a.blocks_per_row = (int32_t)blocks;
+    hipLaunchKernelGGL(pk::beam_reorder, dim3((unsigned)(n_rows * blocks)), dim3(pk::REORDER_THREADS), 0, (hipStream_t)stream_ptr, a);
     return hipGetLastError() == hipSuccess ? PARASON_OK : PARASON_ERR_HIP;
 }
 

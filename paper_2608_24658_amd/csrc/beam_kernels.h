@@ -1,6 +1,20 @@
 /*
  * beam_kernels.h -- beam selection and the reordering of what belongs to a
  * beam for gfx950.
+ *
+ * The selection is one pass over the logits.  Within a row the order of the
+ * candidates is that of the logits, so a block takes a chunk of a row into
+ * registers, and from these the chunk's maximum, its sum of exponentials and
+ * its `beams` largest logits; a block per group then has each row's sum and
+ * chooses among the chunks' candidates, in double precision.  Bound by the
+ * read.
+ *
+ * The largest of many, by a bound from below: of the threads' own maxima each
+ * wave finds the k-th largest, k a quarter of the beams, by counting lanes bit
+ * by bit; the least of these over the four waves has at least `beams` values at or above
+ * it, and rarely many more.  Those go to a list in LDS, where each counts the
+ * ones before it.  A list that overflows (thousands of equal values) is done
+ * without: the best, then the best behind it, and so on.
  */
 #pragma once
 #include "kv_common.h"
@@ -8,127 +22,386 @@
 namespace pk {
 
 constexpr int BEAM_THREADS = 256;
+constexpr int BEAM_PER_THREAD = 32;                              /* logits */
+constexpr int BEAM_CHUNK = BEAM_THREADS * BEAM_PER_THREAD;
+constexpr int BEAM_LIST = 1024;                                  /* candidates of a block */
+
+struct __attribute__((packed, aligned(2))) Unaligned16 {
+    uint32_t w[4];
+};
+
+struct BeamCandidate {
+    float logit;   /* -inf: none */
+    int32_t token;
+};
 
 struct BeamArgs {
     const char *logits;
-    int64_t vocab, row_bytes, rows;
+    int64_t vocab, row_bytes;
     const float *scores;
     const parason_decode_state *states;
-    int32_t beams;
-    double *norm;      /* [rows] score - ln sum exp of the row, NaN: offers no tokens */
+    int32_t beams, chunks;
+    float2 *sums;             /* [rows][chunks]: maximum, sum of exp(logit - maximum) */
+    BeamCandidate *best;      /* [rows][chunks][beams], best first */
     float *new_scores;
     int32_t *parents, *tokens;
 };
 
-template <int T>
-__device__ __forceinline__ float logit(const char *row, int64_t i)
+/* What a row offers. */
+enum : int { BEAM_NONE = 0, BEAM_TOKENS, BEAM_STAYS };
+
+__device__ __forceinline__ int beam_offers(const BeamArgs &a, int64_t row, float score)
 {
-    if (T == PARASON_DTYPE_F32) return reinterpret_cast<const float *>(row)[i];
-    const uint32_t h = reinterpret_cast<const uint16_t *>(row)[i];
-    return T == PARASON_DTYPE_BF16 ? bf16_to_f32(h) : f16_to_f32(h);
+    if (!(score > -INFINITY && score < INFINITY)) return BEAM_NONE;
+    if (!a.states) return BEAM_TOKENS;
+    const uint32_t f = a.states[row].flags;
+    return (f & PARASON_DECODE_ERROR) ? BEAM_NONE : (f & PARASON_DECODE_DONE) ? BEAM_STAYS : BEAM_TOKENS;
 }
 
-template <int T>
-__global__ void __launch_bounds__(BEAM_THREADS) beam_norm(BeamArgs a)
+/* Floats as integers of the same order. */
+__device__ __forceinline__ uint32_t in_order(float x)
 {
-    __shared__ float red[8];
-    const int64_t row = blockIdx.x;
-    const char *x = a.logits + row * a.row_bytes;
-    float m = -INFINITY;
-    bool bad = false;
-    for (int64_t i = threadIdx.x; i < a.vocab; i += BEAM_THREADS) {
-        const float v = logit<T>(x, i);
-        bad = bad || !(v < INFINITY);
-        m = fmaxf(m, v);
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ float from_order(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+
+/* A value that at least k of the wave's lanes (k <= 64) are not below, to 16
+ * bits, and above -inf. */
+__device__ __forceinline__ float wave_kth(float x, int k)
+{
+    const uint32_t key = in_order(x);
+    uint32_t t = 0u;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t trial = t | (1u << b);
+        if (__popcll(__ballot(key >= trial)) >= k) t = trial;
     }
-    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    bad = __syncthreads_or(bad);
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    float s = 0.0f;
-    if (!bad && m > -INFINITY)
-        for (int64_t i = threadIdx.x; i < a.vocab; i += BEAM_THREADS) s += __expf(logit<T>(x, i) - m);
-    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
-    if ((threadIdx.x & 63) == 0) red[4 + (threadIdx.x >> 6)] = s;
+    const uint32_t least = 0x00800000u; /* -FLT_MAX */
+    return from_order(t < least ? least : t);
+}
+
+/* A value that at least n of the block's threads' values are not below (or
+ * -FLT_MAX).  red: 4 floats. */
+__device__ __forceinline__ float block_bound(float x, int n, float *red)
+{
+    const float t = wave_kth(x, (n + 3) / 4);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const float score = a.scores[row];
-        const bool live = isfinite(score) && !bad && m > -INFINITY && !(a.states && a.states[row].flags);
-        const double total = (double)red[4] + red[5] + red[6] + red[7];
-        a.norm[row] = live ? (double)score - ((double)m + log(total)) : (double)NAN;
+    return fminf(fminf(red[0], red[1]), fminf(red[2], red[3]));
+}
+
+template <int T>
+__global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
+{
+    constexpr int ES = T == PARASON_DTYPE_F32 ? 4 : 2, VE = 16 / ES, NV = BEAM_PER_THREAD / VE;
+    __shared__ float red[12];
+    __shared__ BeamCandidate list[BEAM_LIST];
+    __shared__ int32_t n_list;
+    const uint32_t chunk = blockIdx.x % (uint32_t)a.chunks;
+    const int64_t row = blockIdx.x / (uint32_t)a.chunks;
+    const int tid = (int)threadIdx.x;
+    BeamCandidate *const best = a.best + (row * a.chunks + chunk) * a.beams;
+    const char *const x = a.logits + row * a.row_bytes;
+    if (beam_offers(a, row, a.scores[row]) != BEAM_TOKENS) return;
+    /* 16 bytes at a time from the row's first logit on, at whatever alignment that has: which logits a lane adds up, and
+     * so a row's sum, does not depend on where the row lies */
+    const int64_t e0 = ((int64_t)chunk * (BEAM_THREADS * NV) + tid) * VE;
+    uint4 raw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int64_t e = e0 + (int64_t)i * BEAM_THREADS * VE;
+        if (e + VE <= a.vocab) {
+            const Unaligned16 p = *reinterpret_cast<const Unaligned16 *>(x + e * ES);
+            raw[i] = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
+        } else {
+            uint32_t w[4];
+            for (int j = 0; j < 4; ++j) {
+                if (ES == 4) {
+                    w[j] = e + j < a.vocab ? reinterpret_cast<const uint32_t *>(x)[e + j] : 0xFF800000u;
+                } else {
+                    const uint32_t none = T == PARASON_DTYPE_BF16 ? 0xFF80u : 0xFC00u;
+                    const int64_t p = e + 2 * j;
+                    const uint32_t lo = p < a.vocab ? reinterpret_cast<const uint16_t *>(x)[p] : none;
+                    const uint32_t hi = p + 1 < a.vocab ? reinterpret_cast<const uint16_t *>(x)[p + 1] : none;
+                    w[j] = lo | (hi << 16);
+                }
+            }
+            raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    float v[BEAM_PER_THREAD];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            v[i * VE + j] = ES == 4 ? __uint_as_float(w[j & 3])
+                            : T == PARASON_DTYPE_BF16 ? bf16_to_f32((w[(j / 2) & 3] >> (16 * (j & 1))) & 0xFFFFu)
+                                                      : f16_to_f32((w[(j / 2) & 3] >> (16 * (j & 1))) & 0xFFFFu);
+    }
+    auto token_of = [&](int i) { return (int32_t)(e0 + (int64_t)(i / VE) * BEAM_THREADS * VE + i % VE); };
+    float mine = v[0];
+#pragma unroll
+    for (int i = 1; i < BEAM_PER_THREAD; ++i) mine = fmaxf(mine, v[i]);
+    if (!(mine == mine)) mine = -INFINITY; /* nothing but NaN: the sum tells */
+    float m = mine;
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    if ((tid & 63) == 0) red[4 + (tid >> 6)] = m;
+    if (tid == 0) n_list = 0;
+    const float bound = block_bound(mine, a.beams, red);
+    m = fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
+    /* ---- sum */
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < BEAM_PER_THREAD; ++i) s += __builtin_amdgcn_exp2f((v[i] - ref) * 1.44269504f);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+    if ((tid & 63) == 0) red[8 + (tid >> 6)] = s;
+    /* ---- candidates */
+    if (mine >= bound) {
+#pragma unroll
+        for (int i = 0; i < BEAM_PER_THREAD; ++i) {
+            if (v[i] >= bound) {
+                const int at = atomicAdd(&n_list, 1);
+                if (at < BEAM_LIST) list[at] = BeamCandidate{v[i], token_of(i)};
+            }
+        }
+    }
+    __syncthreads();
+    const int n = n_list;
+    if (tid == 0) a.sums[row * a.chunks + chunk] = make_float2(m, red[8] + red[9] + red[10] + red[11]);
+    if (n <= BEAM_LIST) {
+        for (int c = tid; c < n; c += BEAM_THREADS) {
+            const BeamCandidate me = list[c];
+            int before = 0;
+            for (int k = 0; k < n; ++k) {
+                const BeamCandidate o = list[k];
+                before += o.logit > me.logit || (o.logit == me.logit && o.token < me.token);
+            }
+            if (before < a.beams) best[before] = me;
+        }
+        if (tid >= n && tid < a.beams) best[tid] = BeamCandidate{-INFINITY, -1};
+        return;
+    }
+    /* too many equal ones: one after the other */
+    BeamCandidate last{INFINITY, -1};
+    for (int k = 0; k < a.beams; ++k) {
+        BeamCandidate b{-INFINITY, INT32_MAX};
+#pragma unroll
+        for (int i = 0; i < BEAM_PER_THREAD; ++i) {
+            const int32_t t = token_of(i);
+            if ((v[i] < last.logit || (v[i] == last.logit && t > last.token)) && v[i] > b.logit) b = BeamCandidate{v[i], t};
+        }
+        /* a thread's own equal ones come in the order of their tokens */
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const float f = __shfl_xor(b.logit, o);
+            const int32_t t = __shfl_xor(b.token, o);
+            if (f > b.logit || (f == b.logit && t < b.token)) b = BeamCandidate{f, t};
+        }
+        __syncthreads();
+        if ((tid & 63) == 0) list[tid >> 6] = b;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const BeamCandidate o = list[w];
+            if (o.logit > b.logit || (o.logit == b.logit && o.token < b.token)) b = o;
+        }
+        if (tid == 0) best[k] = BeamCandidate{b.logit, b.logit == -INFINITY ? -1 : b.token};
+        last = b;
     }
 }
 
-/* One block per group; a round per beam finds the best candidate behind the
- * one before. */
-template <int T>
-__global__ void __launch_bounds__(BEAM_THREADS) beam_rounds(BeamArgs a)
+struct BeamScored {
+    double score;
+    int64_t place; /* (beam of the group, token + 1) */
+};
+
+__device__ __forceinline__ bool beam_before(const BeamScored &a, const BeamScored &b)
 {
-    __shared__ double best_s[BEAM_THREADS];
-    __shared__ int64_t best_i[BEAM_THREADS];
-    __shared__ float sc[PARASON_BEAM_MAX];
+    return a.score > b.score || (a.score == b.score && a.place < b.place);
+}
+
+/* One block per group. */
+__global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
+{
+    __shared__ float red[4];
+    __shared__ float score[PARASON_BEAM_MAX];
+    __shared__ double norm[PARASON_BEAM_MAX]; /* score - ln of the sum; NaN: the row offers no tokens */
+    __shared__ int32_t offers[PARASON_BEAM_MAX];
+    __shared__ BeamScored list[BEAM_LIST];
+    __shared__ int32_t n_list;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row0 = (int64_t)blockIdx.x * a.beams;
-    if ((int)threadIdx.x < a.beams) sc[threadIdx.x] = a.scores[row0 + threadIdx.x];
-    double last_s = (double)INFINITY;
-    int64_t last_i = -1;
+    if (tid == 0) n_list = 0;
+    for (int b = wave; b < a.beams; b += BEAM_THREADS / 64) {
+        const int64_t row = row0 + b;
+        const float sc = a.scores[row];
+        const int what = beam_offers(a, row, sc);
+        double z = (double)NAN;
+        if (what == BEAM_TOKENS) {
+            float m = -INFINITY;
+            double s = 0.0;
+            for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, a.sums[row * a.chunks + c].x);
+#pragma unroll
+            for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+            for (int c = lane; c < a.chunks; c += 64) {
+                const float2 q = a.sums[row * a.chunks + c];
+                s += q.y == 0.0f ? 0.0 : (double)q.y * exp((double)q.x - (double)m);
+            }
+#pragma unroll
+            for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+            /* NaN or +inf among the logits: s is NaN; nothing but -inf: no sum */
+            if (m > -INFINITY && s < (double)INFINITY) z = (double)sc - ((double)m + log(s));
+        }
+        if (lane == 0) score[b] = sc, norm[b] = z, offers[b] = what;
+    }
+    __syncthreads();
+    const uint32_t per_row = (uint32_t)a.chunks * (uint32_t)a.beams, total = per_row * (uint32_t)a.beams;
+    const BeamCandidate *const best = a.best + row0 * per_row;
+    /* candidate i of the group; a finished row has one, in its first place */
+    auto take = [&](uint32_t i, BeamScored *c) {
+        const uint32_t b = i / per_row;
+        if (offers[b] == BEAM_STAYS) {
+            if (i != b * per_row) return false;
+            *c = BeamScored{(double)score[b], (int64_t)b * (a.vocab + 1)};
+            return true;
+        }
+        const double z = norm[b];
+        if (!(z == z)) return false;
+        const BeamCandidate q = best[i];
+        if (!(q.logit > -INFINITY)) return false;
+        *c = BeamScored{z + (double)q.logit, (int64_t)b * (a.vocab + 1) + q.token + 1};
+        return true;
+    };
+    float mine = -INFINITY;
+    BeamScored c;
+    for (uint32_t i = tid; i < total; i += BEAM_THREADS)
+        if (take(i, &c)) mine = fmaxf(mine, (float)c.score);
+    /* (a rounding to float keeps the order of two scores or makes them equal) */
+    const float bound = block_bound(mine, a.beams, red);
+    if (mine >= bound) {
+        for (uint32_t i = tid; i < total; i += BEAM_THREADS) {
+            if (take(i, &c) && (float)c.score >= bound) {
+                const int at = atomicAdd(&n_list, 1);
+                if (at < BEAM_LIST) list[at] = c;
+            }
+        }
+    }
+    __syncthreads();
+    const int n = n_list;
+    auto put = [&](int k, const BeamScored &s) {
+        const int64_t b = s.place / (a.vocab + 1);
+        a.new_scores[row0 + k] = (float)s.score;
+        a.parents[row0 + k] = (int32_t)(row0 + b);
+        a.tokens[row0 + k] = (int32_t)(s.place - b * (a.vocab + 1)) - 1;
+    };
+    auto put_none = [&](int k) {
+        a.new_scores[row0 + k] = -INFINITY;
+        a.parents[row0 + k] = (int32_t)(row0 + k);
+        a.tokens[row0 + k] = -1;
+    };
+    if (n <= BEAM_LIST) {
+        for (int i = tid; i < n; i += BEAM_THREADS) {
+            const BeamScored me = list[i];
+            int before = 0;
+            for (int k = 0; k < n; ++k) before += beam_before(list[k], me);
+            if (before < a.beams) put(before, me);
+        }
+        if (tid >= n && tid < a.beams) put_none(tid);
+        return;
+    }
+    /* too many equal ones: one after the other */
+    const BeamScored none{-(double)INFINITY, INT64_MAX};
+    BeamScored last{(double)INFINITY, -1};
     for (int k = 0; k < a.beams; ++k) {
-        double bs = -(double)INFINITY;
-        int64_t bi = -1;
+        BeamScored b = none;
+        for (uint32_t i = tid; i < total; i += BEAM_THREADS)
+            if (take(i, &c) && beam_before(last, c) && beam_before(c, b)) b = c;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const BeamScored q{__shfl_xor(b.score, o), (int64_t)__shfl_xor((long long)b.place, o)};
+            if (beam_before(q, b)) b = q;
+        }
         __syncthreads();
-        for (int b = 0; b < a.beams; ++b) {
-            const char *x = a.logits + (row0 + b) * a.row_bytes;
-            const double norm = a.norm[row0 + b];
-            const uint32_t flags = a.states ? a.states[row0 + b].flags : 0u;
-            const bool stay = !(flags & PARASON_DECODE_ERROR) && (flags & PARASON_DECODE_DONE) && isfinite(sc[b]);
-            if (norm != norm && !stay) continue;
-            for (int64_t i = threadIdx.x; i < (stay ? 1 : a.vocab); i += BEAM_THREADS) {
-                const double s = stay ? (double)sc[b] : norm + (double)logit<T>(x, i);
-                const int64_t id = b * (a.vocab + 1) + (stay ? 0 : i + 1);
-                if (!(s > -(double)INFINITY)) continue;
-                if ((s < last_s || (s == last_s && id > last_i)) && (s > bs || (s == bs && id < bi))) bs = s, bi = id;
-            }
-        }
-        best_s[threadIdx.x] = bs, best_i[threadIdx.x] = bi;
+        if (lane == 0) list[wave] = b;
         __syncthreads();
-        for (int o = BEAM_THREADS / 2; o > 0; o >>= 1) {
-            if ((int)threadIdx.x < o) {
-                const double s = best_s[threadIdx.x + o];
-                const int64_t i = best_i[threadIdx.x + o];
-                if (i >= 0 && (best_i[threadIdx.x] < 0 || s > best_s[threadIdx.x] ||
-                               (s == best_s[threadIdx.x] && i < best_i[threadIdx.x])))
-                    best_s[threadIdx.x] = s, best_i[threadIdx.x] = i;
-            }
-            __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (beam_before(list[w], b)) b = list[w];
+        if (tid == 0) {
+            if (b.place == INT64_MAX) put_none(k);
+            else put(k, b);
         }
-        last_s = best_s[0], last_i = best_i[0];
-        if (threadIdx.x == 0) {
-            const int64_t r = row0 + k;
-            a.new_scores[r] = last_i < 0 ? -INFINITY : (float)last_s;
-            a.parents[r] = (int32_t)(last_i < 0 ? r : row0 + last_i / (a.vocab + 1));
-            a.tokens[r] = last_i < 0 ? -1 : (int32_t)(last_i % (a.vocab + 1)) - 1;
-        }
-        if (last_i < 0) last_s = -(double)INFINITY, last_i = INT64_MAX;
+        last = b.place == INT64_MAX ? none : b;
     }
 }
+
+/* ---- reordering ---- */
+
+constexpr int REORDER_THREADS = 256;
+constexpr int64_t REORDER_SEGMENT = 16384; /* bytes of a row that a block copies: four 16-byte pieces a thread */
+constexpr int64_t REORDER_SMALL = 1024;    /* rows of up to this many bytes share a block */
 
 struct ReorderArgs {
     const int32_t *parents;
     int64_t n_rows;
-    int32_t n_arrays;
-    parason_beam_array arrays[PARASON_BEAM_ARRAYS];
+    int32_t n_arrays, n_small, blocks_per_row;
+    parason_beam_array arrays[PARASON_BEAM_ARRAYS]; /* the small ones first */
+    int32_t first_block[PARASON_BEAM_ARRAYS];       /* of a row, for the others */
+    uint8_t width[PARASON_BEAM_ARRAYS];             /* bytes of a piece: what every row's two ends are aligned to */
 };
 
-__global__ void __launch_bounds__(256) beam_reorder(ReorderArgs a)
+template <typename U, int NT>
+__device__ __forceinline__ void copy_pieces(char *dst, const char *src, int64_t lo, int64_t hi, int t)
 {
-    const int64_t row = blockIdx.x;
+    /* lo and hi in bytes, lo a multiple of the piece; a rest shorter than a piece goes byte by byte */
+    constexpr int64_t S = sizeof(U);
+    const int64_t n = (hi - lo) / S;
+    const U *s = reinterpret_cast<const U *>(src + lo);
+    U *d = reinterpret_cast<U *>(dst + lo);
+    int64_t i = t;
+    for (; i + 3 * NT < n; i += 4 * NT) {
+        const U a = s[i], b = s[i + NT], c = s[i + 2 * NT], e = s[i + 3 * NT];
+        d[i] = a, d[i + NT] = b, d[i + 2 * NT] = c, d[i + 3 * NT] = e;
+    }
+    for (; i < n; i += NT) d[i] = s[i];
+    for (int64_t k = lo + n * S + t; k < hi; k += NT) dst[k] = src[k];
+}
+
+template <int NT>
+__device__ __forceinline__ void copy_row(char *dst, const char *src, int64_t lo, int64_t hi, int width, int t)
+{
+    if (width == 16) copy_pieces<uint4, NT>(dst, src, lo, hi, t);
+    else if (width == 4) copy_pieces<uint32_t, NT>(dst, src, lo, hi, t);
+    else copy_pieces<uint8_t, NT>(dst, src, lo, hi, t);
+}
+
+__global__ void __launch_bounds__(REORDER_THREADS) beam_reorder(ReorderArgs a)
+{
+    const int64_t row = blockIdx.x / (uint32_t)a.blocks_per_row;
+    const int32_t part = (int32_t)(blockIdx.x % (uint32_t)a.blocks_per_row);
     const int64_t parent = a.parents[row];
     if (parent < 0 || parent >= a.n_rows) return;
-    for (int k = 0; k < a.n_arrays; ++k) {
-        const parason_beam_array &x = a.arrays[k];
-        const char *src = (const char *)x.src + parent * x.src_stride;
-        char *dst = (char *)x.dst + row * x.dst_stride;
-        for (int64_t i = threadIdx.x; i < x.row_bytes; i += 256) dst[i] = src[i];
+    if (part == 0 && a.n_small > 0) { /* a wave an array */
+        for (int k = (int)threadIdx.x >> 6; k < a.n_small; k += REORDER_THREADS / 64) {
+            const parason_beam_array &x = a.arrays[k];
+            copy_row<64>((char *)x.dst + row * x.dst_stride, (const char *)x.src + parent * x.src_stride, 0, x.row_bytes,
+                         a.width[k], (int)threadIdx.x & 63);
+        }
+        return;
     }
+    int k = a.n_small;
+    while (k + 1 < a.n_arrays && part >= a.first_block[k + 1]) ++k;
+    const parason_beam_array &x = a.arrays[k];
+    const int64_t lo = (part - a.first_block[k]) * REORDER_SEGMENT;
+    const int64_t hi = lo + REORDER_SEGMENT < x.row_bytes ? lo + REORDER_SEGMENT : x.row_bytes;
+    copy_row<REORDER_THREADS>((char *)x.dst + row * x.dst_stride, (const char *)x.src + parent * x.src_stride, lo, hi,
+                              a.width[k], (int)threadIdx.x);
 }
 
 }  // namespace pk
