@@ -62,6 +62,9 @@ int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, i
     a.logits = (const char *)logits;
     a.vocab = vocab, a.row_bytes = row_stride * elem;
     a.scores = scores, a.states = states, a.beams = beams, a.chunks = (int32_t)L.chunks;
+    a.chunks_div = pk::fast_div((uint32_t)L.chunks);
+    const int64_t pieces = (vocab * elem + 15) / 16;
+    a.chunk_pieces = (int32_t)((pieces + L.chunks - 1) / L.chunks);
     a.sums = (float2 *)workspace;
     a.best = (pk::BeamCandidate *)((char *)workspace + L.best);
     a.new_scores = new_scores, a.parents = parents, a.tokens = tokens;

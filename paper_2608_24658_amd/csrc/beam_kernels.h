@@ -17,6 +17,8 @@
  * without: the best, then the best behind it, and so on.
  */
 #pragma once
+#include <float.h>
+
 #include "kv_common.h"
 
 namespace pk {
@@ -25,6 +27,7 @@ constexpr int BEAM_THREADS = 256;
 constexpr int BEAM_PER_THREAD = 32;                              /* logits */
 constexpr int BEAM_CHUNK = BEAM_THREADS * BEAM_PER_THREAD;
 constexpr int BEAM_LIST = 1024;                                  /* candidates of a block */
+constexpr int BEAM_ROW_LANES = 8;                                /* that add up the sums of a row's chunks */
 
 struct __attribute__((packed, aligned(2))) Unaligned16 {
     uint32_t w[4];
@@ -41,6 +44,8 @@ struct BeamArgs {
     const float *scores;
     const parason_decode_state *states;
     int32_t beams, chunks;
+    FastDiv chunks_div;
+    int32_t chunk_pieces;     /* 16-byte pieces of a chunk: the row's, evenly */
     float2 *sums;             /* [rows][chunks]: maximum, sum of exp(logit - maximum) */
     BeamCandidate *best;      /* [rows][chunks][beams], best first */
     float *new_scores;
@@ -83,20 +88,32 @@ __device__ __forceinline__ float wave_kth(float x, int k)
 }
 
 /* A value that at least n of the block's threads' values are not below (or
- * -FLT_MAX).  red: 4 floats. */
+ * -FLT_MAX).  red: 8 floats. */
 __device__ __forceinline__ float block_bound(float x, int n, float *red)
 {
+    const int wave = (int)threadIdx.x >> 6;
     const float t = wave_kth(x, (n + 3) / 4);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
+    if ((threadIdx.x & 63) == 0) red[wave] = t;
     __syncthreads();
-    return fminf(fminf(red[0], red[1]), fminf(red[2], red[3]));
+    const float least = fminf(fminf(red[0], red[1]), fminf(red[2], red[3]));
+    if (least > -FLT_MAX) return least;
+    /* a wave with too few values: one that has n by itself may do */
+    const float u = wave_kth(x, n);
+    if ((threadIdx.x & 63) == 0) red[4 + wave] = u;
+    __syncthreads();
+    return fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t mask)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
 template <int T>
 __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
 {
     constexpr int ES = T == PARASON_DTYPE_F32 ? 4 : 2, VE = 16 / ES, NV = BEAM_PER_THREAD / VE;
-    __shared__ float red[12];
+    __shared__ float red[16];
     __shared__ BeamCandidate list[BEAM_LIST];
     __shared__ int32_t n_list;
     const uint32_t chunk = blockIdx.x % (uint32_t)a.chunks;
@@ -107,24 +124,25 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
     if (beam_offers(a, row, a.scores[row]) != BEAM_TOKENS) return;
     /* 16 bytes at a time from the row's first logit on, at whatever alignment that has: which logits a lane adds up, and
      * so a row's sum, does not depend on where the row lies */
-    const int64_t e0 = ((int64_t)chunk * (BEAM_THREADS * NV) + tid) * VE;
+    const int64_t e0 = ((int64_t)chunk * a.chunk_pieces + tid) * VE;
+    const int64_t next = (int64_t)(chunk + 1) * a.chunk_pieces * VE, end = next < a.vocab ? next : a.vocab;
     uint4 raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int64_t e = e0 + (int64_t)i * BEAM_THREADS * VE;
-        if (e + VE <= a.vocab) {
+        if (e + VE <= end) {
             const Unaligned16 p = *reinterpret_cast<const Unaligned16 *>(x + e * ES);
             raw[i] = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
         } else {
             uint32_t w[4];
             for (int j = 0; j < 4; ++j) {
                 if (ES == 4) {
-                    w[j] = e + j < a.vocab ? reinterpret_cast<const uint32_t *>(x)[e + j] : 0xFF800000u;
+                    w[j] = e + j < end ? reinterpret_cast<const uint32_t *>(x)[e + j] : 0xFF800000u;
                 } else {
                     const uint32_t none = T == PARASON_DTYPE_BF16 ? 0xFF80u : 0xFC00u;
                     const int64_t p = e + 2 * j;
-                    const uint32_t lo = p < a.vocab ? reinterpret_cast<const uint16_t *>(x)[p] : none;
-                    const uint32_t hi = p + 1 < a.vocab ? reinterpret_cast<const uint16_t *>(x)[p + 1] : none;
+                    const uint32_t lo = p < end ? reinterpret_cast<const uint16_t *>(x)[p] : none;
+                    const uint32_t hi = p + 1 < end ? reinterpret_cast<const uint16_t *>(x)[p + 1] : none;
                     w[j] = lo | (hi << 16);
                 }
             }
@@ -149,10 +167,10 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
     float m = mine;
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-    if ((tid & 63) == 0) red[4 + (tid >> 6)] = m;
+    if ((tid & 63) == 0) red[8 + (tid >> 6)] = m;
     if (tid == 0) n_list = 0;
     const float bound = block_bound(mine, a.beams, red);
-    m = fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
+    m = fmaxf(fmaxf(red[8], red[9]), fmaxf(red[10], red[11]));
     /* ---- sum */
     const float ref = m == -INFINITY ? 0.0f : m;
     float s = 0.0f;
@@ -160,20 +178,27 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
     for (int i = 0; i < BEAM_PER_THREAD; ++i) s += __builtin_amdgcn_exp2f((v[i] - ref) * 1.44269504f);
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
-    if ((tid & 63) == 0) red[8 + (tid >> 6)] = s;
+    if ((tid & 63) == 0) red[12 + (tid >> 6)] = s;
     /* ---- candidates */
-    if (mine >= bound) {
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < BEAM_PER_THREAD; ++i) count += __popcll(__ballot(v[i] >= bound));
+    if (count > 0) { /* the same for the whole wave */
+        int base = 0;
+        if ((tid & 63) == 0) base = atomicAdd(&n_list, count);
+        base = __builtin_amdgcn_readfirstlane(base);
 #pragma unroll
         for (int i = 0; i < BEAM_PER_THREAD; ++i) {
-            if (v[i] >= bound) {
-                const int at = atomicAdd(&n_list, 1);
-                if (at < BEAM_LIST) list[at] = BeamCandidate{v[i], token_of(i)};
-            }
+            const uint64_t b = __ballot(v[i] >= bound);
+            if (b == 0) continue;
+            const int at = base + lanes_below(b);
+            if (v[i] >= bound && at < BEAM_LIST) list[at] = BeamCandidate{v[i], token_of(i)};
+            base += __popcll(b);
         }
     }
     __syncthreads();
     const int n = n_list;
-    if (tid == 0) a.sums[row * a.chunks + chunk] = make_float2(m, red[8] + red[9] + red[10] + red[11]);
+    if (tid == 0) a.sums[row * a.chunks + chunk] = make_float2(m, red[12] + red[13] + red[14] + red[15]);
     if (n <= BEAM_LIST) {
         for (int c = tid; c < n; c += BEAM_THREADS) {
             const BeamCandidate me = list[c];
@@ -226,69 +251,95 @@ __device__ __forceinline__ bool beam_before(const BeamScored &a, const BeamScore
     return a.score > b.score || (a.score == b.score && a.place < b.place);
 }
 
-/* One block per group. */
+/* One block per group.  The chunks' candidates are lists, best first: a bound
+ * comes from the heads of the lists, and each list is then read as far as it
+ * reaches. */
 __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
 {
-    __shared__ float red[4];
+    __shared__ float red[8];
     __shared__ float score[PARASON_BEAM_MAX];
     __shared__ double norm[PARASON_BEAM_MAX]; /* score - ln of the sum; NaN: the row offers no tokens */
     __shared__ int32_t offers[PARASON_BEAM_MAX];
     __shared__ BeamScored list[BEAM_LIST];
-    __shared__ int32_t n_list;
+    __shared__ int32_t n_list, n_live;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row0 = (int64_t)blockIdx.x * a.beams;
-    if (tid == 0) n_list = 0;
-    for (int b = wave; b < a.beams; b += BEAM_THREADS / 64) {
-        const int64_t row = row0 + b;
+    if (tid == 0) n_list = n_live = 0;
+    __syncthreads();
+    for (int b0 = 0; b0 < a.beams; b0 += BEAM_THREADS / BEAM_ROW_LANES) {
+        const int b = b0 + tid / BEAM_ROW_LANES, part = tid % BEAM_ROW_LANES;
+        const bool there = b < a.beams;
+        const int64_t row = row0 + (there ? b : 0);
         const float sc = a.scores[row];
-        const int what = beam_offers(a, row, sc);
-        double z = (double)NAN;
+        const int what = there ? beam_offers(a, row, sc) : BEAM_NONE;
+        float m = -INFINITY;
+        double s = 0.0; /* an empty chunk has the maximum -inf and the sum 0 */
         if (what == BEAM_TOKENS) {
-            float m = -INFINITY;
-            double s = 0.0;
-            for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, a.sums[row * a.chunks + c].x);
-#pragma unroll
-            for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-            for (int c = lane; c < a.chunks; c += 64) {
-                const float2 q = a.sums[row * a.chunks + c];
-                s += q.y == 0.0f ? 0.0 : (double)q.y * exp((double)q.x - (double)m);
-            }
-#pragma unroll
-            for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
-            /* NaN or +inf among the logits: s is NaN; nothing but -inf: no sum */
-            if (m > -INFINITY && s < (double)INFINITY) z = (double)sc - ((double)m + log(s));
+            for (int c = part; c < a.chunks; c += BEAM_ROW_LANES) m = fmaxf(m, a.sums[row * a.chunks + c].x);
         }
-        if (lane == 0) score[b] = sc, norm[b] = z, offers[b] = what;
+#pragma unroll
+        for (int k = BEAM_ROW_LANES / 2; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+        if (what == BEAM_TOKENS && m > -INFINITY) {
+            for (int c = part; c < a.chunks; c += BEAM_ROW_LANES) {
+                const float2 q = a.sums[row * a.chunks + c];
+                s += (double)(q.y * __builtin_amdgcn_exp2f((q.x - m) * 1.44269504f));
+            }
+        }
+#pragma unroll
+        for (int k = BEAM_ROW_LANES / 2; k > 0; k >>= 1) s += __shfl_xor(s, k);
+        if (there && part == 0) {
+            /* NaN or +inf among the logits: s is NaN; nothing but -inf: no sum */
+            const bool tokens = what == BEAM_TOKENS && m > -INFINITY && s < (double)INFINITY;
+            score[b] = sc, offers[b] = tokens || what == BEAM_STAYS ? what : BEAM_NONE;
+            norm[b] = tokens ? (double)sc - ((double)m + log(s)) : (double)NAN;
+            if (tokens) atomicAdd(&n_live, 1);
+        }
     }
     __syncthreads();
-    const uint32_t per_row = (uint32_t)a.chunks * (uint32_t)a.beams, total = per_row * (uint32_t)a.beams;
-    const BeamCandidate *const best = a.best + row0 * per_row;
-    /* candidate i of the group; a finished row has one, in its first place */
-    auto take = [&](uint32_t i, BeamScored *c) {
-        const uint32_t b = i / per_row;
-        if (offers[b] == BEAM_STAYS) {
-            if (i != b * per_row) return false;
-            *c = BeamScored{(double)score[b], (int64_t)b * (a.vocab + 1)};
-            return true;
-        }
-        const double z = norm[b];
-        if (!(z == z)) return false;
-        const BeamCandidate q = best[i];
-        if (!(q.logit > -INFINITY)) return false;
-        *c = BeamScored{z + (double)q.logit, (int64_t)b * (a.vocab + 1) + q.token + 1};
-        return true;
+    const uint32_t lists = (uint32_t)a.chunks * (uint32_t)a.beams;
+    const BeamCandidate *const best = a.best + row0 * lists;
+    /* The score of entry k of list i, read as q (-inf: no candidate); a finished row has one, in its first list. */
+    auto score_of = [&](uint32_t i, uint32_t k, const BeamCandidate &q) {
+        const uint32_t b = div_by(i, a.chunks_div);
+        const bool first = k == 0 && i == b * (uint32_t)a.chunks;
+        const double none = -(double)INFINITY;
+        return offers[b] == BEAM_TOKENS ? norm[b] + (double)q.logit : offers[b] == BEAM_STAYS && first ? (double)score[b] : none;
     };
+    auto place_of = [&](uint32_t i, const BeamCandidate &q) {
+        const uint32_t b = div_by(i, a.chunks_div);
+        return (int64_t)b * (a.vocab + 1) + (offers[b] == BEAM_TOKENS ? q.token + 1 : 0);
+    };
+    /* The bound, from the first entries of every list, some 64 for each beam (a power of two of every list).
+     * Neighbouring entries, which are much alike, go to different threads and waves: it is the least of the waves'. */
+    const uint32_t live = (uint32_t)n_live * (uint32_t)a.chunks;
+    uint32_t depth_log = 0;
+    while (live > 0 && (2u << depth_log) <= (uint32_t)a.beams && (live << (depth_log + 1)) <= 64u * (uint32_t)a.beams) ++depth_log;
+    const uint32_t entries = lists << depth_log, depth_mask = (1u << depth_log) - 1u;
     float mine = -INFINITY;
-    BeamScored c;
-    for (uint32_t i = tid; i < total; i += BEAM_THREADS)
-        if (take(i, &c)) mine = fmaxf(mine, (float)c.score);
+    for (uint32_t i0 = lane * 4 + wave; i0 < entries; i0 += 2 * BEAM_THREADS) {
+        const uint32_t i1 = i0 + BEAM_THREADS < entries ? i0 + BEAM_THREADS : i0;
+        const BeamCandidate q0 = best[(int64_t)(i0 >> depth_log) * a.beams + (i0 & depth_mask)];
+        const BeamCandidate q1 = best[(int64_t)(i1 >> depth_log) * a.beams + (i1 & depth_mask)];
+        mine = fmaxf(mine, (float)score_of(i0 >> depth_log, i0 & depth_mask, q0));
+        mine = fmaxf(mine, (float)score_of(i1 >> depth_log, i1 & depth_mask, q1));
+    }
     /* (a rounding to float keeps the order of two scores or makes them equal) */
     const float bound = block_bound(mine, a.beams, red);
-    if (mine >= bound) {
-        for (uint32_t i = tid; i < total; i += BEAM_THREADS) {
-            if (take(i, &c) && (float)c.score >= bound) {
+    /* ---- what reaches it */
+    for (uint32_t i = tid; i < lists; i += BEAM_THREADS) {
+        bool more = true;
+        for (int k0 = 0; more && k0 < a.beams; k0 += 4) {
+            BeamCandidate q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = best[(int64_t)i * a.beams + (k0 + j < a.beams ? k0 + j : k0)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (!more) continue;
+                const double sc = score_of(i, (uint32_t)(k0 + j), q[j]);
+                more = k0 + j < a.beams && (float)sc >= bound;
+                if (!more) continue;
                 const int at = atomicAdd(&n_list, 1);
-                if (at < BEAM_LIST) list[at] = c;
+                if (at < BEAM_LIST) list[at] = BeamScored{sc, place_of(i, q[j])};
             }
         }
     }
@@ -320,8 +371,12 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
     BeamScored last{(double)INFINITY, -1};
     for (int k = 0; k < a.beams; ++k) {
         BeamScored b = none;
-        for (uint32_t i = tid; i < total; i += BEAM_THREADS)
-            if (take(i, &c) && beam_before(last, c) && beam_before(c, b)) b = c;
+        for (uint32_t i = tid; i < lists; i += BEAM_THREADS)
+            for (int j = 0; j < a.beams; ++j) {
+                const BeamCandidate q = best[(int64_t)i * a.beams + j];
+                const BeamScored c{score_of(i, (uint32_t)j, q), place_of(i, q)};
+                if (c.score > -(double)INFINITY && beam_before(last, c) && beam_before(c, b)) b = c;
+            }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             const BeamScored q{__shfl_xor(b.score, o), (int64_t)__shfl_xor((long long)b.place, o)};
