@@ -23,11 +23,15 @@ TreeKernel pick_kind(bool f16, int kind)
     }
 }
 
+template <int DP>
+TreeKernel pick_cols(int cols, bool f16, int kind)
+{
+    return cols == 32 ? pick_kind<DP, 1>(f16, kind) : pick_kind<DP, 4>(f16, kind);
+}
+
 TreeKernel pick(int dim, int cols, bool f16, int kind)
 {
-    if (dim <= 64) return cols == 32 ? pick_kind<64, 1>(f16, kind) : pick_kind<64, 4>(f16, kind);
-    if (dim <= 128) return cols == 32 ? pick_kind<128, 1>(f16, kind) : pick_kind<128, 4>(f16, kind);
-    return cols == 32 ? pick_kind<256, 1>(f16, kind) : pick_kind<256, 4>(f16, kind);
+    return dim <= 64 ? pick_cols<64>(cols, f16, kind) : dim <= 128 ? pick_cols<128>(cols, f16, kind) : pick_cols<256>(cols, f16, kind);
 }
 
 /* How a call is cut into blocks: by its sizes and bounds alone, so that the
@@ -46,12 +50,12 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
 {
     const int64_t group = n_q_heads / c->n_heads, cols = (int64_t)r->max_length * group;
     if (cols > INT32_MAX) return PARASON_ERR_SIZE;
-    p->cols = cols <= 32 ? 32 : 128;
+    p->cols = cols <= 64 ? 32 : 128;
     p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
     const int64_t base = r->n_rows * c->n_heads * p->q_blocks;
     const int64_t tile = p->cols == 32 ? 128 : 64;
-    int64_t len = 4096;
-    while (len > 2 * tile && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
+    int64_t len = 2048;
+    while (len > 512 && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
     const size_t per_part = (size_t)r->n_tokens * n_q_heads * c->head_dim * 4;
     int64_t parts = (r->max_kv_len + len - 1) / len;
     if (parts < 1 || base >= PART_BLOCKS) parts = 1;

@@ -87,6 +87,21 @@ __device__ __forceinline__ uint2 widen4(uint32_t w)
     return make_uint2(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]));
 }
 
+/* Eight codes to the operand of a product. */
+template <bool F16, int KIND>
+__device__ __forceinline__ frag8 widen8(uint2 w)
+{
+    const uint2 a = widen4<F16, KIND>(w.x), b = widen4<F16, KIND>(w.y);
+    return __builtin_bit_cast(frag8, make_uint4(a.x, a.y, b.x, b.y));
+}
+
+/* Whether one of four e4m3 codes is NaN (all ones below the sign). */
+__device__ __forceinline__ bool any_nan_code(uint32_t w)
+{
+    const uint32_t y = ~w & 0x7F7F7F7Fu; /* a zero byte for each */
+    return ((y - 0x01010101u) & ~y & 0x80808080u) != 0u;
+}
+
 /* Whether one of two 16-bit values is an infinity or NaN. */
 template <bool F16>
 __device__ __forceinline__ bool not_finite2(uint32_t w)
@@ -101,18 +116,26 @@ __device__ __forceinline__ float widen1(uint16_t h) { return F16 ? f16_to_f32(h)
 constexpr int TREE_THREADS = 256;
 constexpr int TREE_SKIP_WORDS = 64; /* of the list of a tree's tiles that nobody in the block sees: 2,048 tiles */
 
-template <int DP, int WQ>
+template <int DP, int WQ, int KIND>
 struct TreeShape {
-    static constexpr int TK = WQ == 1 ? 128 : 64;     /* positions of a tile */
-    static constexpr int KW = WQ == 1 ? 32 : 64;      /* of it, those of one wave */
+    static constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
+    /* Few columns: every wave has the same ones and its own positions of a tile, and needs the others only at the end. */
+    static constexpr bool SOLO = WQ == 1;
+    /* Codes go to LDS as they are where one wave reads them again, and are widened behind it; where all four waves take
+     * the same positions they are widened once, in front. */
+    static constexpr bool RAW = CODES && SOLO;
+    static constexpr int WK = 4 / WQ;                 /* waves that take the same columns */
+    static constexpr int TK = SOLO ? 128 : 64;        /* positions of a tile */
+    static constexpr int KW = TK / WK;                /* of it, those of one wave */
     static constexpr int SUBS = KW / 32;
     static constexpr int COLS = 32 * WQ;              /* queries of a block */
-    /* rows of 16-bit values in LDS: 16 bytes more than a multiple of 128 spread the
-     * 16-byte reads of K over the banks, 64 bytes more the transposed reads of V */
-    static constexpr int KS = DP + 8, VS = DP + 32;
-    static constexpr int KBYTES = TK * KS * 2, VBYTES = TK * VS * 2;
+    /* rows in LDS: 16 bytes more than a multiple of 128 spread the reads of K over the banks, 64 bytes more the
+     * transposed reads of 16-bit V */
+    static constexpr int ES = RAW ? 1 : 2;            /* bytes of a value in LDS */
+    static constexpr int KS = RAW ? DP + 16 : DP + 8, VS = RAW ? DP + 16 : DP + 32; /* values */
+    static constexpr int KBYTES = TK * KS * ES, VBYTES = TK * VS * ES;
     static constexpr int OS = DP + 4;                 /* floats of a row of the waves' results when they are joined */
-    static constexpr int JOIN = WQ == 1 ? 4 * 32 * OS * 4 : 0;
+    static constexpr int JOIN = (WK - 1) * COLS * OS * 4;
     static constexpr int TILE = KBYTES + VBYTES > JOIN ? KBYTES + VBYTES : JOIN;
 };
 
@@ -148,9 +171,9 @@ __device__ __forceinline__ int32_t parts_of(const TreeArgs &a, int32_t end)
 template <int DP, int WQ, bool F16, int KIND>
 __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention(TreeArgs a)
 {
-    typedef TreeShape<DP, WQ> Sh;
+    typedef TreeShape<DP, WQ, KIND> Sh;
     constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
-    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
+    constexpr bool CODES = Sh::CODES, RAW = Sh::RAW;
     constexpr bool PF16 = KIND == KV_F16;   /* type of the weights and of V: bfloat16 for codes, whose scales are in the weights */
     /* float16 results over codes: the weights go in as two bfloat16 terms, so that they are not the coarsest step of
      * the whole.  (float16 weights would lose all precision where the positions with nearly all of the weight hold a
@@ -159,23 +182,26 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     /* The largest weight is 2^LIFT: of float16's 30 binades of full precision 29 are then below it. */
     constexpr int LIFT = PF16 ? 15 : 0;
     constexpr int VE = CODES ? 16 : 8;      /* values of a 16-byte piece of the cache */
-    constexpr int VPR = DP / VE, RPP = TREE_THREADS / VPR, NP = TK / RPP;
+    /* a tile's rows are loaded by the block, or its own ones by a wave */
+    constexpr int LOADERS = Sh::SOLO ? 64 : TREE_THREADS, ROWS = Sh::SOLO ? Sh::KW : TK;
+    constexpr int VPR = DP / VE, RPP = LOADERS / VPR, NP = ROWS / RPP;
     constexpr int ES = CODES ? 1 : 2;
     constexpr int NK = DP / 16, ND = DP / 32;
-    static_assert(NP >= 1 && NP * RPP == TK, "the block's loads cover a tile");
+    static_assert(NP >= 1 && NP * RPP == ROWS, "the loads cover a tile");
 
     __shared__ __attribute__((aligned(16))) char tile[Sh::TILE];
     __shared__ __attribute__((aligned(16))) float k_sc[CODES ? TK : 4], v_sc[CODES ? TK : 4];
     __shared__ int64_t place[TK];
     __shared__ int32_t v_stamp[TK];
     __shared__ uint32_t skip[TREE_SKIP_WORDS];
-    __shared__ int32_t flags[2];            /* a bad page; the last tile with a value of V that is not finite */
-    __shared__ float join_ml[2][4][32];
-    uint16_t *const Ks = reinterpret_cast<uint16_t *>(tile), *const Vs = Ks + TK * KS;
+    __shared__ int32_t flags[2];            /* a bad page; the last tile with a value of V that is not finite (of the block) */
+    __shared__ float join_ml[2][Sh::WK][Sh::COLS];
+    char *const Ks = tile, *const Vs = tile + Sh::KBYTES;
+    constexpr int LS = Sh::ES;              /* bytes of a value there */
 
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 31, h = lane >> 5;
-    const int wq = WQ == 1 ? 0 : wave, wk = WQ == 1 ? wave : 0;
+    const int wq = wave % WQ, wk = wave / WQ, k0 = wk * Sh::KW;
 
     /* ---- which row, cache head, part and columns */
     int64_t unit;
@@ -277,52 +303,60 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     };
 
     /* ---- loads: a position's page a tile ahead of its keys and values, these a tile ahead of their use */
-    const int32_t my_piece = tid % VPR, my_row = tid / VPR;
+    const int32_t loader = Sh::SOLO ? lane : tid, row0 = Sh::SOLO ? k0 : 0; /* who loads what of a tile */
+    const int32_t my_piece = loader % VPR, my_row = row0 + loader / VPR;
     const bool piece_live = my_piece * VE < a.c.head_dim;
     const char *const kb = a.c.k + ((int64_t)head * a.c.stride_head + my_piece * VE) * ES;
     const char *const vb = a.c.v + ((int64_t)head * a.c.stride_head + my_piece * VE) * ES;
-    int32_t pg = -1, pg_slot = 0;            /* of position tid of a tile */
+    auto together = [&]() {                  /* what a loader put into LDS is there for the others */
+        if (!Sh::SOLO) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    int32_t pg = -1, pg_slot = 0;            /* of position row0 + loader of a tile */
     auto load_page = [&](int32_t x) {
-        const int32_t p = x * TK + tid;
+        const int32_t p = x * TK + row0 + loader;
         pg = -1;
-        if (tid < TK && p < k_end) {
+        if (loader < ROWS && p < k_end) {
             const uint32_t nth = div_by((uint32_t)p, a.c.page_div);
             pg_slot = p - (int32_t)(nth * (uint32_t)a.c.page_size);
             pg = a.r.pages[row * a.r.pages_stride + nth];
             if (pg < 0 || pg >= a.c.n_pages) pg = -2;
         }
     };
-    float ks_next = 0.0f, vs_next = 0.0f;
+    int64_t scale_at = -1;
     auto put_place = [&]() {
-        if (tid < TK) {
+        if (loader < ROWS) {
             if (pg == -2) flags[0] = 0;
-            place[tid] = pg < 0 ? -1 : (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
-            if (CODES) {
-                ks_next = vs_next = 0.0f;
-                if (pg >= 0) {
-                    const int64_t at = (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
-                                       (int64_t)head * a.c.scale_stride_head;
-                    ks_next = a.c.k_scale[at];
-                    vs_next = a.c.v_scale[at];
-                }
-            }
+            place[row0 + loader] = pg < 0 ? -1 : (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
+            if (CODES)
+                scale_at = pg < 0 ? -1 : (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
+                                             (int64_t)head * a.c.scale_stride_head;
         }
     };
     uint4 kr[NP], vr[NP];
+    float k_scale = 0.0f, v_scale = 0.0f;    /* of position row0 + loader */
     auto load_tile = [&]() {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const int64_t at = place[my_row + p * RPP];
+            const int64_t from = place[my_row + p * RPP];
             kr[p] = vr[p] = make_uint4(0u, 0u, 0u, 0u);
-            if (at >= 0 && piece_live) {
-                kr[p] = *reinterpret_cast<const uint4 *>(kb + at * ES);
-                vr[p] = *reinterpret_cast<const uint4 *>(vb + at * ES);
+            if (from >= 0 && piece_live) {
+                kr[p] = *reinterpret_cast<const uint4 *>(kb + from * ES);
+                vr[p] = *reinterpret_cast<const uint4 *>(vb + from * ES);
             }
+        }
+        if (CODES) {
+            k_scale = v_scale = 0.0f;
+            if (loader < ROWS && scale_at >= 0) k_scale = a.c.k_scale[scale_at], v_scale = a.c.v_scale[scale_at];
         }
     };
     uint64_t m_lo = 0, m_hi = 0;             /* mask words of a tile's positions of this wave */
     auto load_mask = [&](int32_t x) {
-        const int32_t b = x * TK + wk * 32 - sp.base;
+        const int32_t b = x * TK + k0 - sp.base;
         m_lo = m_hi = 0;
         if (a.mask && live && b + Sh::KW > 0) {
             const int32_t i = b < 0 ? 0 : b >> 6;
@@ -334,69 +368,77 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     acc16 o[ND] = {};
     float at = -INFINITY, l = 0.0f;          /* the exponent that o and l are relative to; this lane's share of the sum */
 
+    /* tiles in turn: the one in work, and the one behind it */
     int32_t x = next_tile(k_begin / TK);
-    if (x < t_end) {
-        load_page(x);
-        put_place();
-        __syncthreads();
-        load_tile();
-        load_mask(x);
-        __syncthreads();
-    }
     int32_t x1 = x < t_end ? next_tile(x + 1) : t_end;
-    float ks_now = ks_next, vs_now = vs_next;
-    if (x1 < t_end) load_page(x1);
+    load_page(x);
+    put_place();
+    together();
+    load_page(x1);
+    load_mask(x);
+    load_tile();
+    together();
     while (x < t_end) {
         const int32_t kp = x * TK;
-        const bool masked = kp + TK > open || kp + TK > k_end; /* some column does not see all of the tile */
-        /* ---- the tile goes to LDS */
-        if (x1 < t_end) put_place();         /* (nobody reads the tile's places any more) */
-        if (CODES && tid < TK) k_sc[tid] = ks_now, v_sc[tid] = vs_now;
-        ks_now = ks_next, vs_now = vs_next;
+        /* some column does not see all of the tile (of the wave's part of it) */
+        const bool masked = kp + row0 + ROWS > open || kp + row0 + ROWS > k_end;
+        /* ---- the tile goes to LDS; the next page's places (nobody reads the last ones any more) */
+        put_place();
+        if (CODES && loader < ROWS) k_sc[row0 + loader] = k_scale, v_sc[row0 + loader] = v_scale;
+        bool odd_seen = false;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int r = my_row + p * RPP;
-            if (CODES) {
+            char *const kd = Ks + (r * KS + my_piece * VE) * LS, *const vd = Vs + (r * VS + my_piece * VE) * LS;
+            if (CODES && !RAW) {
                 const uint32_t kw[4] = {kr[p].x, kr[p].y, kr[p].z, kr[p].w}, vw[4] = {vr[p].x, vr[p].y, vr[p].z, vr[p].w};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const uint2 k0 = widen4<F16, KIND>(kw[2 * i]), k1 = widen4<F16, KIND>(kw[2 * i + 1]);
-                    *reinterpret_cast<uint4 *>(Ks + r * KS + my_piece * VE + 8 * i) = make_uint4(k0.x, k0.y, k1.x, k1.y);
-                    const uint2 v0 = widen4<PF16, KIND>(vw[2 * i]), v1 = widen4<PF16, KIND>(vw[2 * i + 1]);
-                    *reinterpret_cast<uint4 *>(Vs + r * VS + my_piece * VE + 8 * i) = make_uint4(v0.x, v0.y, v1.x, v1.y);
-                    if (KIND == KV_FP8 && masked &&
-                        (not_finite2<PF16>(v0.x) || not_finite2<PF16>(v0.y) || not_finite2<PF16>(v1.x) || not_finite2<PF16>(v1.y)))
-                        v_stamp[r] = flags[1] = x;
+                    *reinterpret_cast<frag8 *>(kd + 16 * i) = widen8<F16, KIND>(make_uint2(kw[2 * i], kw[2 * i + 1]));
+                    *reinterpret_cast<frag8 *>(vd + 16 * i) = widen8<PF16, KIND>(make_uint2(vw[2 * i], vw[2 * i + 1]));
                 }
             } else {
-                *reinterpret_cast<uint4 *>(Ks + r * KS + my_piece * VE) = kr[p];
-                *reinterpret_cast<uint4 *>(Vs + r * VS + my_piece * VE) = vr[p];
-                if (masked && (not_finite2<PF16>(vr[p].x) || not_finite2<PF16>(vr[p].y) || not_finite2<PF16>(vr[p].z) ||
-                               not_finite2<PF16>(vr[p].w)))
-                    v_stamp[r] = flags[1] = x;
+                *reinterpret_cast<uint4 *>(kd) = kr[p];
+                *reinterpret_cast<uint4 *>(vd) = vr[p];
+            }
+            if (masked) {
+                const uint4 v = vr[p];
+                const bool odd = KIND == KV_INT8 ? false
+                                 : KIND == KV_FP8 ? any_nan_code(v.x) || any_nan_code(v.y) || any_nan_code(v.z) || any_nan_code(v.w)
+                                                  : not_finite2<PF16>(v.x) || not_finite2<PF16>(v.y) || not_finite2<PF16>(v.z) ||
+                                                        not_finite2<PF16>(v.w);
+                if (odd) v_stamp[r] = x, odd_seen = true;
             }
         }
-        const uint64_t lo = m_lo, hi = m_hi;
-        __syncthreads();
-        /* ---- the next tile is on its way */
-        const int32_t x2 = x1 < t_end ? next_tile(x1 + 1) : t_end;
-        if (x1 < t_end) {
-            load_tile();
-            load_mask(x1);
-            if (x2 < t_end) load_page(x2);
+        bool odd_values = false;             /* of the wave's positions, or of the block's */
+        if (masked && KIND != KV_INT8) {
+            if (Sh::SOLO) odd_values = __ballot(odd_seen) != 0;
+            else if (odd_seen) flags[1] = x;
         }
+        const uint64_t lo = m_lo, hi = m_hi;
+        together();
+        if (masked && KIND != KV_INT8 && !Sh::SOLO) odd_values = flags[1] == x;
+        /* ---- the next one is on its way (loads come back in order, so what is needed first goes first) */
+        const int32_t x2 = x1 < t_end ? next_tile(x1 + 1) : t_end;
+        load_page(x2);
+        load_mask(x1);
+        load_tile();
         /* ---- S^T */
         acc16 s[SUBS];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
             s[u] = acc16{};
-            const uint16_t *ka = Ks + (wk * 32 + u * 32 + n) * KS + h * 8;
+            const char *ka = Ks + ((k0 + u * 32 + n) * KS + h * 8) * LS;
 #pragma unroll
-            for (int k = 0; k < NK; ++k) s[u] = mma<F16>(*reinterpret_cast<const frag8 *>(ka + k * 16), qf[k], s[u]);
+            for (int k = 0; k < NK; ++k) {
+                const frag8 kf = RAW ? widen8<F16, KIND>(*reinterpret_cast<const uint2 *>(ka + k * 16))
+                                     : *reinterpret_cast<const frag8 *>(ka + k * 32);
+                s[u] = mma<F16>(kf, qf[k], s[u]);
+            }
             if (CODES) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float4 f = *reinterpret_cast<const float4 *>(&k_sc[wk * 32 + u * 32 + 8 * i + 4 * h]);
+                    const float4 f = *reinterpret_cast<const float4 *>(&k_sc[k0 + u * 32 + 8 * i + 4 * h]);
                     s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
                 }
             }
@@ -408,7 +450,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
         if (masked) {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
-                const int32_t p0 = kp + wk * 32 + u * 32;
+                const int32_t p0 = kp + k0 + u * 32;
                 const int32_t left = (my_end < k_end ? my_end : k_end) - p0;
                 uint32_t m = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
                 if (a.mask) {
@@ -465,7 +507,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                 const uint32_t mine = see[u] >> (4 * h);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float4 f = *reinterpret_cast<const float4 *>(&v_sc[wk * 32 + u * 32 + 8 * i + 4 * h]);
+                    const float4 f = *reinterpret_cast<const float4 *>(&v_sc[k0 + u * 32 + 8 * i + 4 * h]);
                     s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
                 }
                 if (masked) {                /* no scale, whatever it is, makes a weight where nothing is seen */
@@ -476,8 +518,10 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
             }
         }
         /* ---- O^T */
-        const bool odd_values = masked && flags[1] == x;
-        const uint16_t *va = Vs + (wk * 32 + 4 * h + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        /* transposed reads: each 16 lanes name four (codes: eight) rows of 16 values and get a column each */
+        const int g16 = ((lane >> 4) & 1) * 16, i16 = lane & 15;
+        const char *va = RAW ? Vs + (k0 + 4 * h + ((i16 >> 1) & 3) + 8 * (i16 >> 3)) * VS + g16 + (i16 & 1) * 8
+                             : Vs + ((k0 + 4 * h + (i16 >> 2)) * VS + g16 + (i16 & 3) * 4) * 2;
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
 #pragma unroll
@@ -496,11 +540,19 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                 }
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
+                    typedef int int2v __attribute__((ext_vector_type(2)));
                     typedef __attribute__((address_space(3))) frag4 lds4;
-                    const uint16_t *v0 = va + (u * 32 + k * 16) * VS + d * 32;
-                    const frag4 f0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)v0);
-                    const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + 8 * VS));
-                    frag8 vf = __builtin_shufflevector(f0, f1, 0, 1, 2, 3, 4, 5, 6, 7);
+                    typedef __attribute__((address_space(3))) int2v lds8;
+                    const char *v0 = va + ((u * 32 + k * 16) * VS + d * 32) * LS;
+                    frag8 vf;
+                    if (RAW) {
+                        const int2v f = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8 *)v0);
+                        vf = widen8<PF16, KIND>(make_uint2((uint32_t)f.x, (uint32_t)f.y));
+                    } else {
+                        const frag4 f0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)v0);
+                        const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + 8 * VS * LS));
+                        vf = __builtin_shufflevector(f0, f1, 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
                     if (odd_values) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
@@ -517,7 +569,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
                 for (int kk = 0; kk < 32; ++kk) {
-                    const int r = wk * 32 + u * 32 + kk;
+                    const int r = k0 + u * 32 + kk;
                     if (v_stamp[r] != x) continue;
                     float p = 0.0f;
 #pragma unroll
@@ -528,15 +580,15 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const uint16_t v = Vs[r * VS + d * 32 + 8 * (i / 4) + 4 * h + (i & 3)];
+                            const char *e = Vs + (r * VS + d * 32 + 8 * (i / 4) + 4 * h + (i & 3)) * LS;
+                            const uint16_t v = RAW ? (uint16_t)widen4<PF16, KIND>((uint8_t)*e).x : *reinterpret_cast<const uint16_t *>(e);
                             if (not_finite2<PF16>(v)) o[d][i] += p * widen1<PF16>(v);
                         }
                 }
             }
         }
-        __syncthreads();
-        x = x1;
-        x1 = x2;
+        together();
+        x = x1, x1 = x2;
     }
     __syncthreads();
     const bool bad = !sp.ok || flags[0] == 0;
@@ -545,55 +597,41 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     /* ---- results */
     l += __shfl_xor(l, 32);
     const float nan = __uint_as_float(0x7FC00000u);
-    if (WQ == 1) {
-        /* join the waves: every column's maximum and sum over the four, then their shares of O */
+    if (Sh::WK > 1) {
+        /* the waves of the same columns: the maximum and the sum over them, then their shares of O, which the first
+         * adds to its own */
         float *const Os = reinterpret_cast<float *>(tile);
-        if (h == 0) join_ml[0][wave][n] = at, join_ml[1][wave][n] = l;
+        const int c = wq * 32 + n;
+        if (h == 0) join_ml[0][wk][c] = at, join_ml[1][wk][c] = l;
         __syncthreads();
-        float m4 = -INFINITY, sum = 0.0f;
+        float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m4 = fmaxf(m4, join_ml[0][i][n]);
-        const float ref = m4 == -INFINITY ? 0.0f : m4;
+        for (int i = 0; i < Sh::WK; ++i) top = fmaxf(top, join_ml[0][i][c]);
+        const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += join_ml[1][i][n] * __builtin_amdgcn_exp2f(join_ml[0][i][n] - ref);
+        for (int i = 0; i < Sh::WK; ++i) sum += join_ml[1][i][c] * __builtin_amdgcn_exp2f(join_ml[0][i][c] - ref);
         const float f = __builtin_amdgcn_exp2f(at - ref);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<float4 *>(&Os[(wave * 32 + n) * Sh::OS + d * 32 + 8 * i + 4 * h]) =
-                    make_float4(o[d][4 * i] * f, o[d][4 * i + 1] * f, o[d][4 * i + 2] * f, o[d][4 * i + 3] * f);
-        if (bad) sum = nan;
+            for (int i = 0; i < 4; ++i) {
+                o[d][4 * i] *= f, o[d][4 * i + 1] *= f, o[d][4 * i + 2] *= f, o[d][4 * i + 3] *= f;
+                if (wk > 0)
+                    *reinterpret_cast<float4 *>(&Os[((wk - 1) * Sh::COLS + c) * Sh::OS + d * 32 + 8 * i + 4 * h]) =
+                        make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+            }
+        at = top, l = sum;
         __syncthreads();
-        if (wave == 0 && h == 0) join_ml[0][0][n] = m4, join_ml[1][0][n] = sum;
-        __syncthreads();
-        const int D4 = a.c.head_dim / 4, cols = (sp.tok1 - sp.tok0) * a.group;
-        for (int i = tid; i < cols * D4; i += TREE_THREADS) {
-            const int c = i / D4, d = (i - c * D4) * 4;
-            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (wk > 0) return;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float4 z = *reinterpret_cast<const float4 *>(&Os[(k * 32 + c) * Sh::OS + d]);
-                y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
-            }
-            const float m_c = join_ml[0][0][c], s_c = join_ml[1][0][c];
-            const int32_t tk = (int32_t)div_by((uint32_t)(q_block * Sh::COLS + c), a.group_div);
-            const int32_t qh = head * a.group + (q_block * Sh::COLS + c - tk * a.group);
-            const int64_t un = (w.start + tk) * a.n_q_heads + qh;
-            if (my_parts > 1) {
-                *reinterpret_cast<float4 *>(a.part_out + (un * a.parts + part) * a.c.head_dim + d) = y;
-                if (d == 0) a.part_ml[un * a.parts + part] = make_float2(m_c, s_c);
-                continue;
-            }
-            const float inv = s_c == 0.0f ? 0.0f : 1.0f / s_c;
-            uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + (w.start + tk) * a.out_stride_token + qh * a.out_stride_head + d;
-            y.x *= inv, y.y *= inv, y.z *= inv, y.w *= inv;
-            const uint2 p = make_uint2(pack2<F16>(y.x, y.y), pack2<F16>(y.z, y.w));
-            if (a.out_wide) *reinterpret_cast<uint2 *>(dst) = p;
-            else dst[0] = (uint16_t)p.x, dst[1] = (uint16_t)(p.x >> 16), dst[2] = (uint16_t)p.y, dst[3] = (uint16_t)(p.y >> 16);
-            if (d == 0 && a.lse) a.lse[un] = s_c == 0.0f ? -INFINITY : (m_c + __builtin_amdgcn_logf(s_c)) * 0.6931471805599453f;
-        }
-        return;
+        for (int k = 0; k < Sh::WK - 1; ++k)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 z = *reinterpret_cast<const float4 *>(&Os[(k * Sh::COLS + c) * Sh::OS + d * 32 + 8 * i + 4 * h]);
+                    o[d][4 * i] += z.x, o[d][4 * i + 1] += z.y, o[d][4 * i + 2] += z.z, o[d][4 * i + 3] += z.w;
+                }
     }
     if (!live) return;
     if (bad) l = nan;
@@ -628,8 +666,8 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 }
 
 /* A wave per (token, query head) joins the parts of its row: the parts' maxima
- * give their factors, the sums and the vectors are added in the order of the
- * parts. */
+ * give their factors, the sums and the vectors are added in an order that the
+ * sizes fix.  Four values a lane, so several parts at once. */
 template <bool F16>
 __global__ void __launch_bounds__(TREE_THREADS) tree_join(TreeArgs a, int cols)
 {
@@ -638,7 +676,8 @@ __global__ void __launch_bounds__(TREE_THREADS) tree_join(TreeArgs a, int cols)
     const int64_t i = (int64_t)blockIdx.x * (TREE_THREADS / 64) + (threadIdx.x >> 6);
     const int64_t row = i / per_row;
     if (row >= a.r.n_rows) return;
-    const int32_t tok = (int32_t)(i % per_row / a.n_q_heads), q_head = (int32_t)(i % a.n_q_heads);
+    const int32_t tok = (int32_t)((uint32_t)(i - row * per_row) / (uint32_t)a.n_q_heads);
+    const int32_t q_head = (int32_t)(i - row * per_row - (int64_t)tok * a.n_q_heads);
     const KvRow w = load_row(a.r, a.c, row, false);
     if (!w.out_ok || tok >= w.length) return;
     const int32_t col = tok * a.group + q_head % a.group;
@@ -652,29 +691,41 @@ __global__ void __launch_bounds__(TREE_THREADS) tree_join(TreeArgs a, int cols)
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
     const float ref = m == -INFINITY ? 0.0f : m;
-    float y[4] = {}, sum = 0.0f;
-    for (int32_t p0 = 0; p0 < parts; p0 += 64) {
-        float f = 0.0f, fl = 0.0f;
-        if (p0 + lane < parts) {
-            const float2 v = ml[p0 + lane];
-            f = __builtin_amdgcn_exp2f(v.x - ref);
-            fl = v.y * f;
-        }
-        const int here = parts - p0 < 64 ? parts - p0 : 64;
-        for (int k = 0; k < here; ++k) {
-            const float g = __shfl(f, k);
-            sum += __shfl(fl, k);
-            const float *src = a.part_out + (un * a.parts + p0 + k) * a.c.head_dim;
+    int lanes = 4; /* of a part */
+    while (lanes * 4 < a.c.head_dim) lanes <<= 1;
+    const int at_once = 64 / lanes, d = (lane & (lanes - 1)) * 4;
+    const bool mine = d < a.c.head_dim;
+    const float *src = a.part_out + un * a.parts * a.c.head_dim + (mine ? d : 0);
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float sum = 0.0f;
+    auto add = [&](const float2 &v, const float4 &z) {
+        const float f = __builtin_amdgcn_exp2f(v.x - ref);
+        sum += v.y * f;
+        y.x += z.x * f, y.y += z.y * f, y.z += z.z * f, y.w += z.w * f;
+    };
+    int32_t p = lane / lanes;
+    for (; p + 3 * at_once < parts; p += 4 * at_once) {
+        float2 v[4];
+        float4 z[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e * 64 + lane < a.c.head_dim) y[e] += g * src[e * 64 + lane];
+        for (int k = 0; k < 4; ++k) {
+            v[k] = ml[p + k * at_once];
+            z[k] = *reinterpret_cast<const float4 *>(src + (int64_t)(p + k * at_once) * a.c.head_dim);
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add(v[k], z[k]);
     }
+    for (; p < parts; p += at_once) add(ml[p], *reinterpret_cast<const float4 *>(src + (int64_t)p * a.c.head_dim));
+    for (int k = 32; k >= lanes; k >>= 1) {
+        sum += __shfl_xor(sum, k);
+        y.x += __shfl_xor(y.x, k), y.y += __shfl_xor(y.y, k), y.z += __shfl_xor(y.z, k), y.w += __shfl_xor(y.w, k);
+    }
+    if (lane >= lanes || !mine) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + (w.start + tok) * a.out_stride_token + q_head * a.out_stride_head;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e * 64 + lane < a.c.head_dim) dst[e * 64 + lane] = (uint16_t)(F16 ? f32_to_f16(y[e] * inv) : f32_to_bf16(y[e] * inv));
+    const uint2 r = make_uint2(pack2<F16>(y.x * inv, y.y * inv), pack2<F16>(y.z * inv, y.w * inv));
+    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + (w.start + tok) * a.out_stride_token + q_head * a.out_stride_head + d;
+    if (a.out_wide) *reinterpret_cast<uint2 *>(dst) = r;
+    else dst[0] = (uint16_t)r.x, dst[1] = (uint16_t)(r.x >> 16), dst[2] = (uint16_t)r.y, dst[3] = (uint16_t)(r.y >> 16);
     if (lane == 0 && a.lse) a.lse[un] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
