@@ -12,21 +12,21 @@ namespace {
 
 typedef void (*TreeKernel)(pk::TreeArgs);
 
-template <int DP, int WQ>
+template <int DP, int COLS>
 TreeKernel pick_kind(bool f16, int kind)
 {
     switch (kind) {
-    case pk::KV_BF16: return pk::tree_attention<DP, WQ, false, pk::KV_BF16>;
-    case pk::KV_F16: return pk::tree_attention<DP, WQ, true, pk::KV_F16>;
-    case pk::KV_FP8: return f16 ? pk::tree_attention<DP, WQ, true, pk::KV_FP8> : pk::tree_attention<DP, WQ, false, pk::KV_FP8>;
-    default: return f16 ? pk::tree_attention<DP, WQ, true, pk::KV_INT8> : pk::tree_attention<DP, WQ, false, pk::KV_INT8>;
+    case pk::KV_BF16: return pk::tree_attention<DP, COLS, false, pk::KV_BF16>;
+    case pk::KV_F16: return pk::tree_attention<DP, COLS, true, pk::KV_F16>;
+    case pk::KV_FP8: return f16 ? pk::tree_attention<DP, COLS, true, pk::KV_FP8> : pk::tree_attention<DP, COLS, false, pk::KV_FP8>;
+    default: return f16 ? pk::tree_attention<DP, COLS, true, pk::KV_INT8> : pk::tree_attention<DP, COLS, false, pk::KV_INT8>;
     }
 }
 
 template <int DP>
 TreeKernel pick_cols(int cols, bool f16, int kind)
 {
-    return cols == 32 ? pick_kind<DP, 1>(f16, kind) : pick_kind<DP, 4>(f16, kind);
+    return cols == 16 ? pick_kind<DP, 16>(f16, kind) : cols == 32 ? pick_kind<DP, 32>(f16, kind) : pick_kind<DP, 128>(f16, kind);
 }
 
 TreeKernel pick(int dim, int cols, bool f16, int kind)
@@ -43,22 +43,22 @@ struct TreePlan {
     size_t ml, end; /* workspace: the parts' vectors at 0, their maxima and sums at ml */
 };
 
-constexpr int64_t PART_BLOCKS = 2048;            /* blocks that a call is cut into */
+constexpr int64_t PART_BLOCKS = 1024;            /* blocks that a call is cut into */
 constexpr size_t PART_BYTES = (size_t)1 << 29;   /* of the parts' vectors */
 
 int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads, TreePlan *p)
 {
     const int64_t group = n_q_heads / c->n_heads, cols = (int64_t)r->max_length * group;
     if (cols > INT32_MAX) return PARASON_ERR_SIZE;
-    p->cols = cols <= 64 ? 32 : 128;
+    p->cols = cols <= 16 ? 16 : cols <= 64 ? 32 : 128;
     p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
     const int64_t base = r->n_rows * c->n_heads * p->q_blocks;
-    const int64_t tile = p->cols == 32 ? 128 : 64;
-    int64_t len = 2048;
+    const int64_t tile = p->cols < 128 ? 128 : 64;
+    int64_t len = 1024;
     while (len > 512 && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
     const size_t per_part = (size_t)r->n_tokens * n_q_heads * c->head_dim * 4;
     int64_t parts = (r->max_kv_len + len - 1) / len;
-    if (parts < 1 || base >= PART_BLOCKS) parts = 1;
+    if (parts < 1 || base >= 16 * PART_BLOCKS) parts = 1;
     if (per_part > 0 && (size_t)parts > PART_BYTES / per_part) parts = PART_BYTES / per_part > 1 ? (int64_t)(PART_BYTES / per_part) : 1;
     len = (r->max_kv_len + parts - 1) / parts;
     p->part_len = (int32_t)((len + tile - 1) / tile * tile < INT32_MAX ? (len + tile - 1) / tile * tile : len);

@@ -51,6 +51,24 @@ struct TreeArgs {
 typedef short frag8 __attribute__((ext_vector_type(8)));
 typedef short frag4 __attribute__((ext_vector_type(4)));
 typedef float acc16 __attribute__((ext_vector_type(16)));
+typedef float acc4 __attribute__((ext_vector_type(4)));
+template <int CN>
+struct Acc {
+    typedef acc16 type;
+};
+template <>
+struct Acc<16> {
+    typedef acc4 type;
+};
+
+template <bool F16>
+__device__ __forceinline__ acc4 mma(frag8 a, frag8 b, acc4 c)
+{
+    typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+    if (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
 
 template <bool F16>
 __device__ __forceinline__ acc16 mma(frag8 a, frag8 b, acc16 c)
@@ -116,19 +134,24 @@ __device__ __forceinline__ float widen1(uint16_t h) { return F16 ? f16_to_f32(h)
 constexpr int TREE_THREADS = 256;
 constexpr int TREE_SKIP_WORDS = 64; /* of the list of a tree's tiles that nobody in the block sees: 2,048 tiles */
 
-template <int DP, int WQ, int KIND>
+/* A block of COLS columns: 16 or 32 of them that all four waves take, or 128, 32 a wave. */
+template <int DP, int COLS, int KIND>
 struct TreeShape {
     static constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
-    /* Few columns: every wave has the same ones and its own positions of a tile, and needs the others only at the end. */
-    static constexpr bool SOLO = WQ == 1;
+    /* Few columns: every wave has its own positions of a tile, and needs the others only at the end. */
+    static constexpr bool SOLO = COLS < 128;
     /* Codes go to LDS as they are where one wave reads them again, and are widened behind it; where all four waves take
      * the same positions they are widened once, in front. */
     static constexpr bool RAW = CODES && SOLO;
+    /* columns of a product, CN x CN results; the 64 / CN lanes of a column hold these positions of 32:
+     * KSTEP * (i / 4) + 4 * (lane / CN) + i % 4, and these rows of O^T of CN: 8 * (i / 4) + 4 * (lane / CN) + i % 4 */
+    static constexpr int CN = COLS == 16 ? 16 : 32, G = 64 / CN, NV = 32 / G, KSTEP = 128 / NV;
+    static constexpr int AC = CN * CN / 64;           /* results a lane */
+    static constexpr int WQ = COLS / CN;
     static constexpr int WK = 4 / WQ;                 /* waves that take the same columns */
     static constexpr int TK = SOLO ? 128 : 64;        /* positions of a tile */
     static constexpr int KW = TK / WK;                /* of it, those of one wave */
     static constexpr int SUBS = KW / 32;
-    static constexpr int COLS = 32 * WQ;              /* queries of a block */
     /* rows in LDS: 16 bytes more than a multiple of 128 spread the reads of K over the banks, 64 bytes more the
      * transposed reads of 16-bit V */
     static constexpr int ES = RAW ? 1 : 2;            /* bytes of a value in LDS */
@@ -136,6 +159,8 @@ struct TreeShape {
     static constexpr int KBYTES = TK * KS * ES, VBYTES = TK * VS * ES;
     static constexpr int OS = DP + 4;                 /* floats of a row of the waves' results when they are joined */
     static constexpr int JOIN = (WK - 1) * COLS * OS * 4;
+    /* blocks that a CU holds: by LDS, or by registers */
+    static constexpr int BLOCKS = DP > 128 ? (COLS == 16 && RAW ? 2 : 1) : COLS > 16 ? 2 : RAW ? (DP <= 64 ? 4 : 3) : DP <= 64 ? 3 : 2;
     static constexpr int TILE = KBYTES + VBYTES > JOIN ? KBYTES + VBYTES : JOIN;
 };
 
@@ -168,10 +193,12 @@ __device__ __forceinline__ int32_t parts_of(const TreeArgs &a, int32_t end)
     return n < 1 ? 1 : n < a.parts ? n : a.parts;
 }
 
-template <int DP, int WQ, bool F16, int KIND>
-__global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention(TreeArgs a)
+template <int DP, int COLS, bool F16, int KIND>
+__global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOCKS)) tree_attention(TreeArgs a)
 {
-    typedef TreeShape<DP, WQ, KIND> Sh;
+    typedef TreeShape<DP, COLS, KIND> Sh;
+    constexpr int CN = Sh::CN, G = Sh::G, NV = Sh::NV, KSTEP = Sh::KSTEP, AC = Sh::AC, WQ = Sh::WQ;
+    typedef typename Acc<CN>::type acc;
     constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
     constexpr bool CODES = Sh::CODES, RAW = Sh::RAW;
     constexpr bool PF16 = KIND == KV_F16;   /* type of the weights and of V: bfloat16 for codes, whose scales are in the weights */
@@ -186,7 +213,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     constexpr int LOADERS = Sh::SOLO ? 64 : TREE_THREADS, ROWS = Sh::SOLO ? Sh::KW : TK;
     constexpr int VPR = DP / VE, RPP = LOADERS / VPR, NP = ROWS / RPP;
     constexpr int ES = CODES ? 1 : 2;
-    constexpr int NK = DP / 16, ND = DP / 32;
+    constexpr int KD = 8 * G, NK = DP / KD, ND = DP / CN;
     static_assert(NP >= 1 && NP * RPP == ROWS, "the loads cover a tile");
 
     __shared__ __attribute__((aligned(16))) char tile[Sh::TILE];
@@ -195,12 +222,12 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     __shared__ int32_t v_stamp[TK];
     __shared__ uint32_t skip[TREE_SKIP_WORDS];
     __shared__ int32_t flags[2];            /* a bad page; the last tile with a value of V that is not finite (of the block) */
-    __shared__ float join_ml[2][Sh::WK][Sh::COLS];
+    __shared__ float join_ml[2][Sh::WK][COLS];
     char *const Ks = tile, *const Vs = tile + Sh::KBYTES;
     constexpr int LS = Sh::ES;              /* bytes of a value there */
 
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n = lane & 31, h = lane >> 5;
+    const int n = lane % CN, h = lane / CN;
     const int wq = wave % WQ, wk = wave / WQ, k0 = wk * Sh::KW;
 
     /* ---- which row, cache head, part and columns */
@@ -221,7 +248,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     const int32_t head = (int32_t)(unit / a.parts % a.c.n_heads);
     const int64_t row = unit / a.parts / a.c.n_heads;
     const KvRow w = load_row(a.r, a.c, row, false);
-    const TreeSpan sp = tree_span(a, w, row, q_block, Sh::COLS);
+    const TreeSpan sp = tree_span(a, w, row, q_block, COLS);
     if (!sp.ok && part == 0 && head == 0 && q_block == 0 && tid == 0) report(a.r, row, PARASON_KV_BAD_ROW);
     if (!w.out_ok || sp.tok0 >= w.length) return;
     const int32_t my_parts = parts_of(a, sp.end);
@@ -230,7 +257,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     const int32_t k_end = part == my_parts - 1 ? sp.end : k_begin + a.part_len;
 
     /* ---- this lane's query */
-    const int32_t col = q_block * Sh::COLS + wq * 32 + n;
+    const int32_t col = q_block * COLS + wq * CN + n;
     const int32_t tok = (int32_t)div_by((uint32_t)col, a.group_div);
     const bool live = tok < w.length;
     const int32_t q_head = head * a.group + (col - tok * a.group);
@@ -240,7 +267,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
         const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + t * a.q_stride_token + (live ? q_head : 0) * a.q_stride_head;
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-            const int d = k * 16 + h * 8;
+            const int d = k * KD + h * 8;
             uint4 x = make_uint4(0u, 0u, 0u, 0u);
             if (live && d < a.c.head_dim) {
                 if (a.q_wide) {
@@ -365,7 +392,7 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
         }
     };
 
-    acc16 o[ND] = {};
+    acc o[ND] = {};
     float at = -INFINITY, l = 0.0f;          /* the exponent that o and l are relative to; this lane's share of the sum */
 
     /* tiles in turn: the one in work, and the one behind it */
@@ -424,21 +451,26 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
         load_mask(x1);
         load_tile();
         /* ---- S^T */
-        acc16 s[SUBS];
+        float s[SUBS][NV];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
-            s[u] = acc16{};
-            const char *ka = Ks + ((k0 + u * 32 + n) * KS + h * 8) * LS;
 #pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                const frag8 kf = RAW ? widen8<F16, KIND>(*reinterpret_cast<const uint2 *>(ka + k * 16))
-                                     : *reinterpret_cast<const frag8 *>(ka + k * 32);
-                s[u] = mma<F16>(kf, qf[k], s[u]);
+            for (int i = 0; i < 32 / CN; ++i) {
+                acc c = {};
+                const char *ka = Ks + ((k0 + u * 32 + i * CN + n) * KS + h * 8) * LS;
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    const frag8 kf = RAW ? widen8<F16, KIND>(*reinterpret_cast<const uint2 *>(ka + k * KD))
+                                         : *reinterpret_cast<const frag8 *>(ka + k * KD * 2);
+                    c = mma<F16>(kf, qf[k], c);
+                }
+#pragma unroll
+                for (int r = 0; r < AC; ++r) s[u][i * AC + r] = c[r];
             }
             if (CODES) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 f = *reinterpret_cast<const float4 *>(&k_sc[k0 + u * 32 + 8 * i + 4 * h]);
+                for (int i = 0; i < NV / 4; ++i) {
+                    const float4 f = *reinterpret_cast<const float4 *>(&k_sc[k0 + u * 32 + KSTEP * i + 4 * h]);
                     s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
                 }
             }
@@ -472,8 +504,8 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                 see[u] = m;
                 const uint32_t mine = m >> (4 * h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!((mine >> (8 * (r / 4) + (r & 3))) & 1u)) s[u][r] = -INFINITY;
+                for (int r = 0; r < NV; ++r)
+                    if (!((mine >> (KSTEP * (r / 4) + (r & 3))) & 1u)) s[u][r] = -INFINITY;
             }
         }
         /* ---- maximum, weights, sum */
@@ -481,8 +513,9 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-        top = fmaxf(top, __shfl_xor(top, 32));
+            for (int r = 0; r < NV; ++r) top = fmaxf(top, s[u][r]);
+#pragma unroll
+        for (int k = CN; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
         const float at_new = fmaxf(at, top * a.c2 - LIFT);
         const float ref = at_new == -INFINITY ? 0.0f : at_new;
         if (__ballot(at_new > at)) {
@@ -491,13 +524,13 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[d][r] *= corr;
+                for (int r = 0; r < AC; ++r) o[d][r] *= corr;
             at = at_new;
         }
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
+            for (int r = 0; r < NV; ++r) {
                 s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c2, -ref));
                 l += s[u][r];
             }
@@ -506,26 +539,26 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
             for (int u = 0; u < SUBS; ++u) {
                 const uint32_t mine = see[u] >> (4 * h);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 f = *reinterpret_cast<const float4 *>(&v_sc[k0 + u * 32 + 8 * i + 4 * h]);
+                for (int i = 0; i < NV / 4; ++i) {
+                    const float4 f = *reinterpret_cast<const float4 *>(&v_sc[k0 + u * 32 + KSTEP * i + 4 * h]);
                     s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
                 }
                 if (masked) {                /* no scale, whatever it is, makes a weight where nothing is seen */
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!((mine >> (8 * (r / 4) + (r & 3))) & 1u)) s[u][r] = 0.0f;
+                    for (int r = 0; r < NV; ++r)
+                        if (!((mine >> (KSTEP * (r / 4) + (r & 3))) & 1u)) s[u][r] = 0.0f;
                 }
             }
         }
         /* ---- O^T */
         /* transposed reads: each 16 lanes name four (codes: eight) rows of 16 values and get a column each */
-        const int g16 = ((lane >> 4) & 1) * 16, i16 = lane & 15;
-        const char *va = RAW ? Vs + (k0 + 4 * h + ((i16 >> 1) & 3) + 8 * (i16 >> 3)) * VS + g16 + (i16 & 1) * 8
+        const int g16 = CN == 32 ? ((lane >> 4) & 1) * 16 : 0, i16 = lane & 15;
+        const char *va = RAW ? Vs + (k0 + 4 * h + ((i16 >> 1) & 3) + KSTEP * (i16 >> 3)) * VS + g16 + (i16 & 1) * 8
                              : Vs + ((k0 + 4 * h + (i16 >> 2)) * VS + g16 + (i16 & 3) * 4) * 2;
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < NV / 8; ++k) {
                 uint32_t pw[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pw[i] = pack2<PF16>(s[u][8 * k + 2 * i], s[u][8 * k + 2 * i + 1]);
@@ -543,14 +576,14 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                     typedef int int2v __attribute__((ext_vector_type(2)));
                     typedef __attribute__((address_space(3))) frag4 lds4;
                     typedef __attribute__((address_space(3))) int2v lds8;
-                    const char *v0 = va + ((u * 32 + k * 16) * VS + d * 32) * LS;
+                    const char *v0 = va + ((u * 32 + k * 16) * VS + d * CN) * LS;
                     frag8 vf;
                     if (RAW) {
                         const int2v f = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8 *)v0);
                         vf = widen8<PF16, KIND>(make_uint2((uint32_t)f.x, (uint32_t)f.y));
                     } else {
                         const frag4 f0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)v0);
-                        const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + 8 * VS * LS));
+                        const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + KSTEP * VS * LS));
                         vf = __builtin_shufflevector(f0, f1, 0, 1, 2, 3, 4, 5, 6, 7);
                     }
                     if (odd_values) {
@@ -573,14 +606,14 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
                     if (v_stamp[r] != x) continue;
                     float p = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) p = ((kk >> 3) * 4 + (kk & 3)) == i ? s[u][i] : p;
-                    p = __shfl(p, n + 32 * ((kk >> 2) & 1));
+                    for (int i = 0; i < NV; ++i) p = (kk / KSTEP * 4 + (kk & 3)) == i ? s[u][i] : p;
+                    p = __shfl(p, n + CN * (kk % KSTEP / 4));
                     if (!((see[u] >> kk) & 1u)) continue;
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const char *e = Vs + (r * VS + d * 32 + 8 * (i / 4) + 4 * h + (i & 3)) * LS;
+                        for (int i = 0; i < AC; ++i) {
+                            const char *e = Vs + (r * VS + d * CN + 8 * (i / 4) + 4 * h + (i & 3)) * LS;
                             const uint16_t v = RAW ? (uint16_t)widen4<PF16, KIND>((uint8_t)*e).x : *reinterpret_cast<const uint16_t *>(e);
                             if (not_finite2<PF16>(v)) o[d][i] += p * widen1<PF16>(v);
                         }
@@ -595,13 +628,14 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
     if (flags[0] == 0 && tid == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
 
     /* ---- results */
-    l += __shfl_xor(l, 32);
+#pragma unroll
+    for (int k = CN; k < 64; k <<= 1) l += __shfl_xor(l, k);
     const float nan = __uint_as_float(0x7FC00000u);
     if (Sh::WK > 1) {
         /* the waves of the same columns: the maximum and the sum over them, then their shares of O, which the first
          * adds to its own */
         float *const Os = reinterpret_cast<float *>(tile);
-        const int c = wq * 32 + n;
+        const int c = wq * CN + n;
         if (h == 0) join_ml[0][wk][c] = at, join_ml[1][wk][c] = l;
         __syncthreads();
         float top = -INFINITY, sum = 0.0f;
@@ -614,10 +648,10 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < AC / 4; ++i) {
                 o[d][4 * i] *= f, o[d][4 * i + 1] *= f, o[d][4 * i + 2] *= f, o[d][4 * i + 3] *= f;
                 if (wk > 0)
-                    *reinterpret_cast<float4 *>(&Os[((wk - 1) * Sh::COLS + c) * Sh::OS + d * 32 + 8 * i + 4 * h]) =
+                    *reinterpret_cast<float4 *>(&Os[((wk - 1) * COLS + c) * Sh::OS + d * CN + 8 * i + 4 * h]) =
                         make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
             }
         at = top, l = sum;
@@ -628,8 +662,8 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 z = *reinterpret_cast<const float4 *>(&Os[(k * Sh::COLS + c) * Sh::OS + d * 32 + 8 * i + 4 * h]);
+                for (int i = 0; i < AC / 4; ++i) {
+                    const float4 z = *reinterpret_cast<const float4 *>(&Os[(k * COLS + c) * Sh::OS + d * CN + 8 * i + 4 * h]);
                     o[d][4 * i] += z.x, o[d][4 * i + 1] += z.y, o[d][4 * i + 2] += z.z, o[d][4 * i + 3] += z.w;
                 }
     }
@@ -641,8 +675,8 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = d * 32 + 8 * i + 4 * h;
+            for (int i = 0; i < AC / 4; ++i) {
+                const int at = d * CN + 8 * i + 4 * h;
                 if (at < a.c.head_dim)
                     *reinterpret_cast<float4 *>(dst + at) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
             }
@@ -654,8 +688,8 @@ __global__ void __launch_bounds__(TREE_THREADS, DP > 128 ? 1 : 2) tree_attention
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = d * 32 + 8 * i + 4 * h;
+        for (int i = 0; i < AC / 4; ++i) {
+            const int at = d * CN + 8 * i + 4 * h;
             if (at >= a.c.head_dim) continue;
             const uint2 p = make_uint2(pack2<F16>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
                                        pack2<F16>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
