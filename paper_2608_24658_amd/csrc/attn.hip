@@ -54,11 +54,15 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
     p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
     const int64_t base = r->n_rows * c->n_heads * p->q_blocks;
     const int64_t tile = p->cols < 128 ? 128 : 64;
-    int64_t len = 1024;
-    while (len > 512 && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
+    /* Enough blocks to fill the device, and for few columns, whose partial results are small, parts short enough that
+     * long rows among short ones do not finish last.  A part is worth its results: 8 bytes a column and value, written
+     * and read, against 2 to 4 bytes a position and value. */
+    const int64_t shortest = p->cols < 128 ? 512 : 1024;
+    int64_t len = p->cols < 128 ? 1024 : 4096;
+    while (len > shortest && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
     const size_t per_part = (size_t)r->n_tokens * n_q_heads * c->head_dim * 4;
     int64_t parts = (r->max_kv_len + len - 1) / len;
-    if (parts < 1 || base >= 16 * PART_BLOCKS) parts = 1;
+    if (parts < 1 || base >= (p->cols < 128 ? 16 : 1) * PART_BLOCKS) parts = 1;
     if (per_part > 0 && (size_t)parts > PART_BYTES / per_part) parts = PART_BYTES / per_part > 1 ? (int64_t)(PART_BYTES / per_part) : 1;
     len = (r->max_kv_len + parts - 1) / parts;
     p->part_len = (int32_t)((len + tile - 1) / tile * tile < INT32_MAX ? (len + tile - 1) / tile * tile : len);

@@ -452,6 +452,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         load_tile();
         /* ---- S^T */
         float s[SUBS][NV];
+        __builtin_amdgcn_s_setprio(1);       /* a wave in its products goes before one in its exponentials */
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
 #pragma unroll
@@ -475,6 +476,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         /* ---- what this lane's query sees of the wave's positions, from bit 0 on */
         uint32_t see[SUBS];
 #pragma unroll
@@ -551,6 +553,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             }
         }
         /* ---- O^T */
+        __builtin_amdgcn_s_setprio(1);
         /* transposed reads: each 16 lanes name four (codes: eight) rows of 16 values and get a column each */
         const int g16 = CN == 32 ? ((lane >> 4) & 1) * 16 : 0, i16 = lane & 15;
         const char *va = RAW ? Vs + (k0 + 4 * h + ((i16 >> 1) & 3) + KSTEP * (i16 >> 3)) * VS + g16 + (i16 & 1) * 8
@@ -596,6 +599,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         if (odd_values) {
             /* infinities and NaN of V reach only the queries that see them: a product by zero would not do.  They
              * were left out above and are added one position at a time. */

@@ -32,9 +32,13 @@ struct Read {
     static constexpr MoveKernel f = pk::kv_read<T, KIND>;
 };
 
-/* Blocks that a launch of large rows keeps on the device: eight per CU of 256
- * fill it, and a few rounds of them even out ragged rows. */
-constexpr int64_t MOVE_BLOCKS = 256 * 8 * 4;
+/* Most blocks of a launch.  Rows are cut for the longest one, so many blocks of a ragged call find nothing to do, and
+ * the few long rows need enough of theirs to fill the device: 48 rows of 1 to 36,000 positions, FP8 read as bfloat16,
+ * 406 us at 8,192 blocks, 260 at 32,768, 267 at 131,072. */
+#ifndef PARASON_KV_BLOCKS
+#define PARASON_KV_BLOCKS 32768
+#endif
+constexpr int64_t MOVE_BLOCKS = PARASON_KV_BLOCKS;
 
 int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void *k, const void *v, int32_t dtype,
          int64_t stride_token, int64_t stride_head, uint32_t *row_status, void *stream_ptr, bool write)
@@ -65,7 +69,7 @@ int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void 
     a.group = 1, a.group_log = 0;
     while (a.group * pk::KV_PER_LANE < cache->head_dim) a.group <<= 1, ++a.group_log;
     a.heads_div = pk::fast_div((uint32_t)cache->n_heads);
-    const int64_t per_block = pk::KV_THREADS / a.group;
+    const int64_t per_block = pk::KV_THREADS / a.group * (write ? pk::KV_WRITES : pk::KV_READS);
     int64_t blocks = (units + per_block - 1) / per_block, most = MOVE_BLOCKS / rows->n_rows;
     if (most < 1) most = 1;
     if (blocks > most) blocks = most;

@@ -671,7 +671,7 @@ def kv_alloc(n_pages: int, page_size: int, heads: int, head_dim: int, dtype, dev
     """A cache of zeros, each head's slots of a page next to each other."""
     import torch
 
-    code = _kv_types().get(dtype)
+    code = _types().kv.get(dtype)
     if code is None:
         raise TypeError("a cache holds bfloat16, float16, float8_e4m3fn or int8 values")
     shape = (int(n_pages), int(heads), int(page_size), int(head_dim))
@@ -682,82 +682,86 @@ def kv_alloc(n_pages: int, page_size: int, heads: int, head_dim: int, dtype, dev
     return KVCache(*kv)
 
 
-@functools.lru_cache(maxsize=None)
-def _kv_types():
-    import torch
+class _Types:
+    """torch and its types, looked up once (an import statement in every call costs more than its checks)."""
 
-    return {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_FP8, torch.int8: DTYPE_INT8}
+    torch = None
+
+    @classmethod
+    def load(cls):
+        import torch
+
+        cls.i32, cls.i64, cls.f32, cls.u8 = torch.int32, torch.int64, torch.float32, torch.uint8
+        cls.floats = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+        cls.kv = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_FP8, torch.int8: DTYPE_INT8}
+        cls.empty, cls.torch = torch.empty, torch
+        return cls
 
 
-@functools.lru_cache(maxsize=None)
-def _float_types():
-    import torch
-
-    return {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+def _types():
+    return _Types if _Types.torch is not None else _Types.load()
 
 
-def _cache_args(cache: KVCache) -> KvCacheArgs:
-    import torch
-
+def _cache_args(T, cache: KVCache) -> KvCacheArgs:
     k, v, ks, vs = cache
-    code = _kv_types().get(k.dtype)
-    if code is None or v.dtype is not k.dtype or k.dim() != 4 or not k.is_cuda or not v.is_cuda:
+    code = T.kv.get(k.dtype)
+    if code is None or v.dtype is not k.dtype or k.dim() != 4 or not (k.is_cuda and v.is_cuda):
         raise TypeError("k and v must be [pages, page_size, heads, head_dim] bfloat16/float16/float8_e4m3fn/int8 "
                         "device tensors of one type")
     shape, st = k.shape, k.stride()
-    if v.shape != shape or v.stride() != st or (st[3] != 1 and shape[3] > 1):
+    pages, size, heads, dim = shape
+    if v.shape != shape or v.stride() != st or (st[3] != 1 and dim > 1):
         raise ValueError("k and v must have the same shape and strides, and unit stride along a head")
     if code < DTYPE_FP8:
         if ks is not None or vs is not None:
             raise TypeError("a 16-bit cache has no scales")
-        return KvCacheArgs(k.data_ptr(), v.data_ptr(), None, None, shape[0], st[0], st[1], st[2], 0, 0, 0, shape[1],
-                           shape[2], shape[3], code)
-    if ks is None or vs is None or ks.dtype is not torch.float32 or vs.dtype is not torch.float32 \
-            or not ks.is_cuda or not vs.is_cuda:
+        return KvCacheArgs(k.data_ptr(), v.data_ptr(), None, None, pages, st[0], st[1], st[2], 0, 0, 0, size, heads, dim,
+                           code)
+    if ks is None or vs is None or ks.dtype is not T.f32 or vs.dtype is not T.f32 or not (ks.is_cuda and vs.is_cuda):
         raise TypeError("an 8-bit cache needs float32 device tensors k_scale and v_scale")
     sst = ks.stride()
-    if ks.shape != shape[:3] or vs.shape != shape[:3] or vs.stride() != sst:
+    if ks.shape != shape[:3] or vs.shape != ks.shape or vs.stride() != sst:
         raise ValueError("k_scale and v_scale must be [pages, page_size, heads], with the same strides")
-    return KvCacheArgs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), shape[0], st[0], st[1], st[2], sst[0],
-                       sst[1], sst[2], shape[1], shape[2], shape[3], code)
+    return KvCacheArgs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, st[0], st[1], st[2], *sst, size,
+                       heads, dim, code)
 
 
-def _rows_args(rows: KVRows, n_tokens: int) -> KvRowsArgs:
-    import torch
-
+def _rows_args(T, rows: KVRows, n_tokens: int) -> KvRowsArgs:
     starts, lengths, kv_lens, pages, max_length, max_kv_len = rows
-    n = starts.numel()
-    for t, dt in ((starts, torch.int64), (lengths, torch.int32), (kv_lens, torch.int32)):
-        if t.dtype is not dt or not t.is_cuda or not t.is_contiguous():
-            raise TypeError("expected contiguous %s device tensors" % dt)
-    if pages.dtype is not torch.int32 or not pages.is_cuda or pages.dim() != 2 \
-            or (pages.stride(1) != 1 and pages.shape[1] > 1):
+    if starts.dtype is not T.i64 or lengths.dtype is not T.i32 or kv_lens.dtype is not T.i32 \
+            or not (starts.is_cuda and lengths.is_cuda and kv_lens.is_cuda) \
+            or not (starts.is_contiguous() and lengths.is_contiguous() and kv_lens.is_contiguous()):
+        raise TypeError("starts (int64), lengths and kv_lens (int32) must be contiguous device tensors")
+    if pages.dtype is not T.i32 or not pages.is_cuda or pages.dim() != 2:
         raise TypeError("pages must be an int32 [rows, max_pages] device tensor, unit stride along a row")
-    if lengths.numel() != n or kv_lens.numel() != n or pages.shape[0] != n:
+    n, max_pages = pages.shape
+    st = pages.stride()
+    if st[1] != 1 and max_pages > 1:
+        raise TypeError("pages must be an int32 [rows, max_pages] device tensor, unit stride along a row")
+    if starts.numel() != n or lengths.numel() != n or kv_lens.numel() != n:
         raise ValueError("starts, lengths, kv_lens and pages must have the same number of rows")
-    return KvRowsArgs(n, n_tokens, starts.data_ptr(), lengths.data_ptr(), kv_lens.data_ptr(), pages.data_ptr(),
-                      pages.stride(0), pages.shape[1], int(max_length), int(max_kv_len))
+    return KvRowsArgs(n, n_tokens, starts.data_ptr(), lengths.data_ptr(), kv_lens.data_ptr(), pages.data_ptr(), st[0],
+                      max_pages, int(max_length), int(max_kv_len))
 
 
-def _status_ptr(status, n):
-    import torch
-
+def _status_ptr(T, status, n):
     if status is None:
         return None
-    if status.dtype is not torch.int32 or status.numel() != n or not status.is_contiguous() or not status.is_cuda:
+    if status.dtype is not T.i32 or status.numel() != n or not status.is_contiguous() or not status.is_cuda:
         raise TypeError("status must be a contiguous int32 device tensor of one entry per row")
     return status.data_ptr()
 
 
-def _token_arrays(k, v, cache: KVCache):
+def _token_arrays(T, k, v, ca: KvCacheArgs):
     """Type, token stride and head stride of two [tokens, heads, head_dim] tensors."""
-    code = _float_types().get(k.dtype)
-    if code is None or v.dtype is not k.dtype or k.dim() != 3 or not k.is_cuda or not v.is_cuda:
+    code = T.floats.get(k.dtype)
+    if code is None or v.dtype is not k.dtype or k.dim() != 3 or not (k.is_cuda and v.is_cuda):
         raise TypeError("k and v must be [tokens, heads, head_dim] float32/bfloat16/float16 device tensors of one type")
-    if k.shape != v.shape or k.stride() != v.stride() or k.shape[1:] != cache.k.shape[2:] \
-            or (k.stride(2) != 1 and k.shape[2] > 1):
+    shape, st = k.shape, k.stride()
+    if v.shape != shape or v.stride() != st or shape[1] != ca.n_heads or shape[2] != ca.head_dim \
+            or (st[2] != 1 and shape[2] > 1):
         raise ValueError("k and v must have the cache's heads, the same shape and strides, and unit stride along a head")
-    return code, k.stride(0), k.stride(1)
+    return code, st[0], st[1]
 
 
 def kv_write(k, v, cache: KVCache, rows: KVRows, status=None) -> None:
@@ -765,10 +769,11 @@ def kv_write(k, v, cache: KVCache, rows: KVRows, status=None) -> None:
     tensors) into the cache, at the last lengths[i] of row i's kv_lens[i]
     positions (asynchronous on the current stream).  8-bit caches are quantised
     per slot and head.  status: int32[rows] that KV_BAD_* bits are added to."""
-    ca, ra = _cache_args(cache), _rows_args(rows, k.shape[0])
-    code, st, sh = _token_arrays(k, v, cache)
+    T = _types()
+    ca, ra = _cache_args(T, cache), _rows_args(T, rows, k.shape[0])
+    code, st, sh = _token_arrays(T, k, v, ca)
     rc = (_lib or lib()).parason_kv_write(ca, ra, k.data_ptr(), v.data_ptr(), code, st, sh,
-                                          _status_ptr(status, ra.n_rows), _stream(k.device))
+                                          _status_ptr(T, status, ra.n_rows), _stream(k.device))
     if rc != OK:
         raise ParasonError(rc, "parason_kv_write")
 
@@ -777,25 +782,25 @@ def kv_read(cache: KVCache, rows: KVRows, n_tokens: int, dtype, out=None, status
     """(k, v): the last lengths[i] of row i's kv_lens[i] positions as
     [n_tokens, heads, head_dim] tensors of `dtype` (asynchronous on the current
     stream; `out`: a pair of tensors to write into)."""
-    import torch
-
+    T = _types()
+    ca, ra = _cache_args(T, cache), _rows_args(T, rows, int(n_tokens))
     if out is None:
-        shape = (int(n_tokens),) + tuple(cache.k.shape[2:])
-        out = tuple(torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in "kv")
-    k, v = out
+        k, v = out = T.empty((2, int(n_tokens), ca.n_heads, ca.head_dim), dtype=dtype, device=cache.k.device).unbind()
+    else:
+        k, v = out
+    code, st, sh = _token_arrays(T, k, v, ca)
     if k.shape[0] != n_tokens or k.dtype is not dtype:
         raise ValueError("out must hold n_tokens tokens of dtype")
-    ca, ra = _cache_args(cache), _rows_args(rows, int(n_tokens))
-    code, st, sh = _token_arrays(k, v, cache)
     rc = (_lib or lib()).parason_kv_read(ca, ra, k.data_ptr(), v.data_ptr(), code, st, sh,
-                                         _status_ptr(status, ra.n_rows), _stream(k.device))
+                                         _status_ptr(T, status, ra.n_rows), _stream(k.device))
     if rc != OK:
         raise ParasonError(rc, "parason_kv_read")
-    return out
+    return k, v
 
 
 def tree_attention_workspace_size(cache: KVCache, rows: KVRows, n_tokens: int, q_heads: int) -> int:
-    return _tree_workspace(_cache_args(cache), _rows_args(rows, int(n_tokens)), int(q_heads))
+    T = _types()
+    return _tree_workspace(_cache_args(T, cache), _rows_args(T, rows, int(n_tokens)), int(q_heads))
 
 
 def _tree_workspace(ca, ra, q_heads: int) -> int:
@@ -822,41 +827,44 @@ def tree_attention(q, cache: KVCache, rows: KVRows, mask=None, tree_lens=None, s
     lse     True (or a float32 [tokens, q_heads] tensor): also the logarithm of
             each token's and head's sum of exponentials
     """
-    import torch
-
-    code = _float_types().get(q.dtype)
-    if code is None or code == DTYPE_F32 or q.dim() != 3 or not q.is_cuda or (q.stride(2) != 1 and q.shape[2] > 1):
+    T = _types()
+    code = T.floats.get(q.dtype)
+    if code is None or code == DTYPE_F32 or q.dim() != 3 or not q.is_cuda:
         raise TypeError("q must be a [tokens, q_heads, head_dim] bfloat16/float16 device tensor, unit stride along a head")
-    n_tokens, q_heads, dim = q.shape
-    if dim != cache.k.shape[3]:
+    n_tokens, q_heads, dim = shape = q.shape
+    q_st = q.stride()
+    if q_st[2] != 1 and dim > 1:
+        raise TypeError("q must be a [tokens, q_heads, head_dim] bfloat16/float16 device tensor, unit stride along a head")
+    ca, ra = _cache_args(T, cache), _rows_args(T, rows, n_tokens)
+    if dim != ca.head_dim:
         raise ValueError("q must have the cache's head_dim")
-    ca, ra = _cache_args(cache), _rows_args(rows, n_tokens)
     if out is None:
-        out = torch.empty((n_tokens, q_heads, dim), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_cuda or (out.stride(2) != 1 and dim > 1):
+        out = T.empty(shape, dtype=q.dtype, device=q.device)
+    out_st = out.stride()
+    if out.shape != shape or out.dtype is not q.dtype or not out.is_cuda or (out_st[2] != 1 and dim > 1):
         raise TypeError("out must be a device tensor of q's shape and type, unit stride along a head")
     if lse is True:
-        lse = torch.empty((n_tokens, q_heads), dtype=torch.float32, device=q.device)
+        lse = T.empty((n_tokens, q_heads), dtype=T.f32, device=q.device)
     elif lse is False:
         lse = None
-    elif lse.dtype is not torch.float32 or lse.shape != (n_tokens, q_heads) or not lse.is_contiguous() or not lse.is_cuda:
+    elif lse.dtype is not T.f32 or lse.shape != (n_tokens, q_heads) or not lse.is_contiguous() or not lse.is_cuda:
         raise TypeError("lse must be a contiguous float32 [tokens, q_heads] device tensor")
     words = stride = 0
     if mask is not None:
-        if mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != n_tokens or not mask.is_cuda \
+        if mask.dtype is not T.i64 or mask.dim() != 2 or mask.shape[0] != n_tokens or not mask.is_cuda \
                 or (mask.stride(1) != 1 and mask.shape[1] > 1):
             raise TypeError("mask must be an int64 [tokens, words] device tensor, unit stride along a token")
         words, stride = mask.shape[1], mask.stride(0)
-    if tree_lens is not None and (tree_lens.dtype is not torch.int32 or tree_lens.numel() != ra.n_rows
+    if tree_lens is not None and (tree_lens.dtype is not T.i32 or tree_lens.numel() != ra.n_rows
                                   or not tree_lens.is_contiguous() or not tree_lens.is_cuda):
         raise TypeError("tree_lens must be a contiguous int32 device tensor of one entry per row")
     if workspace is None:
-        workspace = torch.empty(_tree_workspace(ca, ra, q_heads), dtype=torch.uint8, device=q.device)
-    ta = TreeArgs(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q.stride(0), q.stride(1),
-                  out.stride(0), out.stride(1), mask.data_ptr() if mask is not None else None, stride,
+        workspace = T.empty(_tree_workspace(ca, ra, q_heads), dtype=T.u8, device=q.device)
+    ta = TreeArgs(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q_st[0], q_st[1],
+                  out_st[0], out_st[1], mask.data_ptr() if mask is not None else None, stride,
                   tree_lens.data_ptr() if tree_lens is not None else None, words, q_heads, code,
                   dim ** -0.5 if scale is None else float(scale))
-    rc = (_lib or lib()).parason_tree_attention(ca, ra, ta, _status_ptr(status, ra.n_rows), workspace.data_ptr(),
+    rc = (_lib or lib()).parason_tree_attention(ca, ra, ta, _status_ptr(T, status, ra.n_rows), workspace.data_ptr(),
                                                 workspace.numel(), _stream(q.device))
     if rc != OK:
         raise ParasonError(rc, "parason_tree_attention")
@@ -882,28 +890,31 @@ def beam_select(logits, scores, beams: int, states=None, workspace=None) -> dict
     scores  float32 [rows]; -inf: an empty beam
     states  decode states (uint8[rows * 16]) or None: finished rows stay as they
             are, rows with an error are dropped"""
-    import torch
-
-    code = _float_types().get(logits.dtype)
-    if code is None or logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
+    T = _types()
+    code = T.floats.get(logits.dtype)
+    if code is None or logits.dim() != 2 or not logits.is_cuda:
         raise TypeError("logits must be a [rows, vocab] float32/bfloat16/float16 device tensor, unit stride")
     rows, vocab = logits.shape
+    stride = logits.stride()
+    if stride[1] != 1 and vocab > 1:
+        raise TypeError("logits must be a [rows, vocab] float32/bfloat16/float16 device tensor, unit stride")
     beams = int(beams)
     if beams < 1 or rows % beams:
         raise ValueError("the rows must be whole groups of beams")
-    if scores.dtype is not torch.float32 or scores.numel() != rows or not scores.is_contiguous() or not scores.is_cuda:
+    if scores.dtype is not T.f32 or scores.numel() != rows or not scores.is_contiguous() or not scores.is_cuda:
         raise TypeError("scores must be a contiguous float32 device tensor of one entry per row")
-    if states is not None and (states.dtype is not torch.uint8 or states.numel() != rows * DECODE_STATE_BYTES
+    if states is not None and (states.dtype is not T.u8 or states.numel() != rows * DECODE_STATE_BYTES
                                or not states.is_contiguous() or not states.is_cuda):
         raise TypeError("states must be a contiguous uint8 device tensor of rows * 16 bytes")
+    dev = logits.device
     if workspace is None:
-        workspace = torch.empty(beam_workspace_size(rows // beams, beams, vocab), dtype=torch.uint8, device=logits.device)
-    score = torch.empty_like(scores)
-    parent, token = torch.empty((2, rows), dtype=torch.int32, device=logits.device)
+        workspace = T.empty(beam_workspace_size(rows // beams, beams, vocab), dtype=T.u8, device=dev)
+    score = T.empty(rows, dtype=T.f32, device=dev)
+    parent, token = T.empty((2, rows), dtype=T.i32, device=dev).unbind()
     rc = (_lib or lib()).parason_beam_select(
-        logits.data_ptr(), vocab, logits.stride(0) if rows > 1 else vocab, code, scores.data_ptr(),
+        logits.data_ptr(), vocab, stride[0] if rows > 1 else vocab, code, scores.data_ptr(),
         states.data_ptr() if states is not None else None, rows // beams, beams, score.data_ptr(), parent.data_ptr(),
-        token.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(logits.device))
+        token.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(dev))
     if rc != OK:
         raise ParasonError(rc, "parason_beam_select")
     return dict(score=score, parent=parent, token=token)
@@ -914,40 +925,44 @@ def beam_reorder(parent, arrays, out=None) -> list:
     row parent[i] of the array (asynchronous on the current stream).  arrays: up
     to BEAM_ARRAYS device tensors, each [rows, ...] with contiguous rows, or a
     flat one of rows equal parts; out: tensors to write into, other than these."""
-    import torch
-
-    rows = parent.numel()
-    if parent.dtype is not torch.int32 or not parent.is_contiguous() or not parent.is_cuda:
+    T = _types()
+    rows, n = parent.numel(), len(arrays)
+    if parent.dtype is not T.i32 or not parent.is_contiguous() or not parent.is_cuda:
         raise TypeError("parent must be a contiguous int32 device tensor")
-    if len(arrays) > BEAM_ARRAYS:
+    if n > BEAM_ARRAYS:
         raise ValueError("at most %d arrays in one call" % BEAM_ARRAYS)
-    if out is None:
-        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in arrays]
-    if len(out) != len(arrays):
+    if out is not None and len(out) != n:
         raise ValueError("as many results as arrays")
-    args = (BeamArray * max(1, len(arrays)))()
-    for a, x, y in zip(args, arrays, out):
-        if x.dtype is not y.dtype or x.shape != y.shape or not x.is_cuda or not y.is_cuda:
-            raise TypeError("a result must be a device tensor of its array's shape and type")
-        a.src, a.dst = x.data_ptr(), y.data_ptr()
-        a.row_bytes, a.src_stride = _row_bytes(x, rows)
-        a.dst_stride = _row_bytes(y, rows)[1]
-    rc = (_lib or lib()).parason_beam_reorder(parent.data_ptr(), rows, args, len(arrays), _stream(parent.device))
+    args, res = (BeamArray * n)(), []
+    for i, x in enumerate(arrays):
+        if not x.is_cuda:
+            raise TypeError("an array must be a device tensor")
+        size, stride = _row_bytes(x, rows)
+        if out is None:
+            y, to = T.empty(x.shape, dtype=x.dtype, device=x.device), size
+        else:
+            y = out[i]
+            if x.dtype is not y.dtype or x.shape != y.shape or not y.is_cuda:
+                raise TypeError("a result must be a device tensor of its array's shape and type")
+            to = _row_bytes(y, rows)[1]
+        args[i] = (x.data_ptr(), y.data_ptr(), size, stride, to)
+        res.append(y)
+    rc = (_lib or lib()).parason_beam_reorder(parent.data_ptr(), rows, args, n, _stream(parent.device))
     if rc != OK:
         raise ParasonError(rc, "parason_beam_reorder")
-    return out
+    return res
 
 
 def _row_bytes(x, rows: int):
     """Bytes of a row of x, and from one row to the next."""
-    size = x.element_size()
     if x.is_contiguous():
-        n = x.numel()
-        if rows == 0 or n % rows:
+        n = x.numel() * x.element_size()
+        if rows == 0 or x.numel() % rows:
             if rows == n == 0:
                 return 0, 0
             raise ValueError("an array must have rows equal parts")
-        return n // rows * size, n // rows * size
+        return n // rows, n // rows
+    size = x.element_size()
     if x.shape[0] != rows or (rows and not x[0].is_contiguous()) or x.stride(0) < 0:
         raise ValueError("an array must be [rows, ...] with contiguous rows")
     n = x[0].numel() if rows else 0
