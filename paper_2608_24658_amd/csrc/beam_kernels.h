@@ -104,6 +104,12 @@ __device__ __forceinline__ float block_bound(float x, int n, float *red)
     return fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
 }
 
+/* A larger key is the better candidate: the larger logit, of equal ones (zeros of either sign are equal) the lower token. */
+__device__ __forceinline__ uint64_t beam_key(float logit, int32_t token)
+{
+    return ((uint64_t)in_order(logit + 0.0f) << 32) | (uint32_t)~token;
+}
+
 __device__ __forceinline__ int lanes_below(uint64_t mask)
 {
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
@@ -114,7 +120,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
 {
     constexpr int ES = T == PARASON_DTYPE_F32 ? 4 : 2, VE = 16 / ES, NV = BEAM_PER_THREAD / VE;
     __shared__ float red[16];
-    __shared__ BeamCandidate list[BEAM_LIST];
+    __shared__ __attribute__((aligned(16))) uint64_t list[BEAM_LIST + 2]; /* order of the logit, and of the token from the last */
     __shared__ int32_t n_list;
     const uint32_t chunk = blockIdx.x % (uint32_t)a.chunks;
     const int64_t row = blockIdx.x / (uint32_t)a.chunks;
@@ -192,7 +198,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
             const uint64_t b = __ballot(v[i] >= bound);
             if (b == 0) continue;
             const int at = base + lanes_below(b);
-            if (v[i] >= bound && at < BEAM_LIST) list[at] = BeamCandidate{v[i], token_of(i)};
+            if (v[i] >= bound && at < BEAM_LIST) list[at] = beam_key(v[i], token_of(i));
             base += __popcll(b);
         }
     }
@@ -200,14 +206,16 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
     const int n = n_list;
     if (tid == 0) a.sums[row * a.chunks + chunk] = make_float2(m, red[12] + red[13] + red[14] + red[15]);
     if (n <= BEAM_LIST) {
+        if (tid < 2) list[n + tid] = 0;      /* (before everything) */
+        __syncthreads();
         for (int c = tid; c < n; c += BEAM_THREADS) {
-            const BeamCandidate me = list[c];
+            const uint64_t me = list[c];
             int before = 0;
-            for (int k = 0; k < n; ++k) {
-                const BeamCandidate o = list[k];
-                before += o.logit > me.logit || (o.logit == me.logit && o.token < me.token);
+            for (int k = 0; k < n; k += 2) {
+                const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&list[k]);
+                before += (o.x > me) + (o.y > me);
             }
-            if (before < a.beams) best[before] = me;
+            if (before < a.beams) best[before] = BeamCandidate{from_order((uint32_t)(me >> 32)), (int32_t)~(uint32_t)me};
         }
         if (tid >= n && tid < a.beams) best[tid] = BeamCandidate{-INFINITY, -1};
         return;
@@ -229,11 +237,12 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
             if (f > b.logit || (f == b.logit && t < b.token)) b = BeamCandidate{f, t};
         }
         __syncthreads();
-        if ((tid & 63) == 0) list[tid >> 6] = b;
+        BeamCandidate *const heads = reinterpret_cast<BeamCandidate *>(list);
+        if ((tid & 63) == 0) heads[tid >> 6] = b;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const BeamCandidate o = list[w];
+            const BeamCandidate o = heads[w];
             if (o.logit > b.logit || (o.logit == b.logit && o.token < b.token)) b = o;
         }
         if (tid == 0) best[k] = BeamCandidate{b.logit, b.logit == -INFINITY ? -1 : b.token};

@@ -909,7 +909,7 @@ def beam_select(logits, scores, beams: int, states=None, workspace=None) -> dict
     dev = logits.device
     if workspace is None:
         workspace = T.empty(beam_workspace_size(rows // beams, beams, vocab), dtype=T.u8, device=dev)
-    score = T.empty(rows, dtype=T.f32, device=dev)
+    score = scores.new_empty(rows)
     parent, token = T.empty((2, rows), dtype=T.i32, device=dev).unbind()
     rc = (_lib or lib()).parason_beam_select(
         logits.data_ptr(), vocab, stride[0] if rows > 1 else vocab, code, scores.data_ptr(),
@@ -939,7 +939,7 @@ def beam_reorder(parent, arrays, out=None) -> list:
             raise TypeError("an array must be a device tensor")
         size, stride = _row_bytes(x, rows)
         if out is None:
-            y, to = T.empty(x.shape, dtype=x.dtype, device=x.device), size
+            y, to = x.new_empty(x.shape), size
         else:
             y = out[i]
             if x.dtype is not y.dtype or x.shape != y.shape or not y.is_cuda:
