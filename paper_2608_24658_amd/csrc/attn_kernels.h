@@ -48,6 +48,7 @@ struct TreeArgs {
     float2 *part_ml;     /* [n_tokens * n_q_heads][parts]: exponent of the maximum, sum */
 };
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short frag8 __attribute__((ext_vector_type(8)));
 typedef short frag4 __attribute__((ext_vector_type(4)));
 typedef float acc16 __attribute__((ext_vector_type(16)));
@@ -100,6 +101,15 @@ __device__ __forceinline__ uint2 widen4(uint32_t w)
         return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
     }
+    if (F16) {
+        /* 1024 + (code + 128) is the float16 with the code in its low byte */
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        const h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+        const uint32_t u = w ^ 0x80808080u;
+        const h2 a = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
+        const h2 b = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
+        return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+    }
     float x[4];
     int8x4_to_f32(w, x);
     return make_uint2(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]));
@@ -113,23 +123,31 @@ __device__ __forceinline__ frag8 widen8(uint2 w)
     return __builtin_bit_cast(frag8, make_uint4(a.x, a.y, b.x, b.y));
 }
 
-/* Whether one of four e4m3 codes is NaN (all ones below the sign). */
-__device__ __forceinline__ bool any_nan_code(uint32_t w)
+/* A word of V without its infinities and NaN, which become zeros. */
+template <int KIND>
+__device__ __forceinline__ uint32_t finite_word(uint32_t w)
 {
-    const uint32_t y = ~w & 0x7F7F7F7Fu; /* a zero byte for each */
-    return ((y - 0x01010101u) & ~y & 0x80808080u) != 0u;
+    if (KIND == KV_INT8) return w;
+    if (KIND == KV_FP8) {
+        /* NaN is all ones below the sign: a zero byte of the complement */
+        const uint32_t some = ((~w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) & 0x80808080u;
+        return w & ((some >> 7) * 255u);
+    }
+    const uint32_t e = KIND == KV_F16 ? 0x7C00u : 0x7F80u;
+    return w & (((w & e) != e ? 0x0000FFFFu : 0u) | (((w >> 16) & e) != e ? 0xFFFF0000u : 0u));
 }
 
-/* Whether one of two 16-bit values is an infinity or NaN. */
-template <bool F16>
-__device__ __forceinline__ bool not_finite2(uint32_t w)
+/* A value of the cache, and whether it is an infinity or NaN. */
+template <int KIND>
+__device__ __forceinline__ float cached_value(const char *p)
 {
-    const uint32_t e = F16 ? 0x7C00u : 0x7F80u;
-    return (w & e) == e || ((w >> 16) & e) == e;
+    if (KIND == KV_BF16) return bf16_to_f32(*reinterpret_cast<const uint16_t *>(p));
+    if (KIND == KV_F16) return f16_to_f32(*reinterpret_cast<const uint16_t *>(p));
+    float x[4];
+    if (KIND == KV_FP8) fp8x4_to_f32((uint8_t)*p, x);
+    else int8x4_to_f32((uint8_t)*p, x);
+    return x[0];
 }
-
-template <bool F16>
-__device__ __forceinline__ float widen1(uint16_t h) { return F16 ? f16_to_f32(h) : bf16_to_f32(h); }
 
 constexpr int TREE_THREADS = 256;
 constexpr int TREE_SKIP_WORDS = 64; /* of the list of a tree's tiles that nobody in the block sees: 2,048 tiles */
@@ -254,7 +272,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     const int32_t my_parts = parts_of(a, sp.end);
     if (part >= my_parts) return;
     const int32_t k_begin = part * a.part_len;
-    const int32_t k_end = part == my_parts - 1 ? sp.end : k_begin + a.part_len;
+    /* (a pool without pages: nothing is read, and what needs a position is NaN) */
+    const int32_t k_end = a.c.n_pages == 0 ? k_begin : part == my_parts - 1 ? sp.end : k_begin + a.part_len;
 
     /* ---- this lane's query */
     const int32_t col = q_block * COLS + wq * CN + n;
@@ -289,9 +308,12 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     const uint64_t *const my_mask = a.mask ? a.mask + t * a.mask_stride : nullptr;
     const int32_t tree_words = (sp.tree + 63) >> 6;
 
-    if (tid < 2) flags[tid] = -1;
+    if (tid < 2) flags[tid] = tid == 0 && a.c.n_pages == 0 && sp.end > 0 ? 0 : -1;
     if (tid < TREE_SKIP_WORDS) skip[tid] = 0u;
     for (int i = tid; i < TK; i += TREE_THREADS) v_stamp[i] = -1;
+    if (a.c.head_dim < DP)                   /* what is never loaded is zero */
+        for (int i = tid * 16; i < Sh::KBYTES + Sh::VBYTES; i += TREE_THREADS * 16)
+            *reinterpret_cast<uint4 *>(tile + i) = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
 
     /* ---- the tree's tiles that some column sees: bit (tile - first tile of the tree) of `skip` */
@@ -333,8 +355,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     const int32_t loader = Sh::SOLO ? lane : tid, row0 = Sh::SOLO ? k0 : 0; /* who loads what of a tile */
     const int32_t my_piece = loader % VPR, my_row = row0 + loader / VPR;
     const bool piece_live = my_piece * VE < a.c.head_dim;
-    const char *const kb = a.c.k + ((int64_t)head * a.c.stride_head + my_piece * VE) * ES;
-    const char *const vb = a.c.v + ((int64_t)head * a.c.stride_head + my_piece * VE) * ES;
+    const int64_t piece_at = (int64_t)head * a.c.stride_head + (piece_live ? my_piece * VE : 0);
+    const char *const kb = a.c.k + piece_at * ES, *const vb = a.c.v + piece_at * ES;
     auto together = [&]() {                  /* what a loader put into LDS is there for the others */
         if (!Sh::SOLO) {
             __syncthreads();
@@ -343,43 +365,35 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             __builtin_amdgcn_wave_barrier();
         }
     };
-    int32_t pg = -1, pg_slot = 0;            /* of position row0 + loader of a tile */
+    /* Positions behind the part's last one read that again, and bad pages the pool's first value: every load has an
+     * address, and what comes of these is masked, or NaN in the end. */
+    int32_t pg = 0, pg_slot = 0;             /* of position row0 + loader of a tile */
     auto load_page = [&](int32_t x) {
+        if (loader >= ROWS) return;
         const int32_t p = x * TK + row0 + loader;
-        pg = -1;
-        if (loader < ROWS && p < k_end) {
-            const uint32_t nth = div_by((uint32_t)p, a.c.page_div);
-            pg_slot = p - (int32_t)(nth * (uint32_t)a.c.page_size);
-            pg = a.r.pages[row * a.r.pages_stride + nth];
-            if (pg < 0 || pg >= a.c.n_pages) pg = -2;
-        }
+        const uint32_t at = (uint32_t)(p < k_end ? p : k_end - 1), nth = div_by(at, a.c.page_div);
+        pg_slot = (int32_t)(at - nth * (uint32_t)a.c.page_size);
+        pg = a.r.pages[row * a.r.pages_stride + nth];
     };
-    int64_t scale_at = -1;
+    int64_t scale_at = 0;
     auto put_place = [&]() {
-        if (loader < ROWS) {
-            if (pg == -2) flags[0] = 0;
-            place[row0 + loader] = pg < 0 ? -1 : (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
-            if (CODES)
-                scale_at = pg < 0 ? -1 : (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
-                                             (int64_t)head * a.c.scale_stride_head;
-        }
+        if (loader >= ROWS) return;
+        if (pg < 0 || pg >= a.c.n_pages) flags[0] = 0, pg = pg_slot = 0;
+        place[row0 + loader] = (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
+        if (CODES)
+            scale_at = (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
+                       (int64_t)head * a.c.scale_stride_head;
     };
-    uint4 kr[NP], vr[NP];
+    u32x4 kr[NP], vr[NP];
     float k_scale = 0.0f, v_scale = 0.0f;    /* of position row0 + loader */
     auto load_tile = [&]() {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int64_t from = place[my_row + p * RPP];
-            kr[p] = vr[p] = make_uint4(0u, 0u, 0u, 0u);
-            if (from >= 0 && piece_live) {
-                kr[p] = *reinterpret_cast<const uint4 *>(kb + from * ES);
-                vr[p] = *reinterpret_cast<const uint4 *>(vb + from * ES);
-            }
+            kr[p] = *reinterpret_cast<const u32x4 *>(kb + from * ES);
+            vr[p] = *reinterpret_cast<const u32x4 *>(vb + from * ES);
         }
-        if (CODES) {
-            k_scale = v_scale = 0.0f;
-            if (loader < ROWS && scale_at >= 0) k_scale = a.c.k_scale[scale_at], v_scale = a.c.v_scale[scale_at];
-        }
+        if (CODES && loader < ROWS) k_scale = a.c.k_scale[scale_at], v_scale = a.c.v_scale[scale_at];
     };
     uint64_t m_lo = 0, m_hi = 0;             /* mask words of a tile's positions of this wave */
     auto load_mask = [&](int32_t x) {
@@ -398,13 +412,15 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     /* tiles in turn: the one in work, and the one behind it */
     int32_t x = next_tile(k_begin / TK);
     int32_t x1 = x < t_end ? next_tile(x + 1) : t_end;
-    load_page(x);
-    put_place();
-    together();
-    load_page(x1);
-    load_mask(x);
-    load_tile();
-    together();
+    if (x < t_end) {
+        load_page(x);
+        put_place();
+        together();
+        load_page(x1);
+        load_mask(x);
+        load_tile();
+        together();
+    }
     while (x < t_end) {
         const int32_t kp = x * TK;
         /* some column does not see all of the tile (of the wave's part of it) */
@@ -413,28 +429,35 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         put_place();
         if (CODES && loader < ROWS) k_sc[row0 + loader] = k_scale, v_sc[row0 + loader] = v_scale;
         bool odd_seen = false;
+        if (masked && KIND != KV_INT8) {
+            /* infinities and NaN of V reach only the queries that see them, for which a product by zero would not do:
+             * they are left out here and added one position at a time below */
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const int r = my_row + p * RPP;
-            char *const kd = Ks + (r * KS + my_piece * VE) * LS, *const vd = Vs + (r * VS + my_piece * VE) * LS;
-            if (CODES && !RAW) {
-                const uint32_t kw[4] = {kr[p].x, kr[p].y, kr[p].z, kr[p].w}, vw[4] = {vr[p].x, vr[p].y, vr[p].z, vr[p].w};
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    *reinterpret_cast<frag8 *>(kd + 16 * i) = widen8<F16, KIND>(make_uint2(kw[2 * i], kw[2 * i + 1]));
-                    *reinterpret_cast<frag8 *>(vd + 16 * i) = widen8<PF16, KIND>(make_uint2(vw[2 * i], vw[2 * i + 1]));
+            for (int p = 0; p < NP; ++p) {
+                const u32x4 v = vr[p];
+                const u32x4 f = {finite_word<KIND>(v.x), finite_word<KIND>(v.y), finite_word<KIND>(v.z), finite_word<KIND>(v.w)};
+                if (piece_live && ((f.x ^ v.x) | (f.y ^ v.y) | (f.z ^ v.z) | (f.w ^ v.w)) != 0u) {
+                    v_stamp[my_row + p * RPP] = x;
+                    odd_seen = true;
                 }
-            } else {
-                *reinterpret_cast<uint4 *>(kd) = kr[p];
-                *reinterpret_cast<uint4 *>(vd) = vr[p];
+                vr[p] = f;
             }
-            if (masked) {
-                const uint4 v = vr[p];
-                const bool odd = KIND == KV_INT8 ? false
-                                 : KIND == KV_FP8 ? any_nan_code(v.x) || any_nan_code(v.y) || any_nan_code(v.z) || any_nan_code(v.w)
-                                                  : not_finite2<PF16>(v.x) || not_finite2<PF16>(v.y) || not_finite2<PF16>(v.z) ||
-                                                        not_finite2<PF16>(v.w);
-                if (odd) v_stamp[r] = x, odd_seen = true;
+        }
+        if (piece_live) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int r = my_row + p * RPP;
+                char *const kd = Ks + (r * KS + my_piece * VE) * LS, *const vd = Vs + (r * VS + my_piece * VE) * LS;
+                if (CODES && !RAW) {
+                    *reinterpret_cast<frag8 *>(kd) = widen8<F16, KIND>(make_uint2(kr[p].x, kr[p].y));
+                    *reinterpret_cast<frag8 *>(kd + 16) = widen8<F16, KIND>(make_uint2(kr[p].z, kr[p].w));
+                    *reinterpret_cast<frag8 *>(vd) = widen8<PF16, KIND>(make_uint2(vr[p].x, vr[p].y));
+                    *reinterpret_cast<frag8 *>(vd + 16) = widen8<PF16, KIND>(make_uint2(vr[p].z, vr[p].w));
+                    __builtin_amdgcn_sched_barrier(0);
+                } else {
+                    *reinterpret_cast<u32x4 *>(kd) = kr[p];
+                    *reinterpret_cast<u32x4 *>(vd) = vr[p];
+                }
             }
         }
         bool odd_values = false;             /* of the wave's positions, or of the block's */
@@ -532,20 +555,24 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-            for (int r = 0; r < NV; ++r) {
-                s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c2, -ref));
-                l += s[u][r];
-            }
+            for (int r = 0; r < NV; ++r) s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c2, -ref));
+        float l4[4] = {};
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int r = 0; r < NV; ++r) l4[r & 3] += s[u][r];
+        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
         if (CODES) {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
-                const uint32_t mine = see[u] >> (4 * h);
 #pragma unroll
                 for (int i = 0; i < NV / 4; ++i) {
                     const float4 f = *reinterpret_cast<const float4 *>(&v_sc[k0 + u * 32 + KSTEP * i + 4 * h]);
                     s[u][4 * i] *= f.x, s[u][4 * i + 1] *= f.y, s[u][4 * i + 2] *= f.z, s[u][4 * i + 3] *= f.w;
                 }
                 if (masked) {                /* no scale, whatever it is, makes a weight where nothing is seen */
+                    uint32_t mine = see[u] >> (4 * h);
+                    asm volatile("" : "+v"(mine)); /* (not worked out for the tiles that all see) */
 #pragma unroll
                     for (int r = 0; r < NV; ++r)
                         if (!((mine >> (KSTEP * (r / 4) + (r & 3))) & 1u)) s[u][r] = 0.0f;
@@ -558,51 +585,53 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         const int g16 = CN == 32 ? ((lane >> 4) & 1) * 16 : 0, i16 = lane & 15;
         const char *va = RAW ? Vs + (k0 + 4 * h + ((i16 >> 1) & 3) + KSTEP * (i16 >> 3)) * VS + g16 + (i16 & 1) * 8
                              : Vs + ((k0 + 4 * h + (i16 >> 2)) * VS + g16 + (i16 & 3) * 4) * 2;
+        constexpr int STEPS = SUBS * (NV / 8); /* products' worth of positions */
+        auto read_values = [&](int g, u32x4 *vf) {
+            typedef int int2v __attribute__((ext_vector_type(2)));
+            typedef __attribute__((address_space(3))) frag4 lds4;
+            typedef __attribute__((address_space(3))) int2v lds8;
 #pragma unroll
-        for (int u = 0; u < SUBS; ++u) {
-#pragma unroll
-            for (int k = 0; k < NV / 8; ++k) {
-                uint32_t pw[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) pw[i] = pack2<PF16>(s[u][8 * k + 2 * i], s[u][8 * k + 2 * i + 1]);
-                const frag8 pf = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
-                frag8 pf_rest = {};
-                if (SPLIT) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        pw[i] = pack2<PF16>(s[u][8 * k + 2 * i] - __uint_as_float(pw[i] << 16),
-                                            s[u][8 * k + 2 * i + 1] - __uint_as_float(pw[i] & 0xFFFF0000u));
-                    pf_rest = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
-                }
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    typedef int int2v __attribute__((ext_vector_type(2)));
-                    typedef __attribute__((address_space(3))) frag4 lds4;
-                    typedef __attribute__((address_space(3))) int2v lds8;
-                    const char *v0 = va + ((u * 32 + k * 16) * VS + d * CN) * LS;
-                    frag8 vf;
-                    if (RAW) {
-                        const int2v f = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8 *)v0);
-                        vf = widen8<PF16, KIND>(make_uint2((uint32_t)f.x, (uint32_t)f.y));
-                    } else {
-                        const frag4 f0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)v0);
-                        const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + KSTEP * VS * LS));
-                        vf = __builtin_shufflevector(f0, f1, 0, 1, 2, 3, 4, 5, 6, 7);
-                    }
-                    if (odd_values) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (not_finite2<PF16>((uint16_t)vf[i])) vf[i] = 0;
-                    }
-                    o[d] = mma<PF16>(vf, pf, o[d]);
-                    if (SPLIT) o[d] = mma<PF16>(vf, pf_rest, o[d]);
+            for (int d = 0; d < ND; ++d) {
+                const char *v0 = va + ((g / (NV / 8) * 32 + g % (NV / 8) * 16) * VS + d * CN) * LS;
+                if (RAW) {
+                    const int2v f = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8 *)v0);
+                    vf[d].x = (uint32_t)f.x, vf[d].y = (uint32_t)f.y;
+                } else {
+                    const frag4 f0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)v0);
+                    const frag4 f1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v0 + KSTEP * VS * LS));
+                    vf[d] = __builtin_bit_cast(u32x4, (frag8)__builtin_shufflevector(f0, f1, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
             }
+        };
+        u32x4 vf[STEPS + 1][ND];             /* (codes: the first half) */
+        read_values(0, vf[0]);
+#pragma unroll
+        for (int g = 0; g < STEPS; ++g) {
+            const int u = g / (NV / 8), k = g % (NV / 8);
+            if (g + 1 < STEPS) read_values(g + 1, vf[g + 1]);
+            uint32_t pw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pw[i] = pack2<PF16>(s[u][8 * k + 2 * i], s[u][8 * k + 2 * i + 1]);
+            const frag8 pf = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+            frag8 pf_rest = {};
+            if (SPLIT) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    pw[i] = pack2<PF16>(s[u][8 * k + 2 * i] - __uint_as_float(pw[i] << 16),
+                                        s[u][8 * k + 2 * i + 1] - __uint_as_float(pw[i] & 0xFFFF0000u));
+                pf_rest = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const frag8 v = RAW ? widen8<PF16, KIND>(make_uint2(vf[g][d].x, vf[g][d].y)) : __builtin_bit_cast(frag8, vf[g][d]);
+                o[d] = mma<PF16>(v, pf, o[d]);
+                if (SPLIT) o[d] = mma<PF16>(v, pf_rest, o[d]);
+            }
+            /* one step's values are read ahead, and no more: registers */
+            __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
         if (odd_values) {
-            /* infinities and NaN of V reach only the queries that see them: a product by zero would not do.  They
-             * were left out above and are added one position at a time. */
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
                 for (int kk = 0; kk < 32; ++kk) {
@@ -613,14 +642,24 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                     for (int i = 0; i < NV; ++i) p = (kk / KSTEP * 4 + (kk & 3)) == i ? s[u][i] : p;
                     p = __shfl(p, n + CN * (kk % KSTEP / 4));
                     if (!((see[u] >> kk) & 1u)) continue;
+                    int32_t slot;
+                    const int32_t page = page_of(a.r, a.c, row, kp + r < k_end ? kp + r : k_end - 1, &slot);
+                    if (page < 0) continue;
+                    int32_t h4 = 4 * h;      /* not known before: what depends on it is not worth registers in the loop */
+                    asm volatile("" : "+v"(h4));
+                    const char *v = a.c.v + ((int64_t)page * a.c.stride_page + (int64_t)slot * a.c.stride_slot +
+                                             (int64_t)head * a.c.stride_head) * ES;
 #pragma unroll
-                    for (int d = 0; d < ND; ++d)
+                    for (int d = 0; d < ND; ++d) {
 #pragma unroll
                         for (int i = 0; i < AC; ++i) {
-                            const char *e = Vs + (r * VS + d * CN + 8 * (i / 4) + 4 * h + (i & 3)) * LS;
-                            const uint16_t v = RAW ? (uint16_t)widen4<PF16, KIND>((uint8_t)*e).x : *reinterpret_cast<const uint16_t *>(e);
-                            if (not_finite2<PF16>(v)) o[d][i] += p * widen1<PF16>(v);
+                            const int at_d = d * CN + 8 * (i / 4) + h4 + (i & 3);
+                            if (at_d >= a.c.head_dim) continue;
+                            const float e = cached_value<KIND>(v + at_d * ES);
+                            if (!(e > -INFINITY && e < INFINITY)) o[d][i] += p * e;
                         }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             }
         }
