@@ -476,21 +476,42 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         /* ---- S^T */
         float s[SUBS][NV];
         __builtin_amdgcn_s_setprio(1);       /* a wave in its products goes before one in its exponentials */
+        /* the keys of a product are read KG products ahead */
+        constexpr int KROWS = SUBS * (32 / CN), KG = NK < 4 ? NK : 4, KSTEPS = KROWS * NK / KG;
+        auto read_keys = [&](int g, u32x4 *kf) {
+            const char *ka = Ks + ((k0 + g * KG / NK * CN + n) * KS + h * 8) * LS;
+#pragma unroll
+            for (int j = 0; j < KG; ++j) {
+                const int k = (g * KG + j) % NK;
+                if (RAW) {
+                    const uint2 c = *reinterpret_cast<const uint2 *>(ka + k * KD);
+                    kf[j].x = c.x, kf[j].y = c.y;
+                } else {
+                    kf[j] = *reinterpret_cast<const u32x4 *>(ka + k * KD * 2);
+                }
+            }
+        };
+        u32x4 kf[KSTEPS + 1][KG];
+        read_keys(0, kf[0]);
+        acc c[KROWS];
+#pragma unroll
+        for (int i = 0; i < KROWS; ++i) c[i] = acc{};
+#pragma unroll
+        for (int g = 0; g < KSTEPS; ++g) {
+            if (g + 1 < KSTEPS) read_keys(g + 1, kf[g + 1]);
+#pragma unroll
+            for (int j = 0; j < KG; ++j) {
+                const frag8 f = RAW ? widen8<F16, KIND>(make_uint2(kf[g][j].x, kf[g][j].y)) : __builtin_bit_cast(frag8, kf[g][j]);
+                c[g * KG / NK] = mma<F16>(f, qf[(g * KG + j) % NK], c[g * KG / NK]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
 #pragma unroll
-            for (int i = 0; i < 32 / CN; ++i) {
-                acc c = {};
-                const char *ka = Ks + ((k0 + u * 32 + i * CN + n) * KS + h * 8) * LS;
+            for (int i = 0; i < 32 / CN; ++i)
 #pragma unroll
-                for (int k = 0; k < NK; ++k) {
-                    const frag8 kf = RAW ? widen8<F16, KIND>(*reinterpret_cast<const uint2 *>(ka + k * KD))
-                                         : *reinterpret_cast<const frag8 *>(ka + k * KD * 2);
-                    c = mma<F16>(kf, qf[k], c);
-                }
-#pragma unroll
-                for (int r = 0; r < AC; ++r) s[u][i * AC + r] = c[r];
-            }
+                for (int r = 0; r < AC; ++r) s[u][i * AC + r] = c[u * (32 / CN) + i][r];
             if (CODES) {
 #pragma unroll
                 for (int i = 0; i < NV / 4; ++i) {
