@@ -460,6 +460,7 @@ int parason_join_sized(const parason_handle *h, const int32_t *tokens, const int
 
 #define PARASON_KV_MAX_DIM 256
 #define PARASON_KV_MAX_HEADS 1024
+#define PARASON_KV_MAX_LEN (1 << 30) /* of max_kv_len; tree attention: also of max_length * n_q_heads / n_heads */
 
 /* Device memory of the caller; the struct itself is host memory.  Value d of
  * head h in slot t of page p is element
@@ -494,7 +495,7 @@ typedef struct parason_kv_rows {
     int64_t pages_stride;
     int32_t max_pages;
     int32_t max_length;       /* >= every lengths[i] */
-    int32_t max_kv_len;       /* >= every kv_lens[i] */
+    int32_t max_kv_len;       /* >= every kv_lens[i], at most PARASON_KV_MAX_LEN */
 } parason_kv_rows;
 
 /* Bits that the calls below OR into row_status[i] (uint32[n_rows] that the

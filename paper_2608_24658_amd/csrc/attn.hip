@@ -49,7 +49,7 @@ constexpr size_t PART_BYTES = (size_t)1 << 29;   /* of the parts' vectors */
 int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads, TreePlan *p)
 {
     const int64_t group = n_q_heads / c->n_heads, cols = (int64_t)r->max_length * group;
-    if (cols > INT32_MAX) return PARASON_ERR_SIZE;
+    if (cols > PARASON_KV_MAX_LEN) return PARASON_ERR_SIZE; /* (and blocks of columns end within 31 bits) */
     p->cols = cols <= 16 ? 16 : cols <= 64 ? 32 : 128;
     p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
     const int64_t base = r->n_rows * c->n_heads * p->q_blocks;
@@ -151,8 +151,7 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
     hipLaunchKernelGGL(pick(cache->head_dim, p.cols, f16, kind), dim3((unsigned)p.blocks), dim3(pk::TREE_THREADS), 0, stream, a);
     if (p.parts > 1) {
         constexpr int64_t per_block = pk::TREE_THREADS / 64;
-        const int64_t waves = rows->n_rows * rows->max_length * heads;
-        if (waves / per_block >= INT32_MAX) return PARASON_ERR_SIZE;
+        const int64_t waves = rows->n_rows * rows->max_length * heads; /* few: plan cuts no call of many columns */
         hipLaunchKernelGGL(f16 ? pk::tree_join<true> : pk::tree_join<false>, dim3((unsigned)((waves + per_block - 1) / per_block)),
                            dim3(pk::TREE_THREADS), 0, stream, a, p.cols);
     }

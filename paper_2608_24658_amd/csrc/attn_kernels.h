@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
 
     /* ---- the tree's tiles that some column sees: bit (tile - first tile of the tree) of `skip` */
     const int32_t tile0 = sp.base / TK;
-    if (a.mask && k_end > sp.base) {
+    if (a.mask && sp.ok && k_end > sp.base) {   /* (a bad row's tree may be longer than its mask words) */
         const int32_t lo = k_begin > sp.base ? (k_begin - sp.base) >> 6 : 0;
         const int32_t words = ((k_end - sp.base + 63) >> 6) - lo;
         const int64_t total = (int64_t)words * (sp.tok1 - sp.tok0);

@@ -63,7 +63,8 @@ inline int check_row_sizes(const parason_kv_rows *r)
 {
     if (!r) return PARASON_ERR_NULL;
     if (r->n_rows < 0 || r->n_rows > INT32_MAX || r->n_tokens < 0 || r->n_tokens > INT32_MAX || r->max_pages < 0 ||
-        r->max_length < 0 || r->max_kv_len < 0 || !stride_fits(r->pages_stride, r->n_rows))
+        r->max_length < 0 || r->max_kv_len < 0 || r->max_kv_len > PARASON_KV_MAX_LEN ||
+        !stride_fits(r->pages_stride, r->n_rows))
         return PARASON_ERR_SIZE;
     return PARASON_OK;
 }

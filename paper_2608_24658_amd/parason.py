@@ -69,6 +69,7 @@ KV_BAD_ROW = 1 << 0
 KV_BAD_PAGE = 1 << 1
 KV_MAX_DIM = 256
 KV_MAX_HEADS = 1024
+KV_MAX_LEN = 1 << 30
 BEAM_MAX = 64
 BEAM_ARRAYS = 8
 

@@ -109,6 +109,19 @@ def test_tree_attention_rejects_bad_arguments():
     assert call(r=rows(max_length=0), w=None) == P.OK
 
 
+def test_rows_longer_than_31_bits_can_count():
+    """Positions and columns are counted in 32 bits, a tile beyond the last one included."""
+    L, ws, over = P.lib(), ctypes.c_size_t(), P.KV_MAX_LEN + 1
+    for fn in (L.parason_kv_write, L.parason_kv_read):
+        assert fn(cache(), rows(max_kv_len=over), FAKE, FAKE, P.DTYPE_BF16, 1024, 128, None, None) == P.ERR_SIZE
+    size = L.parason_tree_attention_workspace_size
+    assert size(cache(), rows(max_kv_len=over), 32, ctypes.byref(ws)) == P.ERR_SIZE
+    assert size(cache(), rows(max_kv_len=P.KV_MAX_LEN), 32, ctypes.byref(ws)) == P.OK
+    assert size(cache(), rows(max_length=P.KV_MAX_LEN // 4), 32, ctypes.byref(ws)) == P.OK
+    assert size(cache(), rows(max_length=P.KV_MAX_LEN // 4 + 1), 32, ctypes.byref(ws)) == P.ERR_SIZE
+    assert L.parason_tree_attention(cache(), rows(max_length=P.KV_MAX_LEN // 4 + 1), tree(), None, FAKE, 1 << 40, None) == P.ERR_SIZE
+
+
 def test_beam_select_rejects_bad_arguments():
     size, fn = P.lib().parason_beam_workspace_size, P.lib().parason_beam_select
     ws = ctypes.c_size_t()

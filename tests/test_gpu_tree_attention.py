@@ -238,6 +238,31 @@ def test_rows_and_pages_that_are_bad(dev):
     assert status.cpu().tolist() == [0, 0, b, b, b, 0]
 
 
+def test_trees_far_longer_than_their_masks(dev):
+    """Lengths that no mask and no cache holds: reported, NaN, and the rows beside them whole."""
+    log("case bad trees")
+    P = Paged(dev, [40] * 5, 8, 2, 64, "bf16", seed=3)
+    rng = np.random.default_rng(0)
+    P.fill(lambda i, n: rng.standard_normal((2, n, 2, 64)))
+    rows, total, starts = P.rows([2] * 5)
+    kv = rows.kv_lens.clone()
+    kv[3] = -(2 ** 31) + 1
+    rows = rows._replace(kv_lens=kv)
+    q = torch.randn(total, 4, 64, device=dev, dtype=torch.bfloat16)
+    mask = torch.full((total, 1), -1, dtype=torch.int64, device=dev)
+    trees = torch.tensor([2, 2 ** 31 - 1, 10 ** 6, 2, 0], dtype=torch.int32, device=dev)
+    status = torch.zeros(5, dtype=torch.int32, device=dev)
+    got, lse = PX.tree_attention(q, P.cache, rows, mask=mask, tree_lens=trees, lse=True, status=status)
+    b = PX.KV_BAD_ROW
+    assert status.cpu().tolist() == [0, b, b, b, 0]
+    got, lse = got.cpu().double(), lse.cpu()
+    assert torch.isnan(got[2:8]).all() and torch.isnan(lse[2:8]).all()
+    for i in (0, 4):
+        seen = np.ones((2, 40), bool)
+        o, _, tol, _ = D.attention(q[2 * i: 2 * i + 2].cpu().double().numpy(), *P.held[i], seen, 0.125, 7, 7)
+        assert np.all(np.abs(got[2 * i: 2 * i + 2].numpy() - o) <= tol)
+
+
 def test_offsets_beyond_32_bits(dev):
     """Pages whose elements lie behind 2^32 of the pool's first, for one token and for a chain."""
     log("case long offsets")
