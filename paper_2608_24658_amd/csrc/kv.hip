@@ -35,10 +35,7 @@ struct Read {
 /* Most blocks of a launch.  Rows are cut for the longest one, so many blocks of a ragged call find nothing to do, and
  * the few long rows need enough of theirs to fill the device: 48 rows of 1 to 36,000 positions, FP8 read as bfloat16,
  * 406 us at 8,192 blocks, 260 at 32,768, 267 at 131,072. */
-#ifndef PARASON_KV_BLOCKS
-#define PARASON_KV_BLOCKS 32768
-#endif
-constexpr int64_t MOVE_BLOCKS = PARASON_KV_BLOCKS;
+constexpr int64_t MOVE_BLOCKS = 32768;
 
 int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void *k, const void *v, int32_t dtype,
          int64_t stride_token, int64_t stride_head, uint32_t *row_status, void *stream_ptr, bool write)
