@@ -50,13 +50,20 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
 {
     const int64_t group = n_q_heads / c->n_heads, cols = (int64_t)r->max_length * group;
     if (cols > PARASON_KV_MAX_LEN) return PARASON_ERR_SIZE; /* (and blocks of columns end within 31 bits) */
+    /* more than 2^31 blocks of 128 columns; the products below keep within 63 bits otherwise */
+    if ((double)r->n_rows * r->max_length * n_q_heads > 0x1p38) return PARASON_ERR_SIZE;
     p->cols = cols <= 16 ? 16 : cols <= 64 ? 32 : 128;
     p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
-    const int64_t base = r->n_rows * c->n_heads * p->q_blocks;
+    /* blocks that have columns: those of a row's own tokens, at most one of them not full */
+    int64_t base = r->n_rows * c->n_heads * p->q_blocks;
+    const int64_t filled = (r->n_tokens * group / p->cols + r->n_rows) * c->n_heads;
+    if (filled < base) base = filled;
     const int64_t tile = p->cols < 128 ? 128 : 64;
     /* Enough blocks to fill the device, and for few columns, whose partial results are small, parts short enough that
      * long rows among short ones do not finish last.  A part is worth its results: 8 bytes a column and value, written
-     * and read, against 2 to 4 bytes a position and value. */
+     * and read, against 2 to 4 bytes a position and value.  24 parts of prompts of 2 to 300 tokens behind 1 to 18,000
+     * positions, all blocks the longest row would need counted: 247 us, which is the longest row's; those with
+     * columns: 147. */
     const int64_t shortest = p->cols < 128 ? 512 : 1024;
     int64_t len = p->cols < 128 ? 1024 : 4096;
     while (len > shortest && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
@@ -64,6 +71,7 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
     int64_t parts = (r->max_kv_len + len - 1) / len;
     if (parts < 1 || base >= (p->cols < 128 ? 16 : 1) * PART_BLOCKS) parts = 1;
     if (per_part > 0 && (size_t)parts > PART_BYTES / per_part) parts = PART_BYTES / per_part > 1 ? (int64_t)(PART_BYTES / per_part) : 1;
+    if (r->n_rows * r->max_length * n_q_heads > INT32_MAX) parts = 1; /* tree_join's waves */
     len = (r->max_kv_len + parts - 1) / parts;
     p->part_len = (int32_t)((len + tile - 1) / tile * tile < INT32_MAX ? (len + tile - 1) / tile * tile : len);
     if (p->part_len < tile) p->part_len = (int32_t)tile;
@@ -151,7 +159,7 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
     hipLaunchKernelGGL(pick(cache->head_dim, p.cols, f16, kind), dim3((unsigned)p.blocks), dim3(pk::TREE_THREADS), 0, stream, a);
     if (p.parts > 1) {
         constexpr int64_t per_block = pk::TREE_THREADS / 64;
-        const int64_t waves = rows->n_rows * rows->max_length * heads; /* few: plan cuts no call of many columns */
+        const int64_t waves = rows->n_rows * rows->max_length * heads;
         hipLaunchKernelGGL(f16 ? pk::tree_join<true> : pk::tree_join<false>, dim3((unsigned)((waves + per_block - 1) / per_block)),
                            dim3(pk::TREE_THREADS), 0, stream, a, p.cols);
     }

@@ -119,6 +119,8 @@ def test_rows_longer_than_31_bits_can_count():
     assert size(cache(), rows(max_kv_len=P.KV_MAX_LEN), 32, ctypes.byref(ws)) == P.OK
     assert size(cache(), rows(max_length=P.KV_MAX_LEN // 4), 32, ctypes.byref(ws)) == P.OK
     assert size(cache(), rows(max_length=P.KV_MAX_LEN // 4 + 1), 32, ctypes.byref(ws)) == P.ERR_SIZE
+    for n in (1 << 20, (1 << 31) - 1):  # products of sizes that no 64 bits hold among them
+        assert size(cache(), rows(n_rows=n, max_length=P.KV_MAX_LEN // 4), 32, ctypes.byref(ws)) == P.ERR_SIZE
     assert L.parason_tree_attention(cache(), rows(max_length=P.KV_MAX_LEN // 4 + 1), tree(), None, FAKE, 1 << 40, None) == P.ERR_SIZE
 
 

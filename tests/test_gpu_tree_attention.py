@@ -205,6 +205,15 @@ def test_long_rows_of_few_tokens(dev):
     run_case(dev, "int8", 16, 1, 16, 64, [5000, 100], [9, 7], seed=6)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_long_ragged_parts_of_prompts(dev, kind):
+    """Few tokens in all, though the longest row has many: its blocks of columns are cut into parts too."""
+    log("case ragged parts of prompts %s" % kind)
+    lengths = [150, 1, 3, 1, 0, 2, 1, 40]
+    run_case(dev, kind, 64, 2, 2, 64, [9100, 1, 300, 4097, 0, 2049, 1025, 5000], lengths, seed=7)
+    run_case(dev, kind, 64, 2, 2, 64, [9100, 1, 300, 4097, 0, 2049, 1025, 5000], lengths, shape="threads", seed=8)
+
+
 def test_rows_and_pages_that_are_bad(dev):
     log("case bad rows")
     P = Paged(dev, [40] * 6, 8, 2, 64, "bf16", seed=3)
