@@ -78,3 +78,47 @@ def test_example_runs(dev, capsys):
     log("case beam decode example")
     example().main()
     assert "float8" in capsys.readouterr().out
+
+
+def test_a_step_in_a_graph(dev):
+    """A step's write, read back, attention, choice and reordering in one graph, replayed with other work between the
+    replays: every replay as the eager step."""
+    log("case beam step in a graph")
+    beams, heads, dim, vocab, kv = 4, 2, 64, 3000, 200
+    gen = torch.Generator(device=dev).manual_seed(0)
+    r = lambda *s: torch.randn(*s, generator=gen, device=dev)  # noqa: E731
+    cache = PX.kv_alloc(30, 16, heads, dim, torch.float8_e4m3fn, dev)
+    table = torch.arange(28, dtype=torch.int32, device=dev).view(2, 14)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=dev)  # noqa: E731
+    two = lambda n: PX.KVRows(torch.tensor([0, n], device=dev), i32([n, n]), i32([kv, kv]), table, n, kv)  # noqa: E731
+    old, new = two(kv), two(beams)
+    before = r(2, 2 * kv, heads, dim)
+    q, k, v = r(8, 8, dim).bfloat16(), r(8, heads, dim).bfloat16(), r(8, heads, dim).bfloat16()
+    mask = torch.randint(0, 2 ** 12, (8, 1), generator=gen, device=dev) | 1
+    trees, logits, scores = i32([12, 12]), r(8, vocab), -torch.rand(8, generator=gen, device=dev)
+    history = torch.randint(0, vocab, (8, 77), generator=gen, device=dev, dtype=torch.int32)
+
+    def step():
+        PX.kv_write(k, v, cache, new)
+        back = PX.kv_read(cache, new, 8, torch.bfloat16)
+        out, lse = PX.tree_attention(q, cache, new, mask=mask, tree_lens=trees, lse=True)
+        best = PX.beam_select(logits, scores, beams)
+        moved = PX.beam_reorder(best["parent"], [history, mask])
+        return [*back, out, lse, *best.values(), *moved]
+
+    PX.kv_write(before[0], before[1], cache, old)
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        PX.kv_write(before[1], before[0], cache, old)
+        PX.kv_write(before[0], before[1], cache, old)
+        for t in got:
+            t.zero_()
+        (r(1000) * 2).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
