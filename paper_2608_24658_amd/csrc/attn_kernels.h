@@ -16,10 +16,10 @@
  * short drafts): the four waves take a quarter of each tile's positions each and
  * are joined at the end; what bounds it is reading the cache once.  128 single
  * tokens over 1.0 M positions of 8 heads of 128 FP8 values, 2.19 GB, take 435 us
- * (5.0 TB/s); 16 over 55,000 bfloat16 ones, 0.23 GB, 53 us (4.4 TB/s).
+ * (5.0 TB/s); 16 over 55,000 bfloat16 ones, 0.23 GB, 57 us (4.0 TB/s).
  * More queries: the waves take 32 columns each and share the tile; bound by the
  * products and the exponentials beside them.  A prompt of 8,192 tokens, 32
- * query heads over 8 of 128 values, 550 Gflop, takes 621 us (885 Tflop/s, where
+ * query heads over 8 of 128 values, 550 Gflop, takes 635 us (866 Tflop/s, where
  * a library product of 8192^3 reaches 1,348).  Long rows are cut into parts,
  * whose results tree_join puts together.
  */
