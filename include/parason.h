@@ -569,18 +569,23 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
 
 /* ---- beams ---------------------------------------------------------------
  * n_groups prompts of `beams` beams each; beam b of group g is row
- * g * beams + b.  A row's candidates are its tokens t, each with
- *   score + logits[t] - ln sum_u exp(logits[u]),
- * (logits of -inf, as parason_decode_step leaves them for forbidden tokens, are
- * no candidates), or, when its decode state says PARASON_DECODE_DONE, the row
- * as it is (token -1) with its score alone.  The new beams of a group are its
- * `beams` best candidates, best first, ties to the lowest row and token.
- * Candidates are compared in double precision, from a float32 sum of
- * exponentials.
+ * g * beams + b.  A row's candidates are its tokens t, each with the score
+ *   score + (logits[t] - lse),   lse = top + ln sum_u exp(logits[u] - top),
+ * top its largest logit (logits of -inf, as parason_decode_step leaves them for
+ * forbidden tokens, are no candidates), or, when its decode state says
+ * PARASON_DECODE_DONE, the row as it is (token -1) with its score alone.  The
+ * new beams of a group are its `beams` best candidates, best first, ties to the
+ * lowest row and token.  What is compared is the score that is returned: the
+ * sum is rounded to float32, its logarithm is float32 (a unit in the last place
+ * at most), and each of the three additions is rounded.  The sum itself (float32
+ * exponentials, added in float32 for up to 2,048 of them and in double beyond)
+ * is off by a few 2^-24 of itself at most: rows with the same logits in another
+ * order have the same lse, unless that moves the logarithm to the next float.
  *
  * Not a candidate: a row whose score is not finite (the empty beams of a prompt
  * that has just begun have -inf), whose state says PARASON_DECODE_ERROR, or
- * whose sum is not finite (a NaN or +inf among its logits).  Where a group has
+ * whose sum is not finite (a NaN or +inf among its logits), and a token whose
+ * score is -inf.  Where a group has
  * fewer candidates than beams the last beams are empty: score -inf, token -1,
  * parent the beam's own row. */
 #define PARASON_BEAM_MAX 64

@@ -119,3 +119,32 @@ def beam_select(candidates, beams):
         order = order[c[order] > -np.inf]
         out[g, : order.size] = order
     return out
+
+
+def beam_lse(x):
+    """ln sum exp of a row of logits in 64 bits, and as beam_select has it: the logarithm of sum exp(x - top) rounded to
+    float32 (there: a unit in the last place at most), then its sum with top."""
+    x = np.asarray(x, dtype=np.float64)
+    top = x.max()
+    ln = np.log(np.exp(x - top).sum())
+    return top + ln, np.float32(top) + np.float32(ln)
+
+
+def beam_scores(logits, scores, flags, beams, done=2, lse=None):
+    """The float32 scores of beam_candidates' places as beam_select rounds them: score + (logit - lse), each step once.
+    lse: the rows' own, where the last place of the logarithm matters."""
+    x = np.asarray(logits, dtype=np.float32)
+    scores = np.asarray(scores, dtype=np.float32)
+    rows, vocab = x.shape
+    out = np.full((rows, vocab + 1), -np.inf, np.float32)
+    for r in range(rows):
+        if not np.isfinite(scores[r]):
+            continue
+        if flags[r]:
+            if flags[r] == done:
+                out[r, 0] = scores[r]
+            continue
+        if not np.isfinite(x[r].max()) or np.isnan(x[r]).any():
+            continue
+        out[r, 1:] = scores[r] + (x[r] - (beam_lse(x[r])[1] if lse is None else np.float32(lse[r])))
+    return out.reshape(rows // beams, beams * (vocab + 1))

@@ -22,7 +22,7 @@ int layout_for(int64_t n_groups, int32_t beams, int64_t vocab, BeamLayout *L)
     L->chunks = (vocab + pk::BEAM_CHUNK - 1) / pk::BEAM_CHUNK;
     const int64_t rows = n_groups * beams;
     if (rows > INT32_MAX / L->chunks) return PARASON_ERR_SIZE;
-    L->best = abi::align_up((size_t)(rows * L->chunks) * sizeof(float2));
+    L->best = abi::align_up((size_t)(rows * L->chunks) * sizeof(pk::BeamChunk));
     L->end = L->best + abi::align_up((size_t)(rows * L->chunks) * beams * sizeof(pk::BeamCandidate) + 1);
     return PARASON_OK;
 }
@@ -60,12 +60,13 @@ int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, i
     if (cu_count() <= 0) return PARASON_ERR_DEVICE;
     pk::BeamArgs a;
     a.logits = (const char *)logits;
-    a.vocab = vocab, a.row_bytes = row_stride * elem;
+    a.vocab = vocab, a.row_bytes = row_stride * elem, a.dtype = dtype;
     a.scores = scores, a.states = states, a.beams = beams, a.chunks = (int32_t)L.chunks;
     a.chunks_div = pk::fast_div((uint32_t)L.chunks);
     const int64_t pieces = (vocab * elem + 15) / 16;
     a.chunk_pieces = (int32_t)((pieces + L.chunks - 1) / L.chunks);
-    a.sums = (float2 *)workspace;
+    a.chunk_tokens = (int64_t)a.chunk_pieces * (16 / elem);
+    a.sums = (pk::BeamChunk *)workspace;
     a.best = (pk::BeamCandidate *)((char *)workspace + L.best);
     a.new_scores = new_scores, a.parents = parents, a.tokens = tokens;
     hipStream_t stream = (hipStream_t)stream_ptr;

@@ -2,11 +2,15 @@
  * beam_kernels.h -- beam selection and the reordering of what belongs to a
  * beam for gfx950.
  *
- * The selection is one pass over the logits.  Within a row the order of the
- * candidates is that of the logits, so a block takes a chunk of a row into
- * registers, and from these the chunk's maximum, its sum of exponentials and
- * its `beams` largest logits; a block per group then has each row's sum and
- * chooses among the chunks' candidates, in double precision.  Bound by the
+ * The selection is one pass over the logits.  A candidate's score, float32(score
+ * + float32(logit - lse)), does not fall as its logit rises, so a block takes a
+ * chunk of a row into registers, and from these the chunk's maximum, its sum of
+ * exponentials and its `beams` largest logits; a block per group then has each
+ * row's sum and chooses among the chunks' candidates by their scores.  Rounding
+ * can make the scores of different logits equal, and of equal ones the lowest
+ * token counts: a chunk also says how large a logit it has left out, and where
+ * the score of that one is still among the best, the tokens of the last score
+ * are taken from the logits again, in their order.  Bound by the
  * read: 2,048 rows of 50,257 float16 logits and their reordering, 409 MB in
  * all, take 112 us, the scan 67 of them; 256 rows of 151,936 float32 logits 43
  * us.  The beams of one prompt are three launches, 18 us, and the host's checks.
@@ -40,15 +44,23 @@ struct BeamCandidate {
     int32_t token;
 };
 
+struct BeamChunk {
+    float top;     /* the largest logit */
+    float below;   /* the largest logit that is less than that of the last candidate, or a little more; -inf: none */
+    double sum;    /* of exp(logit - top) */
+};
+
 struct BeamArgs {
     const char *logits;
     int64_t vocab, row_bytes;
+    int32_t dtype;
     const float *scores;
     const parason_decode_state *states;
     int32_t beams, chunks;
     FastDiv chunks_div;
     int32_t chunk_pieces;     /* 16-byte pieces of a chunk: the row's, evenly */
-    float2 *sums;             /* [rows][chunks]: maximum, sum of exp(logit - maximum) */
+    int64_t chunk_tokens;     /* logits of these */
+    BeamChunk *sums;          /* [rows][chunks] */
     BeamCandidate *best;      /* [rows][chunks][beams], best first */
     float *new_scores;
     int32_t *parents, *tokens;
@@ -112,22 +124,39 @@ __device__ __forceinline__ uint64_t beam_key(float logit, int32_t token)
     return ((uint64_t)in_order(logit + 0.0f) << 32) | (uint32_t)~token;
 }
 
+/* The sum of exponentials is that of the products logit * log2(e), of which the second part makes up for the rounding
+ * of the first: alike in every term, it would not average out. */
+constexpr float LOG2E_HI = 1.44269502f, LOG2E_LO = 1.92596299e-8f;
+
+/* The largest logit of the type below x, or a little more (of float16's smallest). */
+template <int T>
+__device__ __forceinline__ float logit_below(float x)
+{
+    /* in_order() of 16-bit logits: bits that are all zero, or of negative ones all one */
+    constexpr uint32_t rest = T == PARASON_DTYPE_F32 ? 0u : T == PARASON_DTYPE_BF16 ? 0xFFFFu : 0x1FFFu;
+    const uint32_t k = in_order(x) - 1u;
+    return from_order((k & 0x80000000u) ? k & ~rest : (k & rest) == rest ? k : (k & ~rest) - 1u);
+}
+
 __device__ __forceinline__ int lanes_below(uint64_t mask)
 {
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
+/* Six waves a SIMD: with the registers of five 77 us instead of 68 for 2,048 rows of 50,257 float16 logits. */
 template <int T>
-__global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
+__global__ void __launch_bounds__(BEAM_THREADS, 6) beam_scan(BeamArgs a)
 {
     constexpr int ES = T == PARASON_DTYPE_F32 ? 4 : 2, VE = 16 / ES, NV = BEAM_PER_THREAD / VE;
-    __shared__ float red[16];
+    __shared__ float red[12];
+    __shared__ double red_sum[4];
+    __shared__ uint32_t last_order, below_order;
     __shared__ __attribute__((aligned(16))) uint64_t list[BEAM_LIST + 2]; /* order of the logit, and of the token from the last */
     __shared__ int32_t n_list;
     const uint32_t chunk = blockIdx.x % (uint32_t)a.chunks;
     const int64_t row = blockIdx.x / (uint32_t)a.chunks;
     const int tid = (int)threadIdx.x;
-    BeamCandidate *const best = a.best + (row * a.chunks + chunk) * a.beams;
+    BeamCandidate *const best = a.best + (int64_t)blockIdx.x * a.beams; /* (blocks are counted as [rows][chunks]) */
     const char *const x = a.logits + row * a.row_bytes;
     if (beam_offers(a, row, a.scores[row]) != BEAM_TOKENS) return;
     /* 16 bytes at a time from the row's first logit on, at whatever alignment that has: which logits a lane adds up, and
@@ -176,17 +205,21 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
     if ((tid & 63) == 0) red[8 + (tid >> 6)] = m;
-    if (tid == 0) n_list = 0;
+    if (tid == 0) n_list = 0, below_order = 0u;
     const float bound = block_bound(mine, a.beams, red);
     m = fmaxf(fmaxf(red[8], red[9]), fmaxf(red[10], red[11]));
     /* ---- sum */
     const float ref = m == -INFINITY ? 0.0f : m;
-    float s = 0.0f;
+    float mine_sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < BEAM_PER_THREAD; ++i) s += __builtin_amdgcn_exp2f((v[i] - ref) * 1.44269504f);
+    for (int i = 0; i < BEAM_PER_THREAD; ++i) {
+        const float d = v[i] - ref;
+        mine_sum += __builtin_amdgcn_exp2f(__builtin_fmaf(d, LOG2E_HI, d * LOG2E_LO));
+    }
 #pragma unroll
-    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
-    if ((tid & 63) == 0) red[12 + (tid >> 6)] = s;
+    for (int k = 32; k > 0; k >>= 1) mine_sum += __shfl_xor(mine_sum, k);
+    /* (double beyond a wave: the logarithm is rounded to float32, and the order of adding should not show in it) */
+    if ((tid & 63) == 0) red_sum[tid >> 6] = (double)mine_sum;
     /* ---- candidates */
     int count = 0;
 #pragma unroll
@@ -206,10 +239,14 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
     }
     __syncthreads();
     const int n = n_list;
-    if (tid == 0) a.sums[row * a.chunks + chunk] = make_float2(m, red[12] + red[13] + red[14] + red[15]);
+    auto record = [&](float below) {
+        a.sums[blockIdx.x] = BeamChunk{fmaxf(fmaxf(red[8], red[9]), fmaxf(red[10], red[11])), below,
+                                       red_sum[0] + red_sum[1] + red_sum[2] + red_sum[3]};
+    };
     if (n <= BEAM_LIST) {
         if (tid < 2) list[n + tid] = 0;      /* (before everything) */
         __syncthreads();
+        uint64_t next = 0;                   /* the best that is no candidate, at the thread that ranks it */
         for (int c = tid; c < n; c += BEAM_THREADS) {
             const uint64_t me = list[c];
             int before = 0;
@@ -218,8 +255,31 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
                 before += (o.x > me) + (o.y > me);
             }
             if (before < a.beams) best[before] = BeamCandidate{from_order((uint32_t)(me >> 32)), (int32_t)~(uint32_t)me};
+            if (before == a.beams - 1) last_order = (uint32_t)(me >> 32);
+            if (before == a.beams) next = me;
         }
         if (tid >= n && tid < a.beams) best[tid] = BeamCandidate{-INFINITY, -1};
+        /* what is left out: of the list, or else below the bound, where there is anything below it */
+        const float rest = bound > -FLT_MAX ? logit_below<T>(bound) : -INFINITY;
+        if (n <= a.beams) {
+            if (tid == 0) record(rest);
+            return;
+        }
+        __syncthreads();
+        if (__ballot(next != 0) == 0) return;
+        /* the wave that has it; where it equals the last candidate, what comes behind those that do */
+        const uint32_t last = last_order;
+        uint32_t below = (uint32_t)(next >> 32);
+        if (__ballot(next != 0 && below == last)) {
+            for (int c = tid & 63; c < n; c += 64) {
+                const uint32_t o = (uint32_t)(list[c] >> 32);
+                if (o < last) atomicMax(&below_order, o);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            below = below_order;
+        }
+        if (next != 0) record(below != 0u ? from_order(below) : rest);
         return;
     }
     /* too many equal ones: one after the other */
@@ -250,16 +310,34 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_scan(BeamArgs a)
         if (tid == 0) best[k] = BeamCandidate{b.logit, b.logit == -INFINITY ? -1 : b.token};
         last = b;
     }
+    float below = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < BEAM_PER_THREAD; ++i)
+        if (v[i] < last.logit) below = fmaxf(below, v[i]);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) below = fmaxf(below, __shfl_xor(below, k));
+    __syncthreads();
+    if ((tid & 63) == 0) red[tid >> 6] = below;
+    __syncthreads();
+    if (tid == 0) record(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
 }
 
 struct BeamScored {
-    double score;
+    float score;
     int64_t place; /* (beam of the group, token + 1) */
 };
 
 __device__ __forceinline__ bool beam_before(const BeamScored &a, const BeamScored &b)
 {
     return a.score > b.score || (a.score == b.score && a.place < b.place);
+}
+
+__device__ __forceinline__ float beam_logit(const BeamArgs &a, int64_t row, int64_t token)
+{
+    const char *x = a.logits + row * a.row_bytes;
+    if (a.dtype == PARASON_DTYPE_F32) return reinterpret_cast<const float *>(x)[token];
+    const uint32_t h = reinterpret_cast<const uint16_t *>(x)[token];
+    return a.dtype == PARASON_DTYPE_BF16 ? bf16_to_f32(h) : f16_to_f32(h);
 }
 
 /* One block per group.  The chunks' candidates are lists, best first: a bound
@@ -271,31 +349,43 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
 {
     __shared__ float red[8];
     __shared__ float score[PARASON_BEAM_MAX];
-    __shared__ double norm[PARASON_BEAM_MAX]; /* score - ln of the sum; NaN: the row offers no tokens */
+    __shared__ float lse[PARASON_BEAM_MAX];
+    __shared__ float left_out[PARASON_BEAM_MAX]; /* no candidate that a list of the row lacks has a larger score but for equal logits */
     __shared__ int32_t offers[PARASON_BEAM_MAX];
     __shared__ BeamScored list[BEAM_LIST];
-    __shared__ int32_t n_list, n_live;
+    __shared__ BeamScored chosen[PARASON_BEAM_MAX];
+    __shared__ int32_t n_list, n_live, found[4];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row0 = (int64_t)blockIdx.x * a.beams;
+    const BeamScored none{-INFINITY, INT64_MAX};
     if (tid == 0) n_list = n_live = 0;
+    if (tid < PARASON_BEAM_MAX) chosen[tid] = none;
     __syncthreads();
+    /* a token's score: three float32 roundings, the same wherever it is worked out */
+    auto scored = [&](int b, float logit) { return score[b] + (logit - lse[b]); };
     for (int b0 = 0; b0 < a.beams; b0 += BEAM_THREADS / BEAM_ROW_LANES) {
         const int b = b0 + tid / BEAM_ROW_LANES, part = tid % BEAM_ROW_LANES;
         const bool there = b < a.beams;
         const int64_t row = row0 + (there ? b : 0);
         const float sc = a.scores[row];
         const int what = there ? beam_offers(a, row, sc) : BEAM_NONE;
-        float m = -INFINITY;
+        float m = -INFINITY, below = -INFINITY;
         double s = 0.0; /* an empty chunk has the maximum -inf and the sum 0 */
         if (what == BEAM_TOKENS) {
-            for (int c = part; c < a.chunks; c += BEAM_ROW_LANES) m = fmaxf(m, a.sums[row * a.chunks + c].x);
+            for (int c = part; c < a.chunks; c += BEAM_ROW_LANES) {
+                m = fmaxf(m, a.sums[row * a.chunks + c].top);
+                below = fmaxf(below, a.sums[row * a.chunks + c].below);
+            }
         }
 #pragma unroll
-        for (int k = BEAM_ROW_LANES / 2; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+        for (int k = BEAM_ROW_LANES / 2; k > 0; k >>= 1) {
+            m = fmaxf(m, __shfl_xor(m, k));
+            below = fmaxf(below, __shfl_xor(below, k));
+        }
         if (what == BEAM_TOKENS && m > -INFINITY) {
             for (int c = part; c < a.chunks; c += BEAM_ROW_LANES) {
-                const float2 q = a.sums[row * a.chunks + c];
-                s += (double)(q.y * __builtin_amdgcn_exp2f((q.x - m) * 1.44269504f));
+                const BeamChunk q = a.sums[row * a.chunks + c];
+                s += q.sum * exp((double)q.top - (double)m);
             }
         }
 #pragma unroll
@@ -304,7 +394,8 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
             /* NaN or +inf among the logits: s is NaN; nothing but -inf: no sum */
             const bool tokens = what == BEAM_TOKENS && m > -INFINITY && s < (double)INFINITY;
             score[b] = sc, offers[b] = tokens || what == BEAM_STAYS ? what : BEAM_NONE;
-            norm[b] = tokens ? (double)sc - ((double)m + log(s)) : (double)NAN;
+            lse[b] = tokens ? m + logf((float)s) : 0.0f;
+            left_out[b] = tokens ? scored(b, below) : -INFINITY;
             if (tokens) atomicAdd(&n_live, 1);
         }
     }
@@ -315,8 +406,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
     auto score_of = [&](uint32_t i, uint32_t k, const BeamCandidate &q) {
         const uint32_t b = div_by(i, a.chunks_div);
         const bool first = k == 0 && i == b * (uint32_t)a.chunks;
-        const double none = -(double)INFINITY;
-        return offers[b] == BEAM_TOKENS ? norm[b] + (double)q.logit : offers[b] == BEAM_STAYS && first ? (double)score[b] : none;
+        return offers[b] == BEAM_TOKENS ? scored((int)b, q.logit) : offers[b] == BEAM_STAYS && first ? score[b] : -INFINITY;
     };
     auto place_of = [&](uint32_t i, const BeamCandidate &q) {
         const uint32_t b = div_by(i, a.chunks_div);
@@ -333,10 +423,9 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
         const uint32_t i1 = i0 + BEAM_THREADS < entries ? i0 + BEAM_THREADS : i0;
         const BeamCandidate q0 = best[(int64_t)(i0 >> depth_log) * a.beams + (i0 & depth_mask)];
         const BeamCandidate q1 = best[(int64_t)(i1 >> depth_log) * a.beams + (i1 & depth_mask)];
-        mine = fmaxf(mine, (float)score_of(i0 >> depth_log, i0 & depth_mask, q0));
-        mine = fmaxf(mine, (float)score_of(i1 >> depth_log, i1 & depth_mask, q1));
+        mine = fmaxf(mine, score_of(i0 >> depth_log, i0 & depth_mask, q0));
+        mine = fmaxf(mine, score_of(i1 >> depth_log, i1 & depth_mask, q1));
     }
-    /* (a rounding to float keeps the order of two scores or makes them equal) */
     const float bound = block_bound(mine, a.beams, red);
     /* ---- what reaches it */
     for (uint32_t i = tid; i < lists; i += BEAM_THREADS) {
@@ -348,8 +437,8 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (!more) continue;
-                const double sc = score_of(i, (uint32_t)(k0 + j), q[j]);
-                more = k0 + j < a.beams && (float)sc >= bound;
+                const float sc = score_of(i, (uint32_t)(k0 + j), q[j]);
+                more = k0 + j < a.beams && sc >= bound;
                 if (!more) continue;
                 const int at = atomicAdd(&n_list, 1);
                 if (at < BEAM_LIST) list[at] = BeamScored{sc, place_of(i, q[j])};
@@ -358,55 +447,79 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_choose(BeamArgs a)
     }
     __syncthreads();
     const int n = n_list;
-    auto put = [&](int k, const BeamScored &s) {
-        const int64_t b = s.place / (a.vocab + 1);
-        a.new_scores[row0 + k] = (float)s.score;
-        a.parents[row0 + k] = (int32_t)(row0 + b);
-        a.tokens[row0 + k] = (int32_t)(s.place - b * (a.vocab + 1)) - 1;
-    };
-    auto put_none = [&](int k) {
-        a.new_scores[row0 + k] = -INFINITY;
-        a.parents[row0 + k] = (int32_t)(row0 + k);
-        a.tokens[row0 + k] = -1;
-    };
     if (n <= BEAM_LIST) {
         for (int i = tid; i < n; i += BEAM_THREADS) {
             const BeamScored me = list[i];
             int before = 0;
             for (int k = 0; k < n; ++k) before += beam_before(list[k], me);
-            if (before < a.beams) put(before, me);
+            if (before < a.beams) chosen[before] = me;
         }
-        if (tid >= n && tid < a.beams) put_none(tid);
-        return;
-    }
-    /* too many equal ones: one after the other */
-    const BeamScored none{-(double)INFINITY, INT64_MAX};
-    BeamScored last{(double)INFINITY, -1};
-    for (int k = 0; k < a.beams; ++k) {
-        BeamScored b = none;
-        for (uint32_t i = tid; i < lists; i += BEAM_THREADS)
-            for (int j = 0; j < a.beams; ++j) {
-                const BeamCandidate q = best[(int64_t)i * a.beams + j];
-                const BeamScored c{score_of(i, (uint32_t)j, q), place_of(i, q)};
-                if (c.score > -(double)INFINITY && beam_before(last, c) && beam_before(c, b)) b = c;
+    } else {
+        /* too many equal ones: one after the other */
+        BeamScored last{INFINITY, -1};
+        for (int k = 0; k < a.beams; ++k) {
+            BeamScored b = none;
+            for (uint32_t i = tid; i < lists; i += BEAM_THREADS)
+                for (int j = 0; j < a.beams; ++j) {
+                    const BeamCandidate q = best[(int64_t)i * a.beams + j];
+                    const BeamScored c{score_of(i, (uint32_t)j, q), place_of(i, q)};
+                    if (c.score > -INFINITY && beam_before(last, c) && beam_before(c, b)) b = c;
+                }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                const BeamScored q{__shfl_xor(b.score, o), (int64_t)__shfl_xor((long long)b.place, o)};
+                if (beam_before(q, b)) b = q;
             }
+            __syncthreads();
+            if (lane == 0) list[wave] = b;
+            __syncthreads();
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const BeamScored q{__shfl_xor(b.score, o), (int64_t)__shfl_xor((long long)b.place, o)};
-            if (beam_before(q, b)) b = q;
+            for (int w = 0; w < 4; ++w)
+                if (beam_before(list[w], b)) b = list[w];
+            if (tid == 0) chosen[k] = b;
+            last = b;
         }
-        __syncthreads();
-        if (lane == 0) list[wave] = b;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            if (beam_before(list[w], b)) b = list[w];
-        if (tid == 0) {
-            if (b.place == INT64_MAX) put_none(k);
-            else put(k, b);
-        }
-        last = b.place == INT64_MAX ? none : b;
     }
+    __syncthreads();
+    /* ---- the last score again, where a list may lack a lower token of it (the ones above it are all there: a list that
+     * lacks a candidate has `beams` that are no worse) */
+    const float cut = chosen[a.beams - 1].score;
+    if (__ballot(lane < a.beams && cut > -INFINITY && left_out[lane] >= cut)) { /* the same in every wave */
+        int have = __popcll(__ballot(lane < a.beams && chosen[lane].score > cut));
+        __syncthreads();
+        for (int b = 0; b < a.beams && have < a.beams; ++b) {
+            const int64_t row = row0 + b;
+            if (offers[b] == BEAM_STAYS && score[b] == cut) {
+                if (tid == 0) chosen[have] = BeamScored{cut, (int64_t)b * (a.vocab + 1)};
+                ++have;
+            }
+            if (offers[b] != BEAM_TOKENS) continue;
+            for (int c = 0; c < a.chunks && have < a.beams; ++c) {
+                if (scored(b, a.sums[row * a.chunks + c].top) < cut) continue;
+                const int64_t t0 = (int64_t)c * a.chunk_tokens;
+                const int64_t t1 = t0 + a.chunk_tokens < a.vocab ? t0 + a.chunk_tokens : a.vocab;
+                for (int64_t t = t0; t < t1 && have < a.beams; t += BEAM_THREADS) {
+                    const bool hit = t + tid < t1 && scored(b, beam_logit(a, row, t + tid)) == cut;
+                    const uint64_t hits = __ballot(hit);
+                    __syncthreads(); /* (the last round's counts have been read) */
+                    if (lane == 0) found[wave] = __popcll(hits);
+                    __syncthreads();
+                    int at = have + lanes_below(hits);
+                    for (int w = 0; w < wave; ++w) at += found[w];
+                    if (hit && at < a.beams) chosen[at] = BeamScored{cut, (int64_t)b * (a.vocab + 1) + t + tid + 1};
+                    have += found[0] + found[1] + found[2] + found[3];
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (tid >= a.beams) return;
+    const BeamScored r = chosen[tid];
+    const bool empty = r.place == INT64_MAX;
+    const int64_t b = empty ? tid : r.place / (a.vocab + 1);
+    a.new_scores[row0 + tid] = r.score;
+    a.parents[row0 + tid] = (int32_t)(row0 + b);
+    a.tokens[row0 + tid] = empty ? -1 : (int32_t)(r.place - b * (a.vocab + 1)) - 1;
 }
 
 /* ---- reordering ---- */
