@@ -513,7 +513,8 @@ typedef struct parason_kv_rows {
  * t * stride_token + h * stride_head + d, of type `dtype` (PARASON_DTYPE_F32,
  * _BF16 or _F16; a 16-bit cache takes its own type or F32), at any alignment
  * of the type.  Bad rows are not written, nor are positions whose page is bad.
- * Two tokens that fall on one slot leave either of them. */
+ * Two tokens that fall on one slot leave either of them.  A call takes fewer
+ * than 2^24 rows (PARASON_ERR_SIZE). */
 int parason_kv_write(const parason_kv_cache *cache, const parason_kv_rows *rows, const void *k, const void *v,
                      int32_t dtype, int64_t stride_token, int64_t stride_head, uint32_t *row_status, void *stream);
 
@@ -590,7 +591,8 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
  * parent the beam's own row. */
 #define PARASON_BEAM_MAX 64
 
-/* Bytes of device workspace parason_beam_select needs. */
+/* Bytes of device workspace parason_beam_select needs (PARASON_ERR_SIZE when
+ * the rows times the vocabulary's 8,192s are 2^24 or more). */
 int parason_beam_workspace_size(int64_t n_groups, int32_t beams, int64_t vocab, size_t *bytes);
 
 /* The selection, asynchronously on `stream`.  logits: row i at logits +
@@ -607,7 +609,8 @@ int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, i
  * row parents[i] of its src, byte for byte (decode states, token histories,
  * mask rows of the tree attention, page tables, ...).  A parent outside
  * [0, n_rows) leaves the row of dst as it is.  src and dst do not overlap; up
- * to PARASON_BEAM_ARRAYS arrays, in one launch, asynchronously on `stream`. */
+ * to PARASON_BEAM_ARRAYS arrays, in one launch, asynchronously on `stream`
+ * (PARASON_ERR_SIZE when the rows times their 16-KiB pieces are 2^24 or more). */
 #define PARASON_BEAM_ARRAYS 8
 typedef struct parason_beam_array {
     const void *src;

@@ -37,9 +37,9 @@ TreeKernel pick(int dim, int cols, bool f16, int kind)
 /* How a call is cut into blocks: by its sizes and bounds alone, so that the
  * workspace can be sized without a GPU. */
 struct TreePlan {
+    int32_t max_length; /* of the rows that can be good: their tokens are among the call's */
     int32_t cols, q_blocks, parts, part_len;
-    int64_t units, blocks;
-    bool by_xcd;
+    int64_t rows;       /* of a launch; one does for all that are not many times the device's */
     size_t ml, end; /* workspace: the parts' vectors at 0, their maxima and sums at ml */
 };
 
@@ -48,10 +48,12 @@ constexpr size_t PART_BYTES = (size_t)1 << 29;   /* of the parts' vectors */
 
 int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads, TreePlan *p)
 {
-    const int64_t group = n_q_heads / c->n_heads, cols = (int64_t)r->max_length * group;
-    if (cols > PARASON_KV_MAX_LEN) return PARASON_ERR_SIZE; /* (and blocks of columns end within 31 bits) */
+    const int64_t group = n_q_heads / c->n_heads;
+    if (r->max_length * group > PARASON_KV_MAX_LEN) return PARASON_ERR_SIZE; /* (and blocks of columns end within 31 bits) */
     /* more than 2^31 blocks of 128 columns; the products below keep within 63 bits otherwise */
     if ((double)r->n_rows * r->max_length * n_q_heads > 0x1p38) return PARASON_ERR_SIZE;
+    p->max_length = r->max_length < r->n_tokens ? r->max_length : (int32_t)r->n_tokens;
+    const int64_t cols = p->max_length * group;
     p->cols = cols <= 16 ? 16 : cols <= 64 ? 32 : 128;
     p->q_blocks = cols == 0 ? 1 : (int32_t)((cols + p->cols - 1) / p->cols);
     /* blocks that have columns: those of a row's own tokens, at most one of them not full */
@@ -71,15 +73,14 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
     int64_t parts = (r->max_kv_len + len - 1) / len;
     if (parts < 1 || base >= (p->cols < 128 ? 16 : 1) * PART_BLOCKS) parts = 1;
     if (per_part > 0 && (size_t)parts > PART_BYTES / per_part) parts = PART_BYTES / per_part > 1 ? (int64_t)(PART_BYTES / per_part) : 1;
-    if (r->n_rows * r->max_length * n_q_heads > INT32_MAX) parts = 1; /* tree_join's waves */
+    if (r->n_rows * p->max_length * n_q_heads > abi::MAX_BLOCKS * (pk::TREE_THREADS / 64)) parts = 1; /* tree_join's waves */
     len = (r->max_kv_len + parts - 1) / parts;
     p->part_len = (int32_t)((len + tile - 1) / tile * tile < INT32_MAX ? (len + tile - 1) / tile * tile : len);
     if (p->part_len < tile) p->part_len = (int32_t)tile;
     p->parts = (int32_t)parts;
-    p->units = r->n_rows * c->n_heads * parts;
-    p->by_xcd = p->q_blocks > 1 && p->units >= 8;
-    p->blocks = (p->by_xcd ? (p->units + 7) / 8 * 8 : p->units) * p->q_blocks;
-    if (p->blocks > INT32_MAX) return PARASON_ERR_SIZE;
+    /* (their units rounded up to a multiple of eight) */
+    p->rows = (abi::MAX_BLOCKS / p->q_blocks - 7) / (c->n_heads * parts);
+    if (p->rows < 1) return PARASON_ERR_SIZE;
     p->ml = parts > 1 ? abi::align_up(per_part * parts) : 0;
     p->end = parts > 1 ? p->ml + abi::align_up((size_t)r->n_tokens * n_q_heads * 8 * parts) : abi::ALIGN;
     return PARASON_OK;
@@ -151,15 +152,28 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
     a.negate = args->scale < 0.0f;
     const float c2 = (float)(std::fabs((double)args->scale) * 1.4426950408889634);
     a.c2 = c2 > 0x1p-126f ? c2 : 0x1p-126f;
-    a.q_blocks = p.q_blocks, a.parts = p.parts, a.part_len = p.part_len, a.units = p.units, a.by_xcd = p.by_xcd;
+    a.q_blocks = p.q_blocks, a.parts = p.parts, a.part_len = p.part_len;
+    a.r.max_length = p.max_length;
     a.part_out = (float *)workspace;
     a.part_ml = (float2 *)((char *)workspace + p.ml);
     const bool f16 = args->dtype == PARASON_DTYPE_F16;
     hipStream_t stream = (hipStream_t)stream_ptr;
-    hipLaunchKernelGGL(pick(cache->head_dim, p.cols, f16, kind), dim3((unsigned)p.blocks), dim3(pk::TREE_THREADS), 0, stream, a);
+    const TreeKernel f = pick(cache->head_dim, p.cols, f16, kind);
+    for (int64_t i = 0; i < rows->n_rows; i += p.rows) {
+        pk::TreeArgs b = a;
+        b.r.n_rows = rows->n_rows - i < p.rows ? rows->n_rows - i : p.rows;
+        b.r.starts += i, b.r.lengths += i, b.r.kv_lens += i;
+        if (b.r.pages) b.r.pages += i * b.r.pages_stride;
+        if (b.r.status) b.r.status += i;
+        if (b.tree_lens) b.tree_lens += i;
+        b.units = b.r.n_rows * cache->n_heads * p.parts;
+        b.by_xcd = p.q_blocks > 1 && b.units >= 8;
+        const int64_t blocks = (b.by_xcd ? (b.units + 7) / 8 * 8 : b.units) * p.q_blocks;
+        hipLaunchKernelGGL(f, dim3((unsigned)blocks), dim3(pk::TREE_THREADS), 0, stream, b);
+    }
     if (p.parts > 1) {
         constexpr int64_t per_block = pk::TREE_THREADS / 64;
-        const int64_t waves = rows->n_rows * rows->max_length * heads;
+        const int64_t waves = rows->n_rows * p.max_length * heads;
         hipLaunchKernelGGL(f16 ? pk::tree_join<true> : pk::tree_join<false>, dim3((unsigned)((waves + per_block - 1) / per_block)),
                            dim3(pk::TREE_THREADS), 0, stream, a, p.cols);
     }

@@ -21,7 +21,7 @@ int layout_for(int64_t n_groups, int32_t beams, int64_t vocab, BeamLayout *L)
         return PARASON_ERR_SIZE;
     L->chunks = (vocab + pk::BEAM_CHUNK - 1) / pk::BEAM_CHUNK;
     const int64_t rows = n_groups * beams;
-    if (rows > INT32_MAX / L->chunks) return PARASON_ERR_SIZE;
+    if (rows > abi::MAX_BLOCKS / L->chunks) return PARASON_ERR_SIZE;
     L->best = abi::align_up((size_t)(rows * L->chunks) * sizeof(pk::BeamChunk));
     L->end = L->best + abi::align_up((size_t)(rows * L->chunks) * beams * sizeof(pk::BeamCandidate) + 1);
     return PARASON_OK;
@@ -80,7 +80,7 @@ int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, i
 int parason_beam_reorder(const int32_t *parents, int64_t n_rows, const parason_beam_array *arrays, int32_t n_arrays,
                          void *stream_ptr)
 {
-    if (n_rows < 0 || n_rows > INT32_MAX || n_arrays < 0 || n_arrays > PARASON_BEAM_ARRAYS) return PARASON_ERR_SIZE;
+    if (n_rows < 0 || n_rows > abi::MAX_BLOCKS || n_arrays < 0 || n_arrays > PARASON_BEAM_ARRAYS) return PARASON_ERR_SIZE;
     if (n_rows == 0 || n_arrays == 0) return PARASON_OK;
     if (!parents || !arrays) return PARASON_ERR_NULL;
     pk::ReorderArgs a;
@@ -103,7 +103,7 @@ int parason_beam_reorder(const int32_t *parents, int64_t n_rows, const parason_b
             a.first_block[a.n_arrays] = (int32_t)blocks;
             a.arrays[a.n_arrays++] = x;
             if (!small) blocks += (x.row_bytes + pk::REORDER_SEGMENT - 1) / pk::REORDER_SEGMENT;
-            if (blocks > INT32_MAX / n_rows) return PARASON_ERR_SIZE;
+            if (blocks > abi::MAX_BLOCKS / n_rows) return PARASON_ERR_SIZE;
         }
     }
     if (!aligned(parents, 4)) return PARASON_ERR_ALIGN;

@@ -54,7 +54,7 @@ int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void 
     const int64_t elem = dtype == PARASON_DTYPE_F32 ? 4 : 2;
     /* units of a row (token, k or v, head) are counted in 31 bits */
     const int64_t units = (int64_t)rows->max_length * 2 * cache->n_heads;
-    if (units > INT32_MAX) return PARASON_ERR_SIZE;
+    if (units > INT32_MAX || rows->n_rows > abi::MAX_BLOCKS) return PARASON_ERR_SIZE;
     if (rows->n_rows == 0 || rows->n_tokens == 0 || rows->max_length == 0) return PARASON_OK;
     if (!k || !v) return PARASON_ERR_NULL;
     if (!aligned(k, elem) || !aligned(v, elem)) return PARASON_ERR_ALIGN;
@@ -68,10 +68,9 @@ int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void 
     a.heads_div = pk::fast_div((uint32_t)cache->n_heads);
     const int64_t per_block = pk::KV_THREADS / a.group * (write ? pk::KV_WRITES : pk::KV_READS);
     int64_t blocks = (units + per_block - 1) / per_block, most = MOVE_BLOCKS / rows->n_rows;
-    if (most < 1) most = 1;
+    if (most < 1) most = 1; /* (as many blocks as rows) */
     if (blocks > most) blocks = most;
     a.blocks_per_row = (int32_t)blocks;
-    if (rows->n_rows > INT32_MAX / blocks) return PARASON_ERR_SIZE;
     const MoveKernel f = write ? pick<Write>(dtype, kind) : pick<Read>(dtype, kind);
     hipLaunchKernelGGL(f, dim3((unsigned)(rows->n_rows * blocks)), dim3(pk::KV_THREADS), 0, (hipStream_t)stream_ptr, a);
     return hipGetLastError() == hipSuccess ? PARASON_OK : PARASON_ERR_HIP;

@@ -10,6 +10,9 @@ namespace abi {
 
 constexpr int64_t MAX_ELEMS = (int64_t)1 << 56; /* no product of a stride and an index overflows below this */
 
+/* Blocks of 256 threads that a launch takes: a grid of 2^32 threads or more is refused or, worse, cut to 32 bits. */
+constexpr int64_t MAX_BLOCKS = 0xFFFFFFFFll / 256;
+
 inline bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 /* |stride| * count stays within MAX_ELEMS */
