@@ -182,7 +182,7 @@ struct TreeShape {
     static constexpr int OS = DP + 4;                 /* floats of a row of the waves' results when they are joined */
     static constexpr int JOIN = (WK - 1) * COLS * OS * 4;
     /* blocks that a CU holds: by LDS, or by registers */
-    static constexpr int BLOCKS = DP > 128 ? (COLS == 16 && RAW ? 2 : 1) : COLS > 16 ? 2 : RAW ? (DP <= 64 ? 4 : 3) : DP <= 64 ? 3 : 2;
+    static constexpr int BLOCKS = DP > 128 ? (COLS == 16 && RAW ? 2 : 1) : COLS > 16 ? (DP <= 64 && COLS == 32 ? 3 : 2) : RAW ? (DP <= 64 ? 4 : 3) : DP <= 64 ? 3 : 2;
     static constexpr int TILE = KBYTES + VBYTES > JOIN ? KBYTES + VBYTES : JOIN;
 };
 
@@ -566,7 +566,13 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             for (int r = 0; r < NV; ++r) top = fmaxf(top, s[u][r]);
 #pragma unroll
         for (int k = CN; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
-        const float at_new = fmaxf(at, top * a.c2 - LIFT);
+        /* Exponents beyond FAR are rounded by more than a weight bears (the largest would be 2^(LIFT + 1) or, further on,
+         * infinite or nothing): they are rounded down, and the weights that this takes over 2^LIFT are 2^LIFT, which
+         * makes equal what the scores' own rounding does not tell apart for certain. */
+        constexpr float FAR = 0x1p22f;
+        float want = top * a.c2 - LIFT;
+        want -= fabsf(want) >= FAR ? fminf(fabsf(want), 0x1p127f) * 0x1p-23f : 0.0f;
+        const float at_new = fmaxf(at, want);
         const float ref = at_new == -INFINITY ? 0.0f : at_new;
         if (__ballot(at_new > at)) {
             const float corr = __builtin_amdgcn_exp2f(at - ref);
@@ -581,6 +587,13 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
             for (int r = 0; r < NV; ++r) s[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c2, -ref));
+        if (__ballot(fabsf(ref) >= FAR * (1.0f - 0x1p-20f))) {
+            const float most = fabsf(ref) >= FAR * (1.0f - 0x1p-20f) ? (float)(1 << LIFT) : INFINITY;
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int r = 0; r < NV; ++r) s[u][r] = s[u][r] > most ? most : s[u][r]; /* (NaN stays) */
+        }
         float l4[4] = {};
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
