@@ -861,8 +861,10 @@ def tree_attention(q, cache: KVCache, rows: KVRows, mask=None, tree_lens=None, s
         raise TypeError("tree_lens must be a contiguous int32 device tensor of one entry per row")
     if workspace is None:
         workspace = T.empty(_tree_workspace(ca, ra, q_heads), dtype=T.u8, device=q.device)
+    # (an empty mask has no address, but is one: any address stands for its words, of which none is read)
+    mask_ptr = None if mask is None else mask.data_ptr() or workspace.data_ptr()
     ta = TreeArgs(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q_st[0], q_st[1],
-                  out_st[0], out_st[1], mask.data_ptr() if mask is not None else None, stride,
+                  out_st[0], out_st[1], mask_ptr, stride,
                   tree_lens.data_ptr() if tree_lens is not None else None, words, q_heads, code,
                   dim ** -0.5 if scale is None else float(scale))
     rc = (_lib or lib()).parason_tree_attention(ca, ra, ta, _status_ptr(T, status, ra.n_rows), workspace.data_ptr(),
