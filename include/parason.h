@@ -58,7 +58,8 @@ extern "C" {
 #define PARASON_ERR_GROUP (-3)     /* group_size < 1 or n_traj % group_size != 0 */
 #define PARASON_ERR_WORKSPACE (-4) /* workspace smaller than the call's workspace size */
 #define PARASON_ERR_TAGS (-5)      /* a tag id is negative or two tag ids are equal */
-#define PARASON_ERR_PARAM (-6)     /* a parameter is not finite, or a type or flag is not one that the call takes */
+#define PARASON_ERR_PARAM (-6)     /* a parameter is not finite, a type or flag is not one that the call takes, or a
+                                      result lies over what the call reads */
 #define PARASON_ERR_ALIGN (-7)     /* a pointer or stride not aligned as the call needs (workspace: 256 bytes) */
 #define PARASON_ERR_HIP (-8)       /* a HIP call or kernel launch failed */
 #define PARASON_ERR_DEVICE (-9)    /* the current device is not gfx950 or cannot be queried (checked by
@@ -608,9 +609,11 @@ int parason_beam_select(const void *logits, int64_t vocab, int64_t row_stride, i
 /* What belongs to a beam, in the new order: row i of every array's dst becomes
  * row parents[i] of its src, byte for byte (decode states, token histories,
  * mask rows of the tree attention, page tables, ...).  A parent outside
- * [0, n_rows) leaves the row of dst as it is.  src and dst do not overlap; up
- * to PARASON_BEAM_ARRAYS arrays, in one launch, asynchronously on `stream`
- * (PARASON_ERR_SIZE when the rows times their 16-KiB pieces are 2^24 or more). */
+ * [0, n_rows) leaves the row of dst as it is.  No row of a dst shares memory
+ * with a row of any src, of another dst, or with parents (PARASON_ERR_PARAM; the
+ * gaps between rows may hold each other's rows).  Up to PARASON_BEAM_ARRAYS
+ * arrays, in one launch, asynchronously on `stream` (PARASON_ERR_SIZE when the
+ * rows times their 16-KiB pieces are 2^24 or more). */
 #define PARASON_BEAM_ARRAYS 8
 typedef struct parason_beam_array {
     const void *src;

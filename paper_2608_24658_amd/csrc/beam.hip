@@ -27,6 +27,29 @@ int layout_for(int64_t n_groups, int32_t beams, int64_t vocab, BeamLayout *L)
     return PARASON_OK;
 }
 
+struct Rows {
+    const char *p;
+    int64_t bytes, stride; /* 0 < bytes <= stride */
+};
+
+/* Whether any of n rows here and n rows there share a byte. */
+bool rows_meet(const Rows &a, const Rows &b, int64_t n)
+{
+    const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p); /* rows of b from the first byte of a on */
+    if (d >= (n - 1) * a.stride + a.bytes || -d >= (n - 1) * b.stride + b.bytes) return false;
+    if (a.stride == b.stride) { /* as far behind a row of a, or between two, as all of them */
+        const int64_t in = (d % a.stride + a.stride) % a.stride;
+        return in < a.bytes || in + b.bytes > a.stride;
+    }
+    for (int64_t i = 0, j = 0; i < n && j < n;) {
+        const int64_t x = i * a.stride, y = d + j * b.stride;
+        if (x + a.bytes <= y) i += (y - x - a.bytes) / a.stride + 1;      /* the first that ends behind y */
+        else if (y + b.bytes <= x) j += (x - y - b.bytes) / b.stride + 1;
+        else return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -108,6 +131,17 @@ int parason_beam_reorder(const int32_t *parents, int64_t n_rows, const parason_b
     }
     if (!aligned(parents, 4)) return PARASON_ERR_ALIGN;
     if (a.n_arrays == 0) return PARASON_OK;
+    for (int k = 0; k < a.n_arrays; ++k) { /* rows are written while others are read */
+        const parason_beam_array &x = a.arrays[k];
+        const Rows dst{(const char *)x.dst, x.row_bytes, x.dst_stride};
+        if (rows_meet(dst, Rows{(const char *)parents, 4, 4}, n_rows)) return PARASON_ERR_PARAM;
+        for (int m = 0; m < a.n_arrays; ++m) {
+            const parason_beam_array &y = a.arrays[m];
+            if (rows_meet(dst, Rows{(const char *)y.src, y.row_bytes, y.src_stride}, n_rows) ||
+                (m < k && rows_meet(dst, Rows{(const char *)y.dst, y.row_bytes, y.dst_stride}, n_rows)))
+                return PARASON_ERR_PARAM;
+        }
+    }
     if (cu_count() <= 0) return PARASON_ERR_DEVICE;
     a.blocks_per_row = (int32_t)blocks;
     hipLaunchKernelGGL(pk::beam_reorder, dim3((unsigned)(n_rows * blocks)), dim3(pk::REORDER_THREADS), 0, (hipStream_t)stream_ptr, a);

@@ -273,7 +273,7 @@ const char *parason_strerror(int status)
     case PARASON_ERR_GROUP: return "group_size < 1 or n_traj is not a multiple of group_size";
     case PARASON_ERR_WORKSPACE: return "workspace smaller than the call's workspace size";
     case PARASON_ERR_TAGS: return "tag ids must be distinct and non-negative";
-    case PARASON_ERR_PARAM: return "a parameter is not finite, or a type or flag is not one that the call takes";
+    case PARASON_ERR_PARAM: return "a parameter is not finite, a type or flag is not one that the call takes, or a result lies over what the call reads";
     case PARASON_ERR_ALIGN: return "a pointer or stride is not aligned as the call needs (the workspace: 256 bytes)";
     case PARASON_ERR_HIP: return "a HIP call or kernel launch failed";
     case PARASON_ERR_DEVICE: return "the current HIP device is not a gfx950 GPU or cannot be queried";

@@ -927,7 +927,8 @@ def beam_reorder(parent, arrays, out=None) -> list:
     """What belongs to the beams, in their new order: row i of every result is
     row parent[i] of the array (asynchronous on the current stream).  arrays: up
     to BEAM_ARRAYS device tensors, each [rows, ...] with contiguous rows, or a
-    flat one of rows equal parts; out: tensors to write into, other than these."""
+    flat one of rows equal parts; out: tensors to write into, none of whose rows
+    lies over these, another's or parent."""
     T = _types()
     rows, n = parent.numel(), len(arrays)
     if parent.dtype is not T.i32 or not parent.is_contiguous() or not parent.is_cuda:

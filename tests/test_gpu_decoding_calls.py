@@ -45,3 +45,24 @@ def test_masks_without_words(dev):
     # no tokens at all, with a mask and trees
     rows = rows._replace(lengths=zero, starts=torch.zeros(2, dtype=torch.int64, device=dev), max_length=0)
     assert PX.tree_attention(q[:0], cache, rows, mask=word[:0], tree_lens=zero).shape == (0, 4, 64)
+
+
+def test_results_over_their_sources(dev):
+    """Rows that would be written while others are still read: refused; rows beside each other in one tensor: moved."""
+    log("case reorder in place")
+    parent = torch.tensor([2, 2, 0, 1, 3], dtype=torch.int32, device=dev)
+    both = torch.arange(5 * 2 * 24, dtype=torch.int32, device=dev).view(5, 2, 24)
+    other = torch.zeros(5, 24, dtype=torch.int32, device=dev)
+    a, b = both[:, 0], both[:, 1]
+    for src, dst in (([a], [a]), ([other], [other]), ([a, other], [other, b]), ([b[:, :20]], [b[:, 4:]]),
+                     ([other.view(-1)], [other.view(-1)]), ([other[:, :8]], [other[:, 7:15]])):
+        with pytest.raises((PX.ParasonError, ValueError)):
+            PX.beam_reorder(parent, src, out=dst)
+    with pytest.raises((PX.ParasonError, ValueError)):
+        PX.beam_reorder(parent, [torch.zeros(5, dtype=torch.int32, device=dev)], out=[parent])
+    want = a[parent.long()].clone()
+    PX.beam_reorder(parent, [a], out=[b])
+    assert torch.equal(b, want)
+    want = other[:, :8][parent.long()].clone()
+    PX.beam_reorder(parent, [other[:, :8]], out=[other[:, 8:16]])
+    assert torch.equal(other[:, 8:16], want)
