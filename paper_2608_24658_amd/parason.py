@@ -695,12 +695,19 @@ class _Types:
         cls.i32, cls.i64, cls.f32, cls.u8 = torch.int32, torch.int64, torch.float32, torch.uint8
         cls.floats = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
         cls.kv = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_FP8, torch.int8: DTYPE_INT8}
-        cls.empty, cls.torch = torch.empty, torch
+        cls.empty, cls.grad_enabled, cls.torch = torch.empty, torch.is_grad_enabled, torch
         return cls
 
 
 def _types():
     return _Types if _Types.torch is not None else _Types.load()
+
+
+def _refuse_gradients(T):
+    """For inputs that require one: these operators have no backward pass, so a result would silently have none."""
+    if T.grad_enabled():
+        raise RuntimeError("no gradient flows through the cache and the attention over it: detach the inputs, or call under "
+                           "torch.no_grad()")
 
 
 def _cache_args(T, cache: KVCache) -> KvCacheArgs:
@@ -709,6 +716,8 @@ def _cache_args(T, cache: KVCache) -> KvCacheArgs:
     if code is None or v.dtype is not k.dtype or k.dim() != 4 or not (k.is_cuda and v.is_cuda):
         raise TypeError("k and v must be [pages, page_size, heads, head_dim] bfloat16/float16/float8_e4m3fn/int8 "
                         "device tensors of one type")
+    if k.requires_grad or v.requires_grad:
+        _refuse_gradients(T)
     shape, st = k.shape, k.stride()
     pages, size, heads, dim = shape
     if v.shape != shape or v.stride() != st or (st[3] != 1 and dim > 1):
@@ -827,11 +836,16 @@ def tree_attention(q, cache: KVCache, rows: KVRows, mask=None, tree_lens=None, s
     scale   of the scores (default head_dim ** -0.5)
     lse     True (or a float32 [tokens, q_heads] tensor): also the logarithm of
             each token's and head's sum of exponentials
+
+    There is no backward pass: a q or a cache that requires a gradient is refused
+    while autograd is on.
     """
     T = _types()
     code = T.floats.get(q.dtype)
     if code is None or code == DTYPE_F32 or q.dim() != 3 or not q.is_cuda:
         raise TypeError("q must be a [tokens, q_heads, head_dim] bfloat16/float16 device tensor, unit stride along a head")
+    if q.requires_grad or (out is not None and out.requires_grad):
+        _refuse_gradients(T)
     n_tokens, q_heads, dim = shape = q.shape
     q_st = q.stride()
     if q_st[2] != 1 and dim > 1:

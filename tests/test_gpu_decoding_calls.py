@@ -66,3 +66,26 @@ def test_results_over_their_sources(dev):
     want = other[:, :8][parent.long()].clone()
     PX.beam_reorder(parent, [other[:, :8]], out=[other[:, 8:16]])
     assert torch.equal(other[:, 8:16], want)
+
+
+def test_tensors_that_want_gradients(dev):
+    """The attention has no backward pass: queries and caches that want a gradient are refused, but not where autograd is
+    off.  What goes into a cache leaves the graph."""
+    log("case gradients")
+    cache, rows, q = two_rows(dev)
+    wants = q.detach().clone().requires_grad_()
+    k = torch.randn(6, 2, 64, device=dev, dtype=torch.bfloat16, requires_grad=True)
+    live = PX.KVCache(cache.k.detach().clone().requires_grad_(), cache.v)
+    calls = [lambda: PX.tree_attention(wants, cache, rows), lambda: PX.tree_attention(q, live, rows),
+             lambda: PX.kv_read(live, rows, 6, torch.float32)]
+    PX.kv_write(k, k, cache, rows)
+    for f in calls:
+        with pytest.raises(RuntimeError):
+            f()
+    with torch.no_grad():
+        for f in calls:
+            f()
+        want = PX.tree_attention(q, cache, rows)
+        assert torch.equal(PX.tree_attention(wants, cache, rows), want)
+    with torch.inference_mode():
+        assert torch.equal(PX.tree_attention(wants, cache, rows), want)
