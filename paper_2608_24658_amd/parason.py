@@ -754,6 +754,11 @@ def _rows_args(T, rows: KVRows, n_tokens: int) -> KvRowsArgs:
                       max_pages, int(max_length), int(max_kv_len))
 
 
+def _check_workspace(T, workspace):
+    if workspace.dtype is not T.u8 or not workspace.is_contiguous() or not workspace.is_cuda:
+        raise TypeError("workspace must be a contiguous uint8 device tensor")
+
+
 def _status_ptr(T, status, n):
     if status is None:
         return None
@@ -875,6 +880,8 @@ def tree_attention(q, cache: KVCache, rows: KVRows, mask=None, tree_lens=None, s
         raise TypeError("tree_lens must be a contiguous int32 device tensor of one entry per row")
     if workspace is None:
         workspace = T.empty(_tree_workspace(ca, ra, q_heads), dtype=T.u8, device=q.device)
+    else:
+        _check_workspace(T, workspace)
     # (an empty mask has no address, but is one: any address stands for its words, of which none is read)
     mask_ptr = None if mask is None else mask.data_ptr() or workspace.data_ptr()
     ta = TreeArgs(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q_st[0], q_st[1],
@@ -926,6 +933,8 @@ def beam_select(logits, scores, beams: int, states=None, workspace=None) -> dict
     dev = logits.device
     if workspace is None:
         workspace = T.empty(beam_workspace_size(rows // beams, beams, vocab), dtype=T.u8, device=dev)
+    else:
+        _check_workspace(T, workspace)
     score = scores.new_empty(rows)
     parent, token = T.empty((2, rows), dtype=T.i32, device=dev).unbind()
     rc = (_lib or lib()).parason_beam_select(

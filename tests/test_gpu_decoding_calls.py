@@ -89,3 +89,19 @@ def test_tensors_that_want_gradients(dev):
         assert torch.equal(PX.tree_attention(wants, cache, rows), want)
     with torch.inference_mode():
         assert torch.equal(PX.tree_attention(wants, cache, rows), want)
+
+
+def test_workspaces_that_are_none(dev):
+    """A workspace that is not bytes of the device, one after the other, or too few of them."""
+    log("case workspaces")
+    cache, rows, q = two_rows(dev)
+    logits, scores = torch.randn(4, 50, device=dev), torch.zeros(4, device=dev)
+    for call, size in ((lambda w: PX.tree_attention(q, cache, rows, workspace=w), PX.tree_attention_workspace_size(cache, rows, 6, 4)),
+                       (lambda w: PX.beam_select(logits, scores, 2, workspace=w), PX.beam_workspace_size(2, 2, 50))):
+        for w in (torch.empty(size, dtype=torch.uint8), torch.empty(size, device=dev),
+                  torch.empty(2 * size, dtype=torch.uint8, device=dev)[::2]):
+            with pytest.raises(TypeError):
+                call(w)
+        with pytest.raises(PX.ParasonError):
+            call(torch.empty(size - 1, dtype=torch.uint8, device=dev))
+        call(torch.empty(size, dtype=torch.uint8, device=dev))
