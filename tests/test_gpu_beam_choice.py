@@ -133,3 +133,35 @@ def test_more_equal_candidates_than_a_list_holds(dev, dtype, groups, beams, voca
     lses[b] = -PX.beam_select(x[b: b + 1].to(dev), torch.zeros(1, device=dev), 1)["score"].cpu().numpy()[0] + 1
     assert abs(float(lses[b]) - 1 - np.log(3)) <= 2 * float(np.spacing(np.float32(2)))
     same(select(dev, x, scores, beams, flags, lse=lses))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("beams,vocab,small", [(1, 400, 2.0 ** -20), (6, 9000, 2.0 ** -20), (6, 9000, 2.0 ** -14), (32, 20001, 2.0 ** -12)])
+def test_logits_around_zero(dev, dtype, beams, vocab, small):  # noqa: F811
+    """A token far above the rest, whose logits are near zero with either sign, zeros of either sign and the smallest
+    floats of the type among them: what is left of them behind 200 is rounded to a step of 2^-16."""
+    log("case logits around zero %s beams %d vocab %d" % (dtype, beams, vocab))
+    rng = np.random.default_rng(vocab + beams)
+    rows = 3 * beams
+    x = small * rng.standard_normal((rows, vocab))
+    x = np.where(rng.random((rows, vocab)) < 0.2, np.where(rng.random((rows, vocab)) < 0.5, 0.0, -0.0), x)
+    t = torch.as_tensor(x.astype(np.float32)).to(TYPES[dtype])
+    t[:, vocab // 2] = 200.0
+    scores = np.full(rows, -np.inf, np.float32)
+    scores[::beams] = [-1.0, -300.0, 0.0]
+    same(select(dev, t, scores, beams))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("beams,vocab", [(1, 5), (4, 700), (8, 20001)])
+def test_masks_of_the_lowest_value(dev, dtype, beams, vocab):  # noqa: F811
+    """Forbidden tokens at the type's lowest finite value instead of -inf: candidates like others, behind all the rest."""
+    log("case lowest values %s beams %d vocab %d" % (dtype, beams, vocab))
+    rng = np.random.default_rng(vocab)
+    rows = 4 * beams
+    t = torch.full((rows, vocab), torch.finfo(TYPES[dtype]).min, dtype=TYPES[dtype])
+    t[torch.arange(rows), torch.as_tensor(rng.integers(0, vocab, rows))] = 3.0
+    scores = np.full(rows, -np.inf, np.float32)
+    for g in range(4):
+        scores[g * beams: g * beams + max(1, beams // 4 * g)] = -2.0 - 0.5 * np.arange(max(1, beams // 4 * g))
+    same(select(dev, t, scores, beams))
