@@ -514,7 +514,7 @@ typedef struct parason_kv_rows {
  * t * stride_token + h * stride_head + d, of type `dtype` (PARASON_DTYPE_F32,
  * _BF16 or _F16; a 16-bit cache takes its own type or F32), at any alignment
  * of the type.  Bad rows are not written, nor are positions whose page is bad.
- * Two tokens that fall on one slot leave either of them.  A call takes fewer
+ * Two tokens that fall on one slot leave a mixture of both.  A call takes fewer
  * than 2^24 rows (PARASON_ERR_SIZE). */
 int parason_kv_write(const parason_kv_cache *cache, const parason_kv_rows *rows, const void *k, const void *v,
                      int32_t dtype, int64_t stride_token, int64_t stride_head, uint32_t *row_status, void *stream);
@@ -542,9 +542,11 @@ int parason_kv_read(const parason_kv_cache *cache, const parason_kv_rows *rows, 
  * holds.  Scores, maxima, sums and the accumulation are float32; for the matrix
  * product with v the weights exp(s_p - max), an 8-bit cache's scales of v
  * among them, are rounded to 16 bits (float16 over an F16 cache, else bfloat16;
- * F16 results over an 8-bit cache: to two bfloat16 terms).  Bad rows get NaN (nothing, where starts[i] and lengths[i] themselves
- * are bad), and so do tokens that see a position on a bad page (others of their
- * row may). */
+ * F16 results over an 8-bit cache: to two bfloat16 terms).  Weights below 2^-39
+ * of a token's largest are nothing over an F16 cache: an infinity of v behind
+ * such a weight gives NaN.  Bad rows get NaN (nothing, where starts[i] and
+ * lengths[i] themselves are bad), and so do tokens that see a position on a bad
+ * page (others of their row may). */
 typedef struct parason_tree_args {
     const void *q;            /* value d of head h of token t: element t * q_stride_token + h * q_stride_head + d */
     void *out;                /* the same with its own strides */

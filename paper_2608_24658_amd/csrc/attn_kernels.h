@@ -15,13 +15,13 @@
  * Two shapes.  Few queries (blocks of 16 or 32 columns: single tokens, beams,
  * short drafts): the four waves take a quarter of each tile's positions each and
  * are joined at the end; what bounds it is reading the cache once.  128 single
- * tokens over 1.0 M positions of 8 heads of 128 FP8 values, 2.19 GB, take 435 us
- * (5.0 TB/s); 16 over 55,000 bfloat16 ones, 0.23 GB, 57 us (4.0 TB/s).
+ * tokens over 1.0 M positions of 8 heads of 128 FP8 values, 2.19 GB, take 436 us
+ * (5.0 TB/s); 16 over 55,000 bfloat16 ones, 0.23 GB, 61 us (3.8 TB/s).
  * More queries: the waves take 32 columns each and share the tile; bound by the
  * products and the exponentials beside them.  A prompt of 8,192 tokens, 32
- * query heads over 8 of 128 values, 550 Gflop, takes 635 us (866 Tflop/s, where
+ * query heads over 8 of 128 values, 550 Gflop, takes 632 us (871 Tflop/s, where
  * a library product of 8192^3 reaches 1,348).  Long rows are cut into parts,
- * whose results tree_join puts together.
+ * whose results tree_join puts together.  (Times of whole calls, among others.)
  */
 #pragma once
 #include "kv_common.h"
@@ -141,7 +141,7 @@ __device__ __forceinline__ uint32_t finite_word(uint32_t w)
     return w & (((w & e) != e ? 0x0000FFFFu : 0u) | (((w >> 16) & e) != e ? 0xFFFF0000u : 0u));
 }
 
-/* A value of the cache, and whether it is an infinity or NaN. */
+/* A value of the cache. */
 template <int KIND>
 __device__ __forceinline__ float cached_value(const char *p)
 {
@@ -223,7 +223,11 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     typedef typename Acc<CN>::type acc;
     constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
     constexpr bool CODES = Sh::CODES, RAW = Sh::RAW;
-    constexpr bool PF16 = KIND == KV_F16;   /* type of the weights and of V: bfloat16 for codes, whose scales are in the weights */
+    /* Type of the weights and of V: bfloat16 for codes, whose scales are in the weights.  The weights are rounded to it for
+     * the matrix product: 2^-9 of each, against which a result of the same type is rounded by as much once more (bfloat16
+     * results are off by 0.0020 to 0.0024 of their size in all, and by 0.0017 with float32 weights).  Two terms would take
+     * half as many products again where products are what bounds the call. */
+    constexpr bool PF16 = KIND == KV_F16;
     /* float16 results over codes: the weights go in as two bfloat16 terms, so that they are not the coarsest step of
      * the whole.  (float16 weights would lose all precision where the positions with nearly all of the weight hold a
      * code of zero.) */

@@ -12,8 +12,9 @@
  * the score of that one is still among the best, the tokens of the last score
  * are taken from the logits again, in their order.  Bound by the
  * read: 2,048 rows of 50,257 float16 logits and their reordering, 409 MB in
- * all, take 112 us, the scan 67 of them; 256 rows of 151,936 float32 logits 43
- * us.  The beams of one prompt are three launches, 18 us, and the host's checks.
+ * all, take 117 us, the scan 70 of them; 256 rows of 151,936 float32 logits 46
+ * us.  The beams of one prompt are three launches, 17 us, and the host's checks,
+ * 27 in all.
  *
  * The largest of many, by a bound from below: of the threads' own maxima each
  * wave finds the k-th largest, k a quarter of the beams, by counting lanes bit
@@ -143,7 +144,7 @@ __device__ __forceinline__ int lanes_below(uint64_t mask)
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
-/* Six waves a SIMD: with the registers of five 77 us instead of 68 for 2,048 rows of 50,257 float16 logits. */
+/* Six waves a SIMD: with the registers of five 77 us against 68 for 2,048 rows of 50,257 float16 logits, traced in turn. */
 template <int T>
 __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_scan(BeamArgs a)
 {

@@ -6,10 +6,10 @@
  * magnitude before its first code, which the group finds by exchanges among
  * its lanes, so the values stay in registers between the two.  Bound by memory:
  * 165,000 positions of 8 heads of 128 values from FP8 pages of 24 slots to
- * bfloat16, 1.13 GB in all, take 255 us (4.4 TB/s, where a copy reaches 4.75);
- * 28,000 float16 tokens of 8 heads of 64 values to INT8 and back 43 us, two
+ * bfloat16, 1.13 GB in all, take 256 us (4.4 TB/s, where a copy reaches 4.75);
+ * 28,000 float16 tokens of 8 heads of 64 values to INT8 and back 44 us, two
  * launches of 74 MB each.  A single token of 64 rows is two launches and the
- * host's checks, 22 us.
+ * host's checks, 23 us.
  */
 #pragma once
 #include "kv_common.h"

@@ -796,7 +796,8 @@ def kv_write(k, v, cache: KVCache, rows: KVRows, status=None) -> None:
 def kv_read(cache: KVCache, rows: KVRows, n_tokens: int, dtype, out=None, status=None):
     """(k, v): the last lengths[i] of row i's kv_lens[i] positions as
     [n_tokens, heads, head_dim] tensors of `dtype` (asynchronous on the current
-    stream; `out`: a pair of tensors to write into)."""
+    stream; `out`: a pair of tensors to write into).  There is no backward pass: a
+    cache that requires a gradient is refused while autograd is on."""
     T = _types()
     ca, ra = _cache_args(T, cache), _rows_args(T, rows, int(n_tokens))
     if out is None:
