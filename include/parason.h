@@ -455,9 +455,25 @@ int parason_join_sized(const parason_handle *h, const int32_t *tokens, const int
  * (1 / Q, the product, the quotient and the product read back each rounded to
  * float once).
  * A head that holds a NaN or an infinity gets scale NaN, so that all of it
- * reads back as NaN (16-bit caches keep such values as they are). */
+ * reads back as NaN (16-bit caches keep such values as they are).
+ *
+ * 4-bit caches hold codes of a sign, two exponent bits and one fraction bit
+ * (0, 0.5, 1, 1.5, 2, 3, 4, 6), value 2i of a head in the low half of its byte i
+ * and value 2i + 1 in the high half, and one byte for each 32 values of a head,
+ * e + 127 for the power of two 2^e that they share (255: all 32 are NaN):
+ *   e    = the least one with amax <= 7 * 2^e, amax the largest |x| of the 32,
+ *          but at least -120 and at most 125;
+ *   code = x / 2^e rounded to nearest even, beyond 6 to 6; read back as
+ *          code * 2^e, both exact but for the one rounding.
+ * (A largest value between 6 and 7 times 2^e becomes 6: at most 1 off, as it
+ * would be between 3 and 3.5 times 2^(e + 1), where the other values of the 32
+ * had steps of twice the size.)  32 values that hold a NaN or an infinity read
+ * back as NaN.  4-bit values take 4.25 bits each, scales included, 8-bit ones
+ * of 128 values a head 8.25. */
 #define PARASON_DTYPE_FP8 3  /* 8 bits: sign, 4 exponent bits, 3 fraction bits, no infinities (OCP E4M3) */
 #define PARASON_DTYPE_INT8 4 /* -127 .. 127 */
+#define PARASON_DTYPE_FP4 5  /* 4 bits: sign, 2 exponent bits, 1 fraction bit (OCP E2M1), scales E8M0 */
+#define PARASON_KV_SCALE_GROUP 32 /* values of a 4-bit head that share a scale */
 
 #define PARASON_KV_MAX_DIM 256
 #define PARASON_KV_MAX_HEADS 1024
@@ -468,17 +484,19 @@ int parason_join_sized(const parason_handle *h, const int32_t *tokens, const int
  *   p * stride_page + t * stride_slot + h * stride_head + d
  * of k or v, and its scale element
  *   p * scale_stride_page + t * scale_stride_slot + h * scale_stride_head
- * of k_scale or v_scale.  k and v are 16-byte aligned and their strides
- * multiples of 16 bytes, so that a head's values are read 16 bytes at a time. */
+ * of k_scale or v_scale (4-bit: the first of its head_dim / 32 scales, which
+ * follow each other).  k and v are 16-byte aligned and their strides multiples
+ * of 16 bytes (4-bit: 32 elements), so that a head's values are read 16 bytes
+ * at a time. */
 typedef struct parason_kv_cache {
     void *k, *v;
-    float *k_scale, *v_scale; /* 8-bit caches; NULL for 16-bit ones */
+    void *k_scale, *v_scale;  /* float for 8-bit caches, uint8_t for 4-bit ones; NULL for 16-bit ones */
     int64_t n_pages;
     int64_t stride_page, stride_slot, stride_head;
     int64_t scale_stride_page, scale_stride_slot, scale_stride_head;
     int32_t page_size, n_heads;
-    int32_t head_dim;         /* a multiple of 16, at most PARASON_KV_MAX_DIM */
-    int32_t dtype;            /* PARASON_DTYPE_BF16, _F16, _FP8 or _INT8 */
+    int32_t head_dim;         /* a multiple of 16 (4-bit: of 32), at most PARASON_KV_MAX_DIM */
+    int32_t dtype;            /* PARASON_DTYPE_BF16, _F16, _FP8, _INT8 or _FP4 */
 } parason_kv_cache;
 
 /* The rows of a call (device arrays, host struct).  Row i has lengths[i] tokens
@@ -506,6 +524,127 @@ typedef struct parason_kv_rows {
                                          than max_kv_len or max_pages allow, fewer than the call needs, or more tree
                                          positions than the mask holds */
 #define PARASON_KV_BAD_PAGE (1u << 1) /* a page outside [0, n_pages) in a place that the row needs */
+#define PARASON_KV_NO_PAGES (1u << 2) /* parason_kv_extend: the pool has too few pages left */
+
+/* ---- tables of the cache -------------------------------------------------
+ * Who holds which pages, and where each new token belongs, worked out on the
+ * GPU from the rows' lengths: nothing of it visits the host.
+ *
+ * The pages that belong to nobody are a stack: free_pages[0 .. *free_count),
+ * the last of which is taken first.  A count outside [0, capacity] counts as
+ * the nearer of the two. */
+typedef struct parason_kv_pool {
+    int32_t *free_pages;      /* [capacity] */
+    int32_t *free_count;      /* [1], device memory */
+    int64_t capacity;
+} parason_kv_pool;
+
+/* The rows' tables (device arrays, host struct), updated in place.  Row i holds
+ * kv_lens[i] positions on its first ceil(kv_lens[i] / page_size) pages, at
+ * pages[i * pages_stride ..]; pages_stride >= max_pages where there are several
+ * rows. */
+typedef struct parason_kv_table {
+    int64_t n_rows;           /* at most 2^24 */
+    int32_t *kv_lens;         /* [n_rows] */
+    int32_t *pages;
+    int64_t pages_stride;
+    int32_t max_pages, page_size;
+} parason_kv_table;
+
+/* What parason_kv_extend writes: per row the arguments of parason_kv_rows, and
+ * per token (each of the three arrays may be NULL) where it belongs; -1 for
+ * tokens of no row and of rows that were not served. */
+typedef struct parason_kv_step {
+    int32_t *lengths;         /* [n_rows] the row's tokens, 0 if it was not served; not the array of the wished lengths */
+    int64_t *starts;          /* [n_rows] their first one: the sum of the wished lengths before it, at most n_tokens */
+    uint32_t *row_status;     /* [n_rows] 0, PARASON_KV_BAD_ROW or PARASON_KV_NO_PAGES (set, not ORed); NULL: not reported */
+    int32_t *positions;       /* [n_tokens] position in the row */
+    int64_t *slots;           /* [n_tokens] page * page_size + slot of the page (-1 too where the table holds a negative page) */
+    int32_t *rows;            /* [n_tokens] the row */
+} parason_kv_step;
+
+/* Bytes of device workspace that both calls below need. */
+int parason_kv_tables_workspace_size(int64_t n_rows, size_t *bytes);
+
+/* Room for lengths[i] new tokens behind the kv_lens[i] positions of every row,
+ * asynchronously on `stream`: new pages are taken for the rows in order (page k
+ * of a row's new ones is the pool's next), kv_lens[i] grows by lengths[i], and
+ * `out` is written.  n_tokens: the size of the call's token arrays, of which the
+ * sum of the lengths may leave some over.  Not served, and left as they were:
+ *   - bad rows: a negative length or kv_len, more positions than max_pages or
+ *     PARASON_KV_MAX_LEN allow, tokens that reach beyond n_tokens;
+ *   - rows that need a page when the pages that they and the rows before them
+ *     (bad ones aside) need are more than the pool has.
+ * Pages taken from the pool stay in free_pages, behind the new count. */
+int parason_kv_extend(const parason_kv_pool *pool, const parason_kv_table *table, const int32_t *lengths,
+                      int64_t n_tokens, const parason_kv_step *out, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/* Every row gives back what is behind its first new_lens[i] positions (a
+ * finished rollout: all of them; a draft: the tokens that were refused):
+ * kv_lens[i] becomes new_lens[i], pages that hold none of these go onto the
+ * pool, and their entries become -1.  The first row's first page goes on last:
+ * a shrink to the lengths before an extend undoes it, the order of the free
+ * pages included.  Bad rows (new_lens[i] negative or more than kv_lens[i], a
+ * kv_len that is negative or more than max_pages hold) stay as they are;
+ * entries that are negative go onto the pool too, and pages for which the pool
+ * has no room are lost: both set PARASON_KV_BAD_PAGE.  Pages that several rows
+ * share are the caller's to keep: the rows that do not own them give back what
+ * is behind the shared prefix. */
+int parason_kv_shrink(const parason_kv_pool *pool, const parason_kv_table *table, const int32_t *new_lens,
+                      uint32_t *row_status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- norm and rotation of queries and keys -------------------------------
+ * What a layer does to the heads of its queries and keys before they meet (the
+ * keys in the cache), in one pass.  For a head x of a token at position p:
+ *   n_d = x_d * r * w_d,   r = 1 / sqrt(mean_d x_d^2 + eps),
+ *   y   = n with its pairs j = 0 .. n_turned / 2 - 1 rotated:
+ *   y_a = n_a cos(p f_j) - n_b sin(p f_j),   y_b = n_b cos(p f_j) + n_a sin(p f_j),
+ * (a, b) = (j, j + n_turned / 2), or (2j, 2j + 1) with
+ * PARASON_ROTATE_INTERLEAVED; values from n_turned on are not rotated.  The
+ * angle p f_j is reduced to a turn in double; all else is float32, rounded once
+ * at the end.  (Squares that float32 does not hold are infinite: the head is
+ * zero then.)  A token with a negative position is padding: its results and
+ * gradients are zero, whatever its values are. */
+#define PARASON_ROTATE_INTERLEAVED (1u << 0)
+
+typedef struct parason_rotate {
+    int64_t n_tokens;
+    int32_t n_q_heads, n_k_heads; /* 0 .. PARASON_KV_MAX_HEADS each */
+    int32_t head_dim;         /* a multiple of 16, at most PARASON_KV_MAX_DIM */
+    int32_t n_turned;         /* a multiple of 16, 0 .. head_dim */
+    int32_t dtype;            /* of the heads and the weights: PARASON_DTYPE_F32, _BF16 or _F16 */
+    uint32_t flags;
+    float eps;                /* > 0 */
+    const int32_t *positions; /* [n_tokens] */
+    const double *freqs;      /* [n_turned / 2] radians a position */
+    const void *q_weight, *k_weight; /* [head_dim]; NULL: ones */
+} parason_rotate;
+
+/* Heads of a call's tokens: value d of query head h of token t is element
+ * t * q_stride_token + h * q_stride_head + d of q; keys alike. */
+typedef struct parason_heads {
+    void *q, *k;
+    int64_t q_stride_token, q_stride_head, k_stride_token, k_stride_head;
+} parason_heads;
+
+/* y of every head of x, asynchronously on `stream`.  y may be x itself (the same
+ * addresses and strides); other overlaps give wrong results. */
+int parason_qk_norm_rotate(const parason_rotate *r, const parason_heads *x, const parason_heads *y, void *stream);
+
+/* The backward pass: dx of every head from x and dy = d loss / d y, and d loss /
+ * d weight, the sum over all tokens and heads (float32, in an order that the
+ * sizes fix; either may be NULL).  With g = dy rotated back by the token's
+ * angles and xhat = x * r:
+ *   dw_d = sum g_d xhat_d,   dx_d = r * (g_d w_d - xhat_d mean_d(g_d w_d xhat_d)).
+ * dx may be x or dy itself.  workspace: at least
+ * parason_qk_norm_rotate_workspace_size bytes, 256-byte aligned. */
+int parason_qk_norm_rotate_workspace_size(const parason_rotate *r, size_t *bytes);
+int parason_qk_norm_rotate_grad(const parason_rotate *r, const parason_heads *x, const parason_heads *dy,
+                                const parason_heads *dx, float *q_weight_grad, float *k_weight_grad, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* ---- writing and reading the cache --------------------------------------- */
 
 /* Write the keys and values of the rows' tokens into the cache, asynchronously
  * on `stream`: token j of row i goes to position kv_lens[i] - lengths[i] + j,
@@ -542,7 +681,9 @@ int parason_kv_read(const parason_kv_cache *cache, const parason_kv_rows *rows, 
  * holds.  Scores, maxima, sums and the accumulation are float32; for the matrix
  * product with v the weights exp(s_p - max), an 8-bit cache's scales of v
  * among them, are rounded to 16 bits (float16 over an F16 cache, else bfloat16;
- * F16 results over an 8-bit cache: to two bfloat16 terms).  Weights below 2^-39
+ * F16 results over an 8- or 4-bit cache: to two bfloat16 terms).  Weights below
+ * 2^-126 of a token's largest, and values of a 4-bit cache below 2^-126 (scales
+ * that parason_kv_write does not make), may count as zero.  Weights below 2^-39
  * of a token's largest are nothing over an F16 cache: an infinity of v behind
  * such a weight gives NaN.  Bad rows get NaN (nothing, where starts[i] and
  * lengths[i] themselves are bad), and so do tokens that see a position on a bad

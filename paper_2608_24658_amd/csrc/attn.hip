@@ -18,6 +18,7 @@ TreeKernel pick_kind(bool f16, int kind)
     switch (kind) {
     case pk::KV_BF16: return pk::tree_attention<DP, COLS, false, pk::KV_BF16>;
     case pk::KV_F16: return pk::tree_attention<DP, COLS, true, pk::KV_F16>;
+    case pk::KV_FP4: return f16 ? pk::tree_attention<DP, COLS, true, pk::KV_FP4> : pk::tree_attention<DP, COLS, false, pk::KV_FP4>;
     case pk::KV_FP8: return f16 ? pk::tree_attention<DP, COLS, true, pk::KV_FP8> : pk::tree_attention<DP, COLS, false, pk::KV_FP8>;
     default: return f16 ? pk::tree_attention<DP, COLS, true, pk::KV_INT8> : pk::tree_attention<DP, COLS, false, pk::KV_INT8>;
     }

@@ -127,11 +127,25 @@ __device__ __forceinline__ frag8 widen8(uint2 w)
     return __builtin_bit_cast(frag8, make_uint4(a.x, a.y, b.x, b.y));
 }
 
+/* A piece of a 4-bit cache, 32 codes and their power of two, to four operands' worth of bfloat16: exact. */
+__device__ __forceinline__ void widen32(u32x4 w, float scale, frag8 *to)
+{
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+        const b2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+        const b2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+        to[i] = __builtin_bit_cast(frag8, make_uint4(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1),
+                                                     __builtin_bit_cast(uint32_t, x2), __builtin_bit_cast(uint32_t, x3)));
+    }
+}
+
 /* A word of V without its infinities and NaN, which become zeros. */
 template <int KIND>
 __device__ __forceinline__ uint32_t finite_word(uint32_t w)
 {
-    if (KIND == KV_INT8) return w;
+    if (KIND == KV_INT8 || KIND == KV_FP4) return w; /* (4-bit: NaN is the scale's) */
     if (KIND == KV_FP8) {
         /* NaN is all ones below the sign: a zero byte of the complement */
         const uint32_t some = ((~w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) & 0x80808080u;
@@ -147,7 +161,7 @@ __device__ __forceinline__ float cached_value(const char *p)
 {
     if (KIND == KV_BF16) return bf16_to_f32(*reinterpret_cast<const uint16_t *>(p));
     if (KIND == KV_F16) return f16_to_f32(*reinterpret_cast<const uint16_t *>(p));
-    float x[4];
+    float x[4] = {};
     if (KIND == KV_FP8) fp8x4_to_f32((uint8_t)*p, x);
     else int8x4_to_f32((uint8_t)*p, x);
     return x[0];
@@ -160,6 +174,7 @@ constexpr int TREE_SKIP_WORDS = 64; /* of the list of a tree's tiles that nobody
 template <int DP, int COLS, int KIND>
 struct TreeShape {
     static constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
+    static constexpr bool FOUR = KIND == KV_FP4;      /* codes with their scales go to LDS as bfloat16 */
     /* Few columns: every wave has its own positions of a tile, and needs the others only at the end. */
     static constexpr bool SOLO = COLS < 128;
     /* Codes go to LDS as they are where one wave reads them again, and are widened behind it; where all four waves take
@@ -222,7 +237,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     constexpr int CN = Sh::CN, G = Sh::G, NV = Sh::NV, KSTEP = Sh::KSTEP, AC = Sh::AC, WQ = Sh::WQ;
     typedef typename Acc<CN>::type acc;
     constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
-    constexpr bool CODES = Sh::CODES, RAW = Sh::RAW;
+    constexpr bool CODES = Sh::CODES, RAW = Sh::RAW, FOUR = Sh::FOUR;
+    /* Type of the keys where they meet the queries.  A 4-bit cache's are bfloat16 (float16 does not hold all of its
+     * scales), and float16 queries two bfloat16 terms, which is all of them. */
+    constexpr bool SF16 = F16 && !FOUR, TWO = F16 && FOUR;
     /* Type of the weights and of V: bfloat16 for codes, whose scales are in the weights.  The weights are rounded to it for
      * the matrix product: 2^-9 of each, against which a result of the same type is rounded by as much once more (bfloat16
      * results are off by 0.0020 to 0.0024 of their size in all, and by 0.0017 with float32 weights).  Two terms would take
@@ -231,20 +249,19 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     /* float16 results over codes: the weights go in as two bfloat16 terms, so that they are not the coarsest step of
      * the whole.  (float16 weights would lose all precision where the positions with nearly all of the weight hold a
      * code of zero.) */
-    constexpr bool SPLIT = CODES && F16;
+    constexpr bool SPLIT = (CODES || FOUR) && F16;
     /* The largest weight is 2^LIFT: of float16's 30 binades of full precision 29 are then below it. */
     constexpr int LIFT = PF16 ? 15 : 0;
-    constexpr int VE = CODES ? 16 : 8;      /* values of a 16-byte piece of the cache */
+    constexpr int VE = FOUR ? 32 : CODES ? 16 : 8; /* values of a 16-byte piece of the cache */
     /* a tile's rows are loaded by the block, or its own ones by a wave */
     constexpr int LOADERS = Sh::SOLO ? 64 : TREE_THREADS, ROWS = Sh::SOLO ? Sh::KW : TK;
-    constexpr int VPR = DP / VE, RPP = LOADERS / VPR, NP = ROWS / RPP;
-    constexpr int ES = CODES ? 1 : 2;
+    constexpr int VPR = DP / VE, RPP = LOADERS / VPR < ROWS ? LOADERS / VPR : ROWS, NP = ROWS / RPP;
     constexpr int KD = 8 * G, NK = DP / KD, ND = DP / CN;
     static_assert(NP >= 1 && NP * RPP == ROWS, "the loads cover a tile");
 
     __shared__ __attribute__((aligned(16))) char tile[Sh::TILE];
     __shared__ __attribute__((aligned(16))) float k_sc[CODES ? TK : 4], v_sc[CODES ? TK : 4];
-    __shared__ int64_t place[TK];
+    __shared__ int64_t place[TK], scale_place[FOUR ? TK : 1];
     __shared__ int32_t v_stamp[TK];
     __shared__ uint32_t skip[TREE_SKIP_WORDS];
     __shared__ int32_t flags[2];            /* a bad page; the last tile with a value of V that is not finite (of the block) */
@@ -289,7 +306,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     const bool live = tok < w.length;
     const int32_t q_head = head * a.group + (col - tok * a.group);
     const int64_t t = w.start + (live ? tok : 0);
-    frag8 qf[NK];
+    frag8 qf[NK], qf_rest[TWO ? NK : 1];
     {
         const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + t * a.q_stride_token + (live ? q_head : 0) * a.q_stride_head;
 #pragma unroll
@@ -305,6 +322,19 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                     x = make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16), e[6] | (e[7] << 16));
                 }
                 if (a.negate) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
+            }
+            if (TWO) {
+                uint32_t w[4] = {x.x, x.y, x.z, x.w}, r[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a0 = f16_to_f32(w[i] & 0xFFFFu), a1 = f16_to_f32(w[i] >> 16);
+                    w[i] = pack2<false>(a0, a1);
+                    /* (an infinity is all in the first term) */
+                    const float r0 = a0 - __uint_as_float(w[i] << 16), r1 = a1 - __uint_as_float(w[i] & 0xFFFF0000u);
+                    r[i] = pack2<false>(fabsf(a0) < INFINITY ? r0 : 0.0f, fabsf(a1) < INFINITY ? r1 : 0.0f);
+                }
+                qf_rest[k] = __builtin_bit_cast(frag8, make_uint4(r[0], r[1], r[2], r[3]));
+                x = make_uint4(w[0], w[1], w[2], w[3]);
             }
             qf[k] = __builtin_bit_cast(frag8, x);
         }
@@ -361,10 +391,11 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
 
     /* ---- loads: a position's page a tile ahead of its keys and values, these a tile ahead of their use */
     const int32_t loader = Sh::SOLO ? lane : tid, row0 = Sh::SOLO ? k0 : 0; /* who loads what of a tile */
-    const int32_t my_piece = loader % VPR, my_row = row0 + loader / VPR;
-    const bool piece_live = my_piece * VE < a.c.head_dim;
+    const bool loads = LOADERS / VPR <= ROWS || loader < ROWS * VPR; /* (fewer pieces than lanes) */
+    const int32_t my_piece = loader % VPR, my_row = row0 + (loads ? loader / VPR : 0);
+    const bool piece_live = loads && my_piece * VE < a.c.head_dim;
     const int64_t piece_at = (int64_t)head * a.c.stride_head + (piece_live ? my_piece * VE : 0);
-    const char *const kb = a.c.k + piece_at * ES, *const vb = a.c.v + piece_at * ES;
+    const char *const kb = a.c.k + cache_bytes<KIND>(piece_at), *const vb = a.c.v + cache_bytes<KIND>(piece_at);
     auto together = [&]() {                  /* what a loader put into LDS is there for the others */
         if (!Sh::SOLO) {
             __syncthreads();
@@ -388,18 +419,25 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         if (loader >= ROWS) return;
         if (pg < 0 || pg >= a.c.n_pages) flags[0] = 0, pg = pg_slot = 0;
         place[row0 + loader] = (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
-        if (CODES)
+        if (CODES || FOUR)
             scale_at = (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
                        (int64_t)head * a.c.scale_stride_head;
+        if (FOUR) scale_place[row0 + loader] = scale_at;
     };
     u32x4 kr[NP], vr[NP];
+    uint32_t k_byte[FOUR ? NP : 1], v_byte[FOUR ? NP : 1]; /* the pieces' scales */
     float k_scale = 0.0f, v_scale = 0.0f;    /* of position row0 + loader */
     auto load_tile = [&]() {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int64_t from = place[my_row + p * RPP];
-            kr[p] = *reinterpret_cast<const u32x4 *>(kb + from * ES);
-            vr[p] = *reinterpret_cast<const u32x4 *>(vb + from * ES);
+            kr[p] = *reinterpret_cast<const u32x4 *>(kb + cache_bytes<KIND>(from));
+            vr[p] = *reinterpret_cast<const u32x4 *>(vb + cache_bytes<KIND>(from));
+            if (FOUR) {
+                const int64_t at = scale_place[my_row + p * RPP] + (piece_live ? my_piece : 0);
+                k_byte[p] = reinterpret_cast<const uint8_t *>(a.c.k_scale)[at];
+                v_byte[p] = reinterpret_cast<const uint8_t *>(a.c.v_scale)[at];
+            }
         }
         if (CODES && loader < ROWS) k_scale = a.c.k_scale[scale_at], v_scale = a.c.v_scale[scale_at];
     };
@@ -442,6 +480,14 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
              * they are left out here and added one position at a time below */
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
+                if (FOUR) {
+                    if (piece_live && v_byte[p] == 255u) {
+                        v_stamp[my_row + p * RPP] = x;
+                        odd_seen = true;
+                        v_byte[p] = 127u;
+                    }
+                    continue;
+                }
                 const u32x4 v = vr[p];
                 const u32x4 f = {finite_word<KIND>(v.x), finite_word<KIND>(v.y), finite_word<KIND>(v.z), finite_word<KIND>(v.w)};
                 if (piece_live && ((f.x ^ v.x) | (f.y ^ v.y) | (f.z ^ v.z) | (f.w ^ v.w)) != 0u) {
@@ -456,7 +502,16 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             for (int p = 0; p < NP; ++p) {
                 const int r = my_row + p * RPP;
                 char *const kd = Ks + (r * KS + my_piece * VE) * LS, *const vd = Vs + (r * VS + my_piece * VE) * LS;
-                if (CODES && !RAW) {
+                if (FOUR) {
+                    frag8 wide[4];
+                    widen32(kr[p], fp4_scale(k_byte[p]), wide);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<frag8 *>(kd + 16 * i) = wide[i];
+                    widen32(vr[p], fp4_scale(v_byte[p]), wide);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<frag8 *>(vd + 16 * i) = wide[i];
+                    __builtin_amdgcn_sched_barrier(0);
+                } else if (CODES && !RAW) {
                     *reinterpret_cast<frag8 *>(kd) = widen8<F16, KIND>(make_uint2(kr[p].x, kr[p].y));
                     *reinterpret_cast<frag8 *>(kd + 16) = widen8<F16, KIND>(make_uint2(kr[p].z, kr[p].w));
                     *reinterpret_cast<frag8 *>(vd) = widen8<PF16, KIND>(make_uint2(vr[p].x, vr[p].y));
@@ -510,7 +565,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
 #pragma unroll
             for (int j = 0; j < KG; ++j) {
                 const frag8 f = RAW ? widen8<F16, KIND>(make_uint2(kf[g][j].x, kf[g][j].y)) : __builtin_bit_cast(frag8, kf[g][j]);
-                c[g * KG / NK] = mma<F16>(f, qf[(g * KG + j) % NK], c[g * KG / NK]);
+                c[g * KG / NK] = mma<SF16>(f, qf[(g * KG + j) % NK], c[g * KG / NK]);
+                if (TWO) c[g * KG / NK] = mma<SF16>(f, qf_rest[(g * KG + j) % NK], c[g * KG / NK]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -689,15 +745,19 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                     if (page < 0) continue;
                     int32_t h4 = 4 * h;      /* not known before: what depends on it is not worth registers in the loop */
                     asm volatile("" : "+v"(h4));
-                    const char *v = a.c.v + ((int64_t)page * a.c.stride_page + (int64_t)slot * a.c.stride_slot +
-                                             (int64_t)head * a.c.stride_head) * ES;
+                    const char *v = a.c.v + cache_bytes<KIND>((int64_t)page * a.c.stride_page + (int64_t)slot * a.c.stride_slot +
+                                                              (int64_t)head * a.c.stride_head);
+                    if (FOUR)                /* what is NaN in a 4-bit cache is so by its scale */
+                        v = (const char *)a.c.v_scale + (int64_t)page * a.c.scale_stride_page + (int64_t)slot * a.c.scale_stride_slot +
+                            (int64_t)head * a.c.scale_stride_head;
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
 #pragma unroll
                         for (int i = 0; i < AC; ++i) {
                             const int at_d = d * CN + 8 * (i / 4) + h4 + (i & 3);
                             if (at_d >= a.c.head_dim) continue;
-                            const float e = cached_value<KIND>(v + at_d * ES);
+                            const float e = FOUR ? ((uint8_t)v[at_d / 32] == 255u ? __uint_as_float(0x7FC00000u) : 0.0f)
+                                                 : cached_value<KIND>(v + cache_bytes<KIND>(at_d));
                             if (!(e > -INFINITY && e < INFINITY)) o[d][i] += p * e;
                         }
                         __builtin_amdgcn_sched_barrier(0);

@@ -19,6 +19,7 @@ MoveKernel pick(int dtype, int kind)
     case pk::KV_BF16: return dtype == F32 ? K<F32, pk::KV_BF16>::f : dtype == BF16 ? K<BF16, pk::KV_BF16>::f : K<F16, pk::KV_BF16>::f;
     case pk::KV_F16: return dtype == F32 ? K<F32, pk::KV_F16>::f : dtype == BF16 ? K<BF16, pk::KV_F16>::f : K<F16, pk::KV_F16>::f;
     case pk::KV_FP8: return dtype == F32 ? K<F32, pk::KV_FP8>::f : dtype == BF16 ? K<BF16, pk::KV_FP8>::f : K<F16, pk::KV_FP8>::f;
+    case pk::KV_FP4: return dtype == F32 ? K<F32, pk::KV_FP4>::f : dtype == BF16 ? K<BF16, pk::KV_FP4>::f : K<F16, pk::KV_FP4>::f;
     default: return dtype == F32 ? K<F32, pk::KV_INT8>::f : dtype == BF16 ? K<BF16, pk::KV_INT8>::f : K<F16, pk::KV_INT8>::f;
     }
 }

@@ -30,12 +30,13 @@ inline int check_cache(const parason_kv_cache *c, pk::KvCache *o, int *kind)
     case PARASON_DTYPE_F16: *kind = pk::KV_F16; break;
     case PARASON_DTYPE_FP8: *kind = pk::KV_FP8; break;
     case PARASON_DTYPE_INT8: *kind = pk::KV_INT8; break;
+    case PARASON_DTYPE_FP4: *kind = pk::KV_FP4; break;
     default: return PARASON_ERR_PARAM;
     }
-    const bool codes = *kind == pk::KV_FP8 || *kind == pk::KV_INT8;
+    const bool four = *kind == pk::KV_FP4, codes = *kind == pk::KV_FP8 || *kind == pk::KV_INT8 || four;
     if (c->n_pages < 0 || c->n_pages > INT32_MAX || c->page_size < 1 || c->n_heads < 1 ||
         c->n_heads > PARASON_KV_MAX_HEADS || c->head_dim < 16 || c->head_dim > PARASON_KV_MAX_DIM ||
-        c->head_dim % 16 != 0)
+        c->head_dim % (four ? PARASON_KV_SCALE_GROUP : 16) != 0)
         return PARASON_ERR_SIZE;
     if (!stride_fits(c->stride_page, c->n_pages) || !stride_fits(c->stride_slot, c->page_size) ||
         !stride_fits(c->stride_head, c->n_heads) ||
@@ -44,14 +45,14 @@ inline int check_cache(const parason_kv_cache *c, pk::KvCache *o, int *kind)
                    !stride_fits(c->scale_stride_head, c->n_heads))))
         return PARASON_ERR_SIZE;
     if (c->n_pages > 0 && (!c->k || !c->v || (codes && (!c->k_scale || !c->v_scale)))) return PARASON_ERR_NULL;
-    const int64_t unit = codes ? 16 : 8; /* elements of 16 bytes */
+    const int64_t unit = four ? 32 : codes ? 16 : 8; /* elements of 16 bytes */
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || c->stride_page % unit != 0 || c->stride_slot % unit != 0 ||
-        c->stride_head % unit != 0 || (codes && (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4))))
+        c->stride_head % unit != 0 || (codes && !four && (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4))))
         return PARASON_ERR_ALIGN;
     o->k = (char *)c->k;
     o->v = (char *)c->v;
-    o->k_scale = codes ? c->k_scale : nullptr;
-    o->v_scale = codes ? c->v_scale : nullptr;
+    o->k_scale = codes ? (float *)c->k_scale : nullptr;
+    o->v_scale = codes ? (float *)c->v_scale : nullptr;
     o->n_pages = c->n_pages;
     o->stride_page = c->stride_page, o->stride_slot = c->stride_slot, o->stride_head = c->stride_head;
     o->scale_stride_page = c->scale_stride_page, o->scale_stride_slot = c->scale_stride_slot;

@@ -1,7 +1,7 @@
 /*
  * kv_common.h -- what the cache's kernels and the attention that reads it
  * share: the device views of a cache and of a call's rows, a row's bounds,
- * the place of a position, and the 8-bit codes.
+ * the place of a position, and the 8- and 4-bit codes.
  */
 #pragma once
 #include <hip/hip_runtime.h>
@@ -30,11 +30,18 @@ __device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv &f)
     return (uint32_t)(((uint64_t)n * f.m) >> (31 + f.s));
 }
 
-enum : int { KV_BF16 = 0, KV_F16, KV_FP8, KV_INT8 };
+enum : int { KV_BF16 = 0, KV_F16, KV_FP8, KV_INT8, KV_FP4 };
+
+/* Bytes of n values of a cache. */
+template <int KIND>
+__device__ __forceinline__ constexpr int64_t cache_bytes(int64_t n)
+{
+    return KIND == KV_FP4 ? n / 2 : KIND == KV_FP8 || KIND == KV_INT8 ? n : n * 2;
+}
 
 struct KvCache {
     char *k, *v;
-    float *k_scale, *v_scale;
+    float *k_scale, *v_scale;                                        /* 4-bit caches: bytes */
     int64_t n_pages;
     int64_t stride_page, stride_slot, stride_head;                   /* elements */
     int64_t scale_stride_page, scale_stride_slot, scale_stride_head;
@@ -130,6 +137,38 @@ __device__ __forceinline__ uint32_t f32_to_int8x4(const float *x)
 #pragma unroll
     for (int e = 0; e < 4; ++e) w |= ((uint32_t)(int32_t)__builtin_rintf(x[e]) & 255u) << (8 * e);
     return w;
+}
+
+/* The power of two that 32 values of four bits share, as the conversions take
+ * it: they read a float's exponent field, and 255 there (a byte of 255) makes
+ * every value NaN. */
+__device__ __forceinline__ float fp4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+/* Eight codes of one 32-bit word, times their power of two: exact. */
+__device__ __forceinline__ void fp4x8_to_f32(uint32_t w, float scale, float *x)
+{
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+    const f2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
+}
+
+/* Eight values to codes: divided by their power of two, rounded to nearest even, at most 6. */
+__device__ __forceinline__ uint32_t f32_to_fp4x8(const float *x, float scale)
+{
+    uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+}
+
+/* The byte of the least power of two, within the bounds of parason.h, with amax
+ * <= 7 times it; top: amax's bits, finite. */
+__device__ __forceinline__ uint32_t fp4_scale_byte(uint32_t top)
+{
+    /* amax = f * 2^(E - 127), 1 <= f < 2: E - 2 for f <= 1.75, else E - 1 (the carry of the fraction) */
+    const int32_t e = (int32_t)((top + 0x1FFFFFu) >> 23) - 2;
+    return (uint32_t)(e < 7 ? 7 : e > 252 ? 252 : e);
 }
 
 }  // namespace pk

@@ -35,11 +35,15 @@ struct KvMoveArgs {
 };
 
 /* A lane's eight values are two fours, at value lo and hi of the head: neighbours for 16-bit token arrays, 16 bytes in
- * all; for float32 ones half the group's lanes apart, so that neighbouring lanes read neighbouring 16 bytes. */
-template <int T>
-__device__ __forceinline__ int piece_lo(int lane) { return lane * (T == PARASON_DTYPE_F32 ? 4 : 8); }
-template <int T>
-__device__ __forceinline__ int piece_hi(int lane, int group) { return T == PARASON_DTYPE_F32 ? (group + lane) * 4 : lane * 8 + 4; }
+ * all; for float32 ones half the group's lanes apart, so that neighbouring lanes read neighbouring 16 bytes (but for
+ * 4-bit caches, where eight neighbours are one word of codes and four lanes' share a scale). */
+template <int T, int KIND>
+__device__ __forceinline__ int piece_lo(int lane) { return lane * (T == PARASON_DTYPE_F32 && KIND != KV_FP4 ? 4 : 8); }
+template <int T, int KIND>
+__device__ __forceinline__ int piece_hi(int lane, int group)
+{
+    return T == PARASON_DTYPE_F32 && KIND != KV_FP4 ? (group + lane) * 4 : lane * 8 + 4;
+}
 
 /* T: type of the token arrays, PARASON_DTYPE_F32, _BF16 or _F16; p: the head */
 template <int T>
@@ -134,10 +138,10 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
-    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
+    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8 || KIND == KV_FP4;
     const int lane = (int)threadIdx.x & (a.group - 1);
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.c.n_heads;
-    const int lo = piece_lo<T>(lane), hi = piece_hi<T>(lane, a.group);
+    const int lo = piece_lo<T, KIND>(lane), hi = piece_hi<T, KIND>(lane, a.group);
     const bool live = lo < a.c.head_dim, hi_live = hi < a.c.head_dim;
     for (int64_t u0 = part * step * KV_WRITES; u0 < units; u0 += a.blocks_per_row * step * KV_WRITES) {
         KvUnit x[KV_WRITES];
@@ -178,8 +182,20 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write(KvMoveArgs a)
             uint32_t top = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7FFFFFFFu);
-            for (int o = a.group >> 1; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+            for (int o = KIND == KV_FP4 ? 2 : a.group >> 1; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
             const bool finite = top < 0x7F800000u;
+            if (KIND == KV_FP4) {
+                /* (top of the four lanes that share a scale: the loop above ends early) */
+                const uint32_t byte = finite ? fp4_scale_byte(top) : 255u;
+                if (!mine[i]) continue;
+                *reinterpret_cast<uint32_t *>(cache + (at + lo) / 2) = finite ? f32_to_fp4x8(f[i], fp4_scale(byte)) : 0u;
+                if ((lane & 3) == 0)
+                    reinterpret_cast<uint8_t *>(x[i].is_v ? a.c.v_scale : a.c.k_scale)[(int64_t)x[i].page * a.c.scale_stride_page +
+                                                                                       (int64_t)x[i].slot * a.c.scale_stride_slot +
+                                                                                       x[i].head * a.c.scale_stride_head + (lane >> 2)] =
+                        (uint8_t)byte;
+                continue;
+            }
             float scale = fmaxf(__uint_as_float(top) * (KIND == KV_FP8 ? 1.0f / 448.0f : 1.0f / 127.0f), 0x1p-126f);
             if (!finite) scale = __uint_as_float(0x7FC00000u);
 #pragma unroll
@@ -211,10 +227,10 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
-    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
+    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8 || KIND == KV_FP4;
     const int lane = (int)threadIdx.x & (a.group - 1);
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.c.n_heads;
-    const int lo = piece_lo<T>(lane), hi = piece_hi<T>(lane, a.group);
+    const int lo = piece_lo<T, KIND>(lane), hi = piece_hi<T, KIND>(lane, a.group);
     if (lo >= a.c.head_dim) return;
     const bool hi_live = hi < a.c.head_dim;
     for (int64_t u0 = part * step * KV_READS; u0 < units; u0 += a.blocks_per_row * step * KV_READS) {
@@ -244,6 +260,12 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
                     raw[i] = *reinterpret_cast<const uint4 *>(cache + (at + lo) * 2);
                 }
                 scale[i] = 1.0f;
+            } else if (KIND == KV_FP4) {
+                raw[i].x = *reinterpret_cast<const uint32_t *>(cache + (at + lo) / 2);
+                scale[i] = fp4_scale(
+                    reinterpret_cast<const uint8_t *>(x[i].is_v ? a.c.v_scale : a.c.k_scale)[(int64_t)x[i].page * a.c.scale_stride_page +
+                                                                                             (int64_t)x[i].slot * a.c.scale_stride_slot +
+                                                                                             x[i].head * a.c.scale_stride_head + (lane >> 2)]);
             } else {
                 if (T == PARASON_DTYPE_F32) {
                     raw[i].x = *reinterpret_cast<const uint32_t *>(cache + at + lo);
@@ -268,6 +290,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
                     const uint32_t b = (h[e / 2] >> (16 * (e & 1))) & 0xFFFFu;
                     f[e] = x[i].page < 0 ? scale[i] : KIND == KV_BF16 ? bf16_to_f32(b) : f16_to_f32(b);
                 }
+            } else if (KIND == KV_FP4) {
+                fp4x8_to_f32(raw[i].x, scale[i], f);
             } else {
                 if (KIND == KV_FP8) fp8x4_to_f32(raw[i].x, f), fp8x4_to_f32(raw[i].y, f + 4);
                 else int8x4_to_f32(raw[i].x, f), int8x4_to_f32(raw[i].y, f + 4);

@@ -48,7 +48,9 @@ EXPORTED = ("parason_create", "parason_workspace_size", "parason_run", "parason_
             "parason_decode_step", "parason_fork_workspace_size", "parason_join_workspace_size", "parason_fork",
             "parason_join", "parason_read_probe", "parason_run_noalloc", "parason_fork_sized", "parason_join_sized",
             "parason_kv_write", "parason_kv_read", "parason_tree_attention_workspace_size", "parason_tree_attention",
-            "parason_beam_workspace_size", "parason_beam_select", "parason_beam_reorder")
+            "parason_beam_workspace_size", "parason_beam_select", "parason_beam_reorder",
+            "parason_kv_tables_workspace_size", "parason_kv_extend", "parason_kv_shrink", "parason_qk_norm_rotate",
+            "parason_qk_norm_rotate_workspace_size", "parason_qk_norm_rotate_grad")
 
 FORK_SEED_ENTRY = 1 << 0
 JOIN_CLOSE_PARALLEL = 1 << 0
@@ -62,14 +64,17 @@ PACK_BAD_ROW = 1 << 5
 
 DECODE_ERROR = 1 << 0
 DECODE_DONE = 1 << 1
-DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_FP8, DTYPE_INT8 = range(5)
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_FP8, DTYPE_INT8, DTYPE_FP4 = range(6)
 DECODE_STATE_BYTES = 16
 
 KV_BAD_ROW = 1 << 0
 KV_BAD_PAGE = 1 << 1
+KV_NO_PAGES = 1 << 2
 KV_MAX_DIM = 256
 KV_MAX_HEADS = 1024
 KV_MAX_LEN = 1 << 30
+KV_SCALE_GROUP = 32
+ROTATE_INTERLEAVED = 1 << 0
 BEAM_MAX = 64
 BEAM_ARRAYS = 8
 
@@ -194,6 +199,60 @@ class TreeArgs(ctypes.Structure):
     ]
 
 
+class KvPoolArgs(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("capacity", ctypes.c_int64)]
+
+
+class KvTableArgs(ctypes.Structure):
+    _fields_ = [
+        ("n_rows", ctypes.c_int64),
+        ("kv_lens", ctypes.c_void_p),
+        ("pages", ctypes.c_void_p),
+        ("pages_stride", ctypes.c_int64),
+        ("max_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+    ]
+
+
+class KvStepArgs(ctypes.Structure):
+    _fields_ = [
+        ("lengths", ctypes.c_void_p),
+        ("starts", ctypes.c_void_p),
+        ("row_status", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+        ("rows", ctypes.c_void_p),
+    ]
+
+
+class RotateArgs(ctypes.Structure):
+    _fields_ = [
+        ("n_tokens", ctypes.c_int64),
+        ("n_q_heads", ctypes.c_int32),
+        ("n_k_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("n_turned", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("eps", ctypes.c_float),
+        ("positions", ctypes.c_void_p),
+        ("freqs", ctypes.c_void_p),
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+    ]
+
+
+class HeadsArgs(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("k", ctypes.c_void_p),
+        ("q_stride_token", ctypes.c_int64),
+        ("q_stride_head", ctypes.c_int64),
+        ("k_stride_token", ctypes.c_int64),
+        ("k_stride_head", ctypes.c_int64),
+    ]
+
+
 class BeamArray(ctypes.Structure):
     _fields_ = [
         ("src", ctypes.c_void_p),
@@ -295,6 +354,8 @@ def lib():
         L.parason_read_probe.restype = ctypes.c_int
         L.parason_read_probe.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_int64,
                                          ctypes.c_void_p]
+        pool, table, size, heads = (ctypes.POINTER(t) for t in (KvPoolArgs, KvTableArgs, ctypes.c_size_t, HeadsArgs))
+        rotate = ctypes.POINTER(RotateArgs)
         cache, rows, void, i64 = ctypes.POINTER(KvCacheArgs), ctypes.POINTER(KvRowsArgs), ctypes.c_void_p, ctypes.c_int64
         for name, args in (
             ("parason_kv_write", [cache, rows, void, void, ctypes.c_int32, i64, i64, void, void]),
@@ -305,6 +366,12 @@ def lib():
             ("parason_beam_select", [void, i64, i64, ctypes.c_int32, void, void, i64, ctypes.c_int32, void, void, void,
                                      void, ctypes.c_size_t, void]),
             ("parason_beam_reorder", [void, i64, ctypes.POINTER(BeamArray), ctypes.c_int32, void]),
+            ("parason_kv_tables_workspace_size", [i64, size]),
+            ("parason_kv_extend", [pool, table, void, i64, ctypes.POINTER(KvStepArgs), void, ctypes.c_size_t, void]),
+            ("parason_kv_shrink", [pool, table, void, void, void, ctypes.c_size_t, void]),
+            ("parason_qk_norm_rotate", [rotate, heads, heads, void]),
+            ("parason_qk_norm_rotate_workspace_size", [rotate, size]),
+            ("parason_qk_norm_rotate_grad", [rotate, heads, heads, heads, void, void, void, ctypes.c_size_t, void]),
         ):
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = args
@@ -645,7 +712,9 @@ class KVCache(NamedTuple):
     heads, head_dim] in any layout whose last stride is 1, of one type (bfloat16,
     float16, float8_e4m3fn or int8) and with the same strides; k_scale and
     v_scale (8-bit types only) float32 [pages, page_size, heads], with the same
-    strides."""
+    strides.  A 4-bit cache is float4_e2m1fn_x2 [pages, page_size, heads,
+    head_dim / 2], two values an element, and its scales float8_e8m0fnu [pages,
+    page_size, heads, head_dim / 32] with a last stride of 1."""
 
     k: Any
     v: Any
@@ -674,8 +743,13 @@ def kv_alloc(n_pages: int, page_size: int, heads: int, head_dim: int, dtype, dev
 
     code = _types().kv.get(dtype)
     if code is None:
-        raise TypeError("a cache holds bfloat16, float16, float8_e4m3fn or int8 values")
+        raise TypeError("a cache holds bfloat16, float16, float8_e4m3fn, int8 or float4_e2m1fn_x2 values")
     shape = (int(n_pages), int(heads), int(page_size), int(head_dim))
+    if code == DTYPE_FP4:
+        if head_dim % KV_SCALE_GROUP:
+            raise ValueError("head_dim of a 4-bit cache must be a multiple of %d" % KV_SCALE_GROUP)
+        return KVCache(*(torch.zeros(shape[:3] + (head_dim // n,), dtype=torch.uint8, device=device).view(dt).permute(0, 2, 1, 3)
+                         for n, dt in ((2, dtype), (2, dtype)) + ((KV_SCALE_GROUP, torch.float8_e8m0fnu),) * 2))
     kv = [torch.zeros(shape, dtype=torch.uint8 if code >= DTYPE_FP8 else dtype, device=device).view(dtype)
           .permute(0, 2, 1, 3) for _ in "kv"]
     if code >= DTYPE_FP8:
@@ -694,7 +768,9 @@ class _Types:
 
         cls.i32, cls.i64, cls.f32, cls.u8 = torch.int32, torch.int64, torch.float32, torch.uint8
         cls.floats = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
-        cls.kv = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_FP8, torch.int8: DTYPE_INT8}
+        cls.kv = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_FP8, torch.int8: DTYPE_INT8,
+                  torch.float4_e2m1fn_x2: DTYPE_FP4}
+        cls.e8m0, cls.f64 = torch.float8_e8m0fnu, torch.float64
         cls.empty, cls.grad_enabled, cls.torch = torch.empty, torch.is_grad_enabled, torch
         return cls
 
@@ -715,7 +791,7 @@ def _cache_args(T, cache: KVCache) -> KvCacheArgs:
     code = T.kv.get(k.dtype)
     if code is None or v.dtype is not k.dtype or k.dim() != 4 or not (k.is_cuda and v.is_cuda):
         raise TypeError("k and v must be [pages, page_size, heads, head_dim] bfloat16/float16/float8_e4m3fn/int8 "
-                        "device tensors of one type")
+                        "device tensors of one type (float4_e2m1fn_x2: [.., head_dim / 2])")
     if k.requires_grad or v.requires_grad:
         _refuse_gradients(T)
     shape, st = k.shape, k.stride()
@@ -727,6 +803,16 @@ def _cache_args(T, cache: KVCache) -> KvCacheArgs:
             raise TypeError("a 16-bit cache has no scales")
         return KvCacheArgs(k.data_ptr(), v.data_ptr(), None, None, pages, st[0], st[1], st[2], 0, 0, 0, size, heads, dim,
                            code)
+    if code == DTYPE_FP4:
+        if ks is None or vs is None or ks.dtype is not T.e8m0 or vs.dtype is not T.e8m0 or not (ks.is_cuda and vs.is_cuda):
+            raise TypeError("a 4-bit cache needs float8_e8m0fnu device tensors k_scale and v_scale")
+        sst = ks.stride()
+        if ks.shape != shape[:3] + (dim * 2 // KV_SCALE_GROUP,) or vs.shape != ks.shape or vs.stride() != sst \
+                or (sst[3] != 1 and ks.shape[3] > 1):
+            raise ValueError("k_scale and v_scale must be [pages, page_size, heads, head_dim / %d], with the same strides and "
+                             "unit stride along a head" % KV_SCALE_GROUP)
+        return KvCacheArgs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, st[0] * 2, st[1] * 2, st[2] * 2,
+                           sst[0], sst[1], sst[2], size, heads, dim * 2, code)
     if ks is None or vs is None or ks.dtype is not T.f32 or vs.dtype is not T.f32 or not (ks.is_cuda and vs.is_cuda):
         raise TypeError("an 8-bit cache needs float32 device tensors k_scale and v_scale")
     sst = ks.stride()
@@ -783,7 +869,7 @@ def kv_write(k, v, cache: KVCache, rows: KVRows, status=None) -> None:
     """Write the keys and values of the rows' tokens ([tokens, heads, head_dim]
     tensors) into the cache, at the last lengths[i] of row i's kv_lens[i]
     positions (asynchronous on the current stream).  8-bit caches are quantised
-    per slot and head.  status: int32[rows] that KV_BAD_* bits are added to."""
+    per slot and head, 4-bit ones per 32 values.  status: int32[rows] that KV_BAD_* bits are added to."""
     T = _types()
     ca, ra = _cache_args(T, cache), _rows_args(T, rows, k.shape[0])
     code, st, sh = _token_arrays(T, k, v, ca)
@@ -894,6 +980,194 @@ def tree_attention(q, cache: KVCache, rows: KVRows, mask=None, tree_lens=None, s
     if rc != OK:
         raise ParasonError(rc, "parason_tree_attention")
     return out if lse is None else (out, lse)
+
+
+class KVPool(NamedTuple):
+    """The pages of a cache that belong to nobody (device tensors): a stack of
+    which the first count[0] entries hold, the last of them taken first.  free
+    int32, one entry for each page of the cache; count int32 [1]."""
+
+    free: Any
+    count: Any
+
+
+def kv_pool(n_pages: int, device) -> KVPool:
+    """A pool of all pages of a cache, page 0 taken first."""
+    import torch
+
+    n = int(n_pages)
+    return KVPool(torch.arange(n - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), n, dtype=torch.int32, device=device))
+
+
+def kv_tables_workspace_size(n_rows: int) -> int:
+    return _ws_size("parason_kv_tables_workspace_size", int(n_rows))
+
+
+def _table_args(T, pool: KVPool, kv_lens, pages, lengths, page_size):
+    free, count = pool
+    for t in (free, count, kv_lens, lengths):
+        if t.dtype is not T.i32 or not t.is_cuda or not t.is_contiguous():
+            raise TypeError("free, count, kv_lens and the lengths must be contiguous int32 device tensors")
+    if pages.dtype is not T.i32 or not pages.is_cuda or pages.dim() != 2 or (pages.stride(1) != 1 and pages.shape[1] > 1):
+        raise TypeError("pages must be an int32 [rows, max_pages] device tensor, unit stride along a row")
+    n, max_pages = pages.shape
+    if kv_lens.numel() != n or lengths.numel() != n or count.numel() != 1:
+        raise ValueError("kv_lens, the lengths and pages must have the same number of rows, and count one entry")
+    return (KvPoolArgs(free.data_ptr(), count.data_ptr(), free.numel()),
+            KvTableArgs(n, kv_lens.data_ptr(), pages.data_ptr(), pages.stride(0), max_pages, int(page_size)))
+
+
+def kv_extend(pool: KVPool, lengths, kv_lens, pages, page_size: int, n_tokens: int, workspace=None) -> dict:
+    """Room for lengths[i] new tokens in every row (asynchronous on the current
+    stream): pages are taken from the pool, and pool, kv_lens (int32) and pages
+    (int32 [rows, max_pages]) updated in place.  Nothing is read on the host, so
+    n_tokens, the size of the call's token arrays, is the caller's bound of the
+    sum of the lengths.  A dict:
+
+    lengths, starts  the rows' tokens, as KVRows takes them (a row that was not
+                     served has none; starts count the wished lengths)
+    status           int32 [rows]: 0, KV_BAD_ROW or KV_NO_PAGES
+    positions, slots, rows  of every token: its position in its row (int32), its
+                     slot in the cache (int64, page * page_size + slot of the
+                     page) and its row (int32); -1 for tokens of no served row"""
+    T = _types()
+    pa, ta = _table_args(T, pool, kv_lens, pages, lengths, page_size)
+    n, n_tokens, dev = ta.n_rows, int(n_tokens), pages.device
+    if workspace is None:
+        workspace = T.empty(kv_tables_workspace_size(n), dtype=T.u8, device=dev)
+    else:
+        _check_workspace(T, workspace)
+    if n_tokens < 0:
+        raise ValueError("n_tokens must not be negative")
+    # one allocation for the 64-bit results, one for the 32-bit ones
+    wide, narrow = T.empty(n + n_tokens, dtype=T.i64, device=dev), T.empty(2 * (n + n_tokens), dtype=T.i32, device=dev)
+    starts, slots = wide.split((n, n_tokens))
+    taken, status, positions, rows = narrow.split((n, n, n_tokens, n_tokens))
+    at, to = wide.data_ptr(), narrow.data_ptr()
+    step = KvStepArgs(to, at, to + 4 * n, to + 8 * n, at + 8 * n, to + 8 * n + 4 * n_tokens)
+    rc = (_lib or lib()).parason_kv_extend(pa, ta, lengths.data_ptr(), n_tokens, step, workspace.data_ptr(), workspace.numel(),
+                                           _stream(dev))
+    if rc != OK:
+        raise ParasonError(rc, "parason_kv_extend")
+    return dict(lengths=taken, starts=starts, status=status, positions=positions, slots=slots, rows=rows)
+
+
+def kv_shrink(pool: KVPool, new_lens, kv_lens, pages, page_size: int, status=None, workspace=None) -> None:
+    """Every row gives back what is behind its first new_lens[i] positions
+    (asynchronous on the current stream): pool, kv_lens and pages are updated in
+    place, pages that go become -1.  status: int32[rows] that KV_BAD_* bits are
+    added to."""
+    T = _types()
+    pa, ta = _table_args(T, pool, kv_lens, pages, new_lens, page_size)
+    if workspace is None:
+        workspace = T.empty(kv_tables_workspace_size(ta.n_rows), dtype=T.u8, device=pages.device)
+    else:
+        _check_workspace(T, workspace)
+    rc = (_lib or lib()).parason_kv_shrink(pa, ta, new_lens.data_ptr(), _status_ptr(T, status, ta.n_rows), workspace.data_ptr(),
+                                           workspace.numel(), _stream(pages.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_kv_shrink")
+
+
+def _heads_args(T, q, k, like=None) -> HeadsArgs:
+    """Strides of query and key heads; like: (q, k) whose shapes and type they must have."""
+    qs, ks = q.stride(), k.stride()
+    if q.dim() != 3 or k.dim() != 3 or k.dtype is not q.dtype or not (q.is_cuda and k.is_cuda) \
+            or (qs[2] != 1 and q.shape[2] > 1) or (ks[2] != 1 and k.shape[2] > 1):
+        raise TypeError("queries and keys must be [tokens, heads, head_dim] device tensors of one type, unit stride along a head")
+    if like is not None and (q.shape != like[0].shape or k.shape != like[1].shape or q.dtype is not like[0].dtype):
+        raise ValueError("gradients and results must have the shapes and the type of q and k")
+    return HeadsArgs(q.data_ptr(), k.data_ptr(), qs[0], qs[1], ks[0], ks[1])
+
+
+def _rotate_args(T, q, k, positions, freqs, q_weight, k_weight, eps, interleaved) -> RotateArgs:
+    code = T.floats.get(q.dtype)
+    n, q_heads, dim = q.shape
+    if code is None:
+        raise TypeError("q and k must be float32, bfloat16 or float16")
+    if k.shape[0] != n or k.shape[2] != dim:
+        raise ValueError("q and k must have the same tokens and head_dim")
+    if positions.dtype is not T.i32 or positions.numel() != n or not positions.is_contiguous() or not positions.is_cuda:
+        raise TypeError("positions must be a contiguous int32 device tensor of one entry per token")
+    if freqs.dtype is not T.f64 or not freqs.is_contiguous() or not freqs.is_cuda:
+        raise TypeError("freqs must be a contiguous float64 device tensor")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype is not q.dtype or w.numel() != dim or not w.is_contiguous() or not w.is_cuda):
+            raise TypeError("a weight must be a contiguous device tensor of head_dim values of q's type")
+    return RotateArgs(n, q_heads, k.shape[1], dim, 2 * freqs.numel(), code, ROTATE_INTERLEAVED if interleaved else 0, float(eps),
+                      positions.data_ptr(), freqs.data_ptr(), q_weight.data_ptr() if q_weight is not None else None,
+                      k_weight.data_ptr() if k_weight is not None else None)
+
+
+def qk_norm_rotate(q, k, positions, freqs, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
+    """(q, k) with every head divided by its root mean square, weighted, and
+    rotated by its token's position (asynchronous on the current stream).
+
+    q, k      [tokens, heads, head_dim] float32/bfloat16/float16, any strides with
+              unit stride along a head (views of one packed projection, say)
+    positions int32 [tokens]; a negative one is padding, whose results are zero
+    freqs     float64 [n]: the angle of pair j is positions * freqs[j]; the first
+              2n values of a head are rotated
+    q_weight, k_weight  [head_dim] of q's type (None: ones)
+    interleaved  pairs are neighbours (2j, 2j + 1) instead of (j, j + n)
+    out       a pair of tensors to write into; (q, k) themselves: in place
+
+    The backward pass is a call of its own, qk_norm_rotate_grad: inputs that
+    require a gradient are refused here while autograd is on."""
+    T = _types()
+    xa = _heads_args(T, q, k)
+    ra = _rotate_args(T, q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
+    for t in (q, k, q_weight, k_weight, freqs) + (tuple(out) if out is not None else ()):
+        if t is not None and t.requires_grad and T.grad_enabled():
+            raise RuntimeError("no gradient flows through qk_norm_rotate: call it under torch.no_grad() and its backward pass, "
+                               "qk_norm_rotate_grad, by itself")
+    if out is None:
+        out = T.empty(q.shape, dtype=q.dtype, device=q.device), T.empty(k.shape, dtype=q.dtype, device=q.device)
+        ya = HeadsArgs(out[0].data_ptr(), out[1].data_ptr(), ra.n_q_heads * ra.head_dim, ra.head_dim, ra.n_k_heads * ra.head_dim,
+                       ra.head_dim)
+    else:
+        ya = _heads_args(T, *out, like=(q, k))
+    rc = (_lib or lib()).parason_qk_norm_rotate(ra, xa, ya, _stream(q.device))
+    if rc != OK:
+        raise ParasonError(rc, "parason_qk_norm_rotate")
+    return tuple(out)
+
+
+def qk_norm_rotate_grad(dq, dk, q, k, positions, freqs, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None,
+                        weights=True, workspace=None) -> dict:
+    """The backward pass of qk_norm_rotate: dict of the gradients q and k from
+    those of its results, dq and dk (shapes and type of q and k), and q_weight
+    and k_weight, float32 [head_dim] (weights=False: without these).  out: a pair
+    of tensors for q and k, which may be (dq, dk) or (q, k) themselves.
+    Asynchronous on the current stream."""
+    T = _types()
+    xa, ga = _heads_args(T, q, k), _heads_args(T, dq, dk, like=(q, k))
+    ra = _rotate_args(T, q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
+    dim, dev = ra.head_dim, q.device
+    if out is None:
+        out = T.empty(q.shape, dtype=q.dtype, device=dev), T.empty(k.shape, dtype=q.dtype, device=dev)
+        ya = HeadsArgs(out[0].data_ptr(), out[1].data_ptr(), ra.n_q_heads * dim, dim, ra.n_k_heads * dim, dim)
+    else:
+        ya = _heads_args(T, *out, like=(q, k))
+    b = ctypes.c_size_t()
+    rc = (_lib or lib()).parason_qk_norm_rotate_workspace_size(ra, b)
+    if rc != OK:
+        raise ParasonError(rc, "parason_qk_norm_rotate_workspace_size")
+    if workspace is None:
+        workspace = T.empty(b.value, dtype=T.u8, device=dev)
+    else:
+        _check_workspace(T, workspace)
+    res = dict(q=out[0], k=out[1])
+    dwq = dwk = None
+    if weights:
+        w = T.empty((2, dim), dtype=T.f32, device=dev)
+        res["q_weight"], res["k_weight"] = w.unbind()
+        dwq = w.data_ptr()
+        dwk = dwq + 4 * dim
+    rc = _lib.parason_qk_norm_rotate_grad(ra, xa, ga, ya, dwq, dwk, workspace.data_ptr(), workspace.numel(), _stream(dev))
+    if rc != OK:
+        raise ParasonError(rc, "parason_qk_norm_rotate_grad")
+    return res
 
 
 @functools.lru_cache(maxsize=256)

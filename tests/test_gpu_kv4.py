@@ -1,0 +1,166 @@
+"""A 4-bit cache's write and read on the GPU against the oracle: codes, scales and values bit for bit."""
+import numpy as np
+import pytest
+
+from decoding_cases import torch_type
+from gpu_util import log
+from oracle import serving_oracle as S
+from paper_2608_24658_amd import parason as PX
+from serving_cases import Paged4
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch.device("cuda:0")
+
+
+def raw(P):
+    return [t.view(torch.uint8).cpu().numpy() for t in P.kv + P.scales]
+
+
+SHAPES = [
+    # lengths, positions before them, page, heads, dim, layout
+    ([1], [0], 16, 1, 128, "heads"),
+    ([1, 1, 1, 0, 1], [0, 15, 16, 40, 1000], 16, 8, 128, "heads"),
+    ([5, 0, 37, 130], [0, 0, 27, 3], 24, 3, 64, "slots"),
+    ([300, 1], [0, 511], 1, 2, 96, "heads"),
+    ([33, 64], [100, 1], 128, 5, 32, "slots"),
+    ([7, 90], [2, 10], 100, 16, 256, "heads"),
+    ([11, 2], [2, 10], 8, 2, 192, "slots"),
+]
+
+
+@pytest.mark.parametrize("given", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_write_then_read(dev, shape, given):
+    lengths, before, page, heads, dim, layout = SHAPES[shape]
+    log("case kv4 given %s shape %d" % (given, shape))
+    lengths = np.array(lengths)
+    P = Paged4(dev, np.array(before) + lengths, page, heads, dim, "fp4", seed=shape, layout=layout, pad=16 * (shape % 2))
+    rng = np.random.default_rng(100 + shape)
+    rows, total, starts = P.rows(lengths, gap=2)
+    x = rng.standard_normal((2, total, heads, dim)) * 10.0 ** rng.integers(-6, 5, (2, total, heads, dim // 32)).repeat(32, -1)
+    x[:, :, 0, :3] = 0.0
+    # midpoints between codes, and largest values on both sides of 7 times a power of two
+    x[:, total // 2] = np.tile([0.25, -0.75, 1.25, 1.75, 2.5, -3.5, 5.0, 6.0], dim // 8)
+    x[0, total // 3, :, :] = np.tile([7.0, 0.1, -0.4, 3.0], dim // 4)
+    x[1, total // 3, :, :] = np.tile([-7.0625, 0.1, -0.4, 3.0], dim // 4)
+    if total > 4:
+        x[:, 3] = 0.0
+        x[0, 2, 0, 5], x[1, 4, heads - 1, 31] = np.inf, np.nan
+        x[:, 4, 0, :] = 2.0 ** -24 if given == "fp16" else 1e-37  # below the least scale, but for float16's smallest
+    x = torch.as_tensor(x.astype(np.float32)).to(torch_type(given))
+    flat = torch.zeros(2, total, heads, dim + 3 * (shape % 2), dtype=x.dtype, device=dev)[..., :dim]
+    flat.copy_(x)
+    k, v = flat if shape % 3 else (flat[0].clone(), flat[1].clone())
+    expect = [c.copy() for c in raw(P)]
+    status = torch.zeros(len(lengths), dtype=torch.int32, device=dev)
+    PX.kv_write(k, v, P.cache, rows, status=status)
+    for i, n in enumerate(lengths):
+        pg, slot = P.place(i, before[i] + np.arange(n))
+        for w in range(2):
+            codes, s = S.quantise4(x[w, starts[i]: starts[i] + n].float().numpy())
+            expect[w][pg, slot], expect[2 + w][pg, slot] = S.pack4(codes), s
+    for name, e, g in zip(("k", "v", "k_scale", "v_scale"), expect, raw(P)):
+        assert np.array_equal(e, g), (name, np.nonzero(e != g))
+    for to in ("fp32", "bf16", "fp16"):
+        all_rows, n, begin = P.rows(P.kv_lens, gap=1)
+        out = torch.full((2, n, heads, dim), 77.0, dtype=torch_type(to), device=dev)
+        got = PX.kv_read(P.cache, all_rows, n, torch_type(to), out=(out[0], out[1]), status=status)
+        for w in range(2):
+            want = torch.full((n, heads, dim), 77.0, dtype=torch_type(to))
+            for i, m in enumerate(P.kv_lens):
+                pg, slot = P.place(i, np.arange(m))
+                val = S.values4(S.unpack4(expect[w][pg, slot]), expect[2 + w][pg, slot])
+                want[begin[i]: begin[i] + m] = torch.from_numpy(val).to(torch_type(to))
+            same = torch.equal(torch.nan_to_num(want.float(), nan=12345.0), torch.nan_to_num(got[w].cpu().float(), nan=12345.0))
+            assert same, (to, w)
+    assert status.cpu().tolist() == [0] * len(lengths)
+
+
+def test_every_code_and_scale(dev):
+    """All 16 codes under every scale byte that a write makes, and 255, read back as float32."""
+    log("case every code")
+    cache = PX.kv_alloc(16, 16, 1, 32, torch.float4_e2m1fn_x2, dev)
+    codes = np.tile(np.arange(16, dtype=np.uint8), (256, 2))
+    scale = np.arange(256, dtype=np.uint8)
+    scale[(scale < 7) | ((scale > 252) & (scale < 255))] = 127
+    for t in (cache.k, cache.v):
+        t.view(torch.uint8).copy_(torch.from_numpy(S.pack4(codes)).view(16, 16, 1, 16))
+    for t in (cache.k_scale, cache.v_scale):
+        t.view(torch.uint8).copy_(torch.from_numpy(scale).view(16, 16, 1, 1))
+    one = lambda v, dt: torch.tensor(v, dtype=dt, device=dev)  # noqa: E731
+    rows = PX.KVRows(one([0], torch.int64), one([256], torch.int32), one([256], torch.int32), one([list(range(16))], torch.int32), 256, 256)
+    k, v = PX.kv_read(cache, rows, 256, torch.float32)
+    want = torch.from_numpy(S.values4(codes, scale[:, None]))
+    for t in (k, v):
+        assert torch.equal(torch.nan_to_num(t[:, 0].cpu(), nan=3e38), torch.nan_to_num(want, nan=3e38))
+
+
+def test_rows_and_pages_that_are_bad(dev):
+    log("case kv4 bad rows")
+    P = Paged4(dev, [20, 20, 20], 8, 2, 64, "fp4", seed=3)
+    rows, total, starts = P.rows([4] * 3)
+    x = torch.randn(total, 2, 64).to(dev)
+    kv, pages = rows.kv_lens.clone(), rows.pages.clone()
+    kv[1] = 3
+    pages[2, 2] = 10 ** 6
+    rows = rows._replace(kv_lens=kv, pages=pages)
+    before = raw(P)
+    status = torch.zeros(3, dtype=torch.int32, device=dev)
+    PX.kv_write(x, x, P.cache, rows, status=status)
+    assert status.cpu().tolist() == [0, PX.KV_BAD_ROW, PX.KV_BAD_PAGE]
+    codes, s = S.quantise4(x[:4].cpu().numpy())
+    pg, slot = P.place(0, 16 + np.arange(4))
+    for w in range(2):
+        before[w][pg, slot], before[2 + w][pg, slot] = S.pack4(codes), s
+    for b, g in zip(before, raw(P)):
+        assert np.array_equal(b, g)
+    out = torch.full((2, total, 2, 64), 5.0, device=dev)
+    PX.kv_read(P.cache, rows, total, torch.float32, out=(out[0], out[1]))
+    got = out.cpu()
+    assert torch.equal(got[0, :4], torch.from_numpy(S.values4(codes, s)))
+    assert torch.all(got[:, 4:8] == 5.0) and torch.isnan(got[:, 8:12]).all()
+
+
+def test_offsets_beyond_32_bits(dev):
+    """Pages whose bytes lie behind 2^32 of the pool's first."""
+    log("case kv4 long offsets")
+    n_pages, page, heads, dim = 600_000, 16, 4, 256
+    cache = PX.kv_alloc(n_pages, page, heads, dim, torch.float4_e2m1fn_x2, dev)
+    far = cache.k.numel() > 1 << 32
+    assert far
+    pages = torch.tensor([[n_pages - 1, 0, n_pages - 2]], dtype=torch.int32, device=dev)
+    one = lambda v, dt: torch.tensor([v], dtype=dt, device=dev)  # noqa: E731
+    rows = PX.KVRows(one(0, torch.int64), one(40, torch.int32), one(40, torch.int32), pages, 40, 40)
+    x = torch.randn(2, 40, heads, dim, device=dev)
+    PX.kv_write(x[0], x[1], cache, rows)
+    k, v = PX.kv_read(cache, rows, 40, torch.float32)
+    for g, w in ((k, x[0]), (v, x[1])):
+        assert np.array_equal(g.cpu().numpy(), S.values4(*S.quantise4(w.cpu().numpy())))
+    assert int((cache.k_scale.view(torch.uint8) != 0).sum()) == 40 * heads * dim // 32
+    q = torch.randn(1, 8, dim, device=dev, dtype=torch.bfloat16)
+    got = PX.tree_attention(q, cache, rows._replace(lengths=one(1, torch.int32), max_length=1)).cpu().double().numpy()
+    from oracle import decoding_oracle as D
+    o, _, tol, _ = D.attention(q.cpu().double().numpy(), k.cpu().double().numpy(), v.cpu().double().numpy(), D.visible(40, 1), dim ** -0.5, 7, 7)
+    assert (np.abs(got - o) <= tol).all()
+
+
+def test_refusals(dev):
+    log("case kv4 refusals")
+    c = PX.kv_alloc(4, 16, 2, 64, torch.float4_e2m1fn_x2, dev)
+    i32 = lambda *s: torch.ones(s, dtype=torch.int32, device=dev)  # noqa: E731
+    r = PX.KVRows(torch.zeros(1, dtype=torch.int64, device=dev), i32(1), i32(1), i32(1, 2), 1, 1)
+    x = torch.zeros(1, 2, 64, device=dev)
+    for bad in (PX.KVCache(c.k, c.v), PX.KVCache(c.k, c.v, c.k_scale.view(torch.uint8), c.v_scale.view(torch.uint8)),
+                PX.KVCache(c.k, c.v, c.k_scale[..., :1], c.v_scale[..., :1]), PX.KVCache(c.k, c.v, c.k_scale, c.v_scale.transpose(0, 1)),
+                PX.KVCache(c.k, c.v, torch.zeros(4, 16, 2, device=dev), torch.zeros(4, 16, 2, device=dev))):
+        with pytest.raises((TypeError, ValueError)):
+            PX.kv_write(x, x, bad, r)
+    with pytest.raises(ValueError):
+        PX.kv_write(x[..., :32], x[..., :32], c, r)

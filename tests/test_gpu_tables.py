@@ -1,0 +1,186 @@
+"""The cache's tables on the GPU against the oracle: whole numbers, all of them equal."""
+import numpy as np
+import pytest
+
+from gpu_util import log
+from oracle import serving_oracle as S
+from paper_2608_24658_amd import parason as PX
+from serving_cases import Tables
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch.device("cuda:0")
+
+
+@pytest.mark.parametrize("page", [1, 3, 16, 100])
+@pytest.mark.parametrize("rows,most", [(1, 1), (1, 4000), (7, 40), (64, 1), (65, 300), (1024, 3), (1025, 3), (300, 70)])
+def test_extend_then_shrink(dev, rows, most, page):
+    """Rows of all lengths, some without new tokens; a shrink in between, and one to the lengths before, which undoes the
+    extend."""
+    log("case tables rows %d tokens to %d pages of %d" % (rows, most, page))
+    rng = np.random.default_rng(rows + most + page)
+    kv = rng.integers(0, 4 * page + 2, rows)
+    new = rng.integers(0, most + 1, rows)
+    T = Tables(dev, kv, page, int(max(kv) + 2 * most) // page + 1, seed=page, spare=int(2 * (new // page + 1).sum()), pad=page % 3)
+    before = [t.clone() for t in (T.d_lens, T.d_pages, T.d_free, T.d_count)]
+    T.extend(new, int(new.sum()) + 17)
+    T.shrink(kv)
+    for a, b in zip(before, (T.d_lens, T.d_pages, T.d_free, T.d_count)):
+        assert torch.equal(a, b)
+    T.extend(new)
+    T.shrink(T.kv_lens - rng.integers(0, T.kv_lens + 1))
+    T.extend(rng.integers(0, most + 1, rows) * (rng.random(rows) < 0.5))
+    T.shrink(np.zeros(rows))
+    assert T.count >= sum(-(-kv // page)) and (T.pages == -1).all()
+
+
+def test_many_rows(dev):
+    """More rows than one block sums, most of them empty; a long prompt among them."""
+    log("case tables many rows")
+    rng = np.random.default_rng(0)
+    for rows in (4096, 4097, 20000):
+        kv = rng.integers(0, 9, rows)
+        new = np.where(rng.random(rows) < 0.2, rng.integers(0, 6, rows), 0)
+        new[rows // 2] = 6001
+        T = Tables(dev, kv, 8, 760, seed=1, spare=int((new // 8 + 1).sum()))
+        T.extend(new, int(new.sum()) + 1)
+        T.shrink(np.where(rng.random(rows) < 0.5, T.kv_lens // 2, T.kv_lens))
+        T.extend(np.minimum(new, 3))
+
+
+def test_no_pages_left(dev):
+    """The pool ends in the middle: rows before that are served, later ones only where they need no page."""
+    log("case no pages")
+    for rows, each in ((40, 5), (40, 300), (3000, 2)):
+        for pages in (0, 1, 7, 24):
+            kv = np.arange(rows) % 7
+            T = Tables(dev, kv, 4, 80, spare=pages)
+            new = np.where(np.arange(rows) % 3 == 1, 0, each)
+            _, want = T.extend(new)
+            assert (want["status"] == S.NO_PAGES).any()
+            T.extend(new)
+            T.shrink(np.zeros(rows))
+            assert T.count == T.free.size
+
+
+def test_rows_that_are_bad(dev):
+    """Negative lengths, rows that outgrow their table, tokens behind the arrays: reported and left as they were, with the
+    rows beside them whole."""
+    log("case bad rows")
+    for rows in (12, 2000):  # one block, and a launch of its own for the tokens
+        kv = np.full(rows, 5)
+        T = Tables(dev, kv, 4, 4, spare=3 * rows)
+        new = np.full(rows, 6)
+        new[1], new[3], new[4] = -1, 12, -(2 ** 31)
+        T.kv_lens[6] = -3
+        T.d_lens[6] = -3
+        _, want = T.extend(new, 6 * rows)
+        assert want["status"][[1, 3, 4, 6]].tolist() == [S.BAD_ROW] * 4
+        # fewer tokens than the rows have: the row that goes beyond, and all behind it
+        T = Tables(dev, kv, 4, 4, spare=3 * rows)
+        _, want = T.extend(np.full(rows, 6), 6 * (rows - 3) + 2)
+        assert want["status"].tolist() == [0] * (rows - 3) + [S.BAD_ROW] * 3
+        new = np.full(rows, 4)
+        new[2], new[5], new[6] = 6, -1, 0
+        T = Tables(dev, kv, 4, 4, spare=3 * rows)
+        T.kv_lens[7] = 17
+        T.d_lens[7] = 17
+        want = T.shrink(new)
+        assert want[[2, 5, 7]].tolist() == [S.BAD_ROW] * 3
+    # lengths whose sum passes 31 bits
+    T = Tables(dev, np.zeros(3), 4, 4, spare=3)
+    _, want = T.extend(np.array([2 ** 31 - 1, 2 ** 31 - 1, 2]), 100)
+    assert want["status"].tolist() == [S.BAD_ROW] * 3
+
+
+def test_pools_that_are_bad(dev):
+    """A count out of bounds is the nearer bound; pages for which there is no room are lost; pages that are none."""
+    log("case bad pools")
+    for count in (-5, 1000):
+        T = Tables(dev, [4, 9], 4, 8, spare=6)
+        T.count = count
+        T.d_count.fill_(count)
+        T.free[T.free < 0] = 0
+        T.d_free.copy_(torch.as_tensor(T.free))
+        T.extend([3, 3])
+    T = Tables(dev, [16, 16], 4, 8, spare=2)
+    T.count = T.free.size - 3
+    T.d_count.fill_(T.count)
+    T.pages[0, 1] = -1
+    T.d_pages[0, 1] = -1
+    want = T.shrink([0, 0])
+    assert want.tolist() == [S.BAD_PAGE, 0] or want.tolist() == [S.BAD_PAGE] * 2
+    # a row whose last page is none
+    T = Tables(dev, [6, 6], 4, 8, spare=4)
+    T.pages[0, 1] = -1
+    T.d_pages[0, 1] = -1
+    got, _ = T.extend([1, 1])
+    assert got["slots"][0] == -1
+
+
+def test_calls_without_rows_or_tokens(dev):
+    log("case empty")
+    T = Tables(dev, np.zeros(0, np.int64), 4, 3)
+    got, _ = T.extend([], 5000)
+    assert got["slots"].tolist() == [-1] * 5000
+    T.extend([], 0)
+    T.shrink([])
+    T = Tables(dev, [3, 0], 4, 3)
+    T.extend([0, 0])
+    T.extend([0, 0], 3)
+    T = Tables(dev, [0, 0], 4, 0)
+    T.extend([0, 0])
+    T.extend([1, 0])
+    T.shrink([0, 0])
+
+
+def test_tokens_that_nobody_asks_for(dev):
+    """Through the C call: token arrays that are NULL are not written, and the status neither."""
+    log("case no token arrays")
+    for rows in (5, 1500):
+        T = Tables(dev, np.full(rows, 3), 4, 4, spare=2 * rows)
+        lengths = torch.full((rows,), 2, dtype=torch.int32, device=dev)
+        starts, ws = torch.empty(rows, dtype=torch.int64, device=dev), torch.empty(PX.kv_tables_workspace_size(rows), dtype=torch.uint8, device=dev)
+        pa, ta = PX._table_args(PX._types(), T.pool, T.d_lens, T.d_pages, lengths, 4)
+        # the wished lengths may be the array of the served ones
+        step = PX.KvStepArgs(lengths.data_ptr(), starts.data_ptr(), None, None, None, None)
+        rc = PX.lib().parason_kv_extend(pa, ta, lengths.data_ptr(), 2 * rows, step, ws.data_ptr(), ws.numel(), PX._stream(dev))
+        assert rc == PX.OK
+        T.count, want = S.extend(T.free, T.count, T.kv_lens, T.pages, np.full(rows, 2), 4, 2 * rows)
+        T.check()
+        assert lengths.tolist() == [2] * rows
+
+
+def test_in_a_graph(dev):
+    """A captured step, replayed: every replay moves the state on by one step."""
+    log("case graph")
+    for rows in (16, 3000):
+        T = Tables(dev, np.arange(rows) % 9, 4, 40, spare=8 * rows)
+        new = torch.as_tensor(np.arange(rows) % 5).to(device=dev, dtype=torch.int32)
+        n, ws = int(new.sum()) + 3, torch.empty(PX.kv_tables_workspace_size(rows), dtype=torch.uint8, device=dev)
+        kept = torch.zeros(rows, dtype=torch.int32, device=dev)
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(s), torch.cuda.graph(g, stream=s):
+            torch.sub(T.d_lens, 1, out=kept).clamp_(min=0)
+            PX.kv_shrink(T.pool, kept, T.d_lens, T.d_pages, 4, workspace=ws)
+            got = PX.kv_extend(T.pool, new, T.d_lens, T.d_pages, 4, n, workspace=ws)
+        for _ in range(3):
+            for t in got.values():
+                t.fill_(77)
+            ws.fill_(0xFF)
+            (torch.randn(1000, device=dev) * 2).sum().item()
+            g.replay()
+            torch.cuda.synchronize()
+            T.count = S.shrink(T.free, T.count, T.kv_lens, T.pages, np.maximum(T.kv_lens - 1, 0), 4, np.zeros(rows, np.uint32))
+            T.count, want = S.extend(T.free, T.count, T.kv_lens, T.pages, new.cpu().numpy(), 4, n)
+            T.check()
+            for k, w in want.items():
+                assert np.array_equal(got[k].cpu().numpy().view(w.dtype), w), k
