@@ -63,12 +63,13 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
     if (filled < base) base = filled;
     const int64_t tile = p->cols < 128 ? 128 : 64;
     /* Enough blocks to fill the device, and for few columns, whose partial results are small, parts short enough that
-     * long rows among short ones do not finish last.  A part is worth its results: 8 bytes a column and value, written
+     * long rows among short ones do not finish last (4-bit positions are half as long as 8-bit ones, so that a part's
+     * beginning and end weigh more: 128 single tokens 247 us in parts of 4,096, 278 in parts of 1,024).  A part is worth its results: 8 bytes a column and value, written
      * and read, against 2 to 4 bytes a position and value.  24 parts of prompts of 2 to 300 tokens behind 1 to 18,000
      * positions, all blocks the longest row would need counted: 247 us, which is the longest row's; those with
      * columns: 147. */
     const int64_t shortest = p->cols < 128 ? 512 : 1024;
-    int64_t len = p->cols < 128 ? 1024 : 4096;
+    int64_t len = p->cols < 128 && c->dtype != PARASON_DTYPE_FP4 ? 1024 : 4096;
     while (len > shortest && base * ((r->max_kv_len + len - 1) / len) < PART_BLOCKS) len /= 2;
     const size_t per_part = (size_t)r->n_tokens * n_q_heads * c->head_dim * 4;
     int64_t parts = (r->max_kv_len + len - 1) / len;
@@ -154,6 +155,8 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
     const float c2 = (float)(std::fabs((double)args->scale) * 1.4426950408889634);
     a.c2 = c2 > 0x1p-126f ? c2 : 0x1p-126f;
     a.q_blocks = p.q_blocks, a.parts = p.parts, a.part_len = p.part_len;
+    a.q_blocks_div = pk::fast_div((uint32_t)p.q_blocks), a.parts_div = pk::fast_div((uint32_t)p.parts);
+    a.heads_div = pk::fast_div((uint32_t)cache->n_heads), a.part_len_div = pk::fast_div((uint32_t)p.part_len);
     a.r.max_length = p.max_length;
     a.part_out = (float *)workspace;
     a.part_ml = (float2 *)((char *)workspace + p.ml);
@@ -167,14 +170,16 @@ int parason_tree_attention(const parason_kv_cache *cache, const parason_kv_rows 
         if (b.r.pages) b.r.pages += i * b.r.pages_stride;
         if (b.r.status) b.r.status += i;
         if (b.tree_lens) b.tree_lens += i;
-        b.units = b.r.n_rows * cache->n_heads * p.parts;
+        b.units = (uint32_t)(b.r.n_rows * cache->n_heads * p.parts);
         b.by_xcd = p.q_blocks > 1 && b.units >= 8;
-        const int64_t blocks = (b.by_xcd ? (b.units + 7) / 8 * 8 : b.units) * p.q_blocks;
+        const int64_t blocks = (int64_t)(b.by_xcd ? (b.units + 7) / 8 * 8 : b.units) * p.q_blocks;
         hipLaunchKernelGGL(f, dim3((unsigned)blocks), dim3(pk::TREE_THREADS), 0, stream, b);
     }
     if (p.parts > 1) {
         constexpr int64_t per_block = pk::TREE_THREADS / 64;
+        /* (2^26 waves at most, and so many tokens and heads of a row) */
         const int64_t waves = rows->n_rows * p.max_length * heads;
+        a.row_div = pk::fast_div((uint32_t)(p.max_length * heads)), a.q_heads_div = pk::fast_div((uint32_t)heads);
         hipLaunchKernelGGL(f16 ? pk::tree_join<true> : pk::tree_join<false>, dim3((unsigned)((waves + per_block - 1) / per_block)),
                            dim3(pk::TREE_THREADS), 0, stream, a, p.cols);
     }

@@ -46,7 +46,9 @@ struct TreeArgs {
     int32_t q_blocks;    /* blocks of columns of a row and head */
     int32_t parts;       /* parts of a row's positions, part_len each (the last block of a row: the rest) */
     int32_t part_len;
-    int64_t units;       /* rows * cache heads * parts */
+    uint32_t units;      /* rows * cache heads * parts */
+    FastDiv q_blocks_div, parts_div, heads_div, part_len_div;
+    FastDiv row_div, q_heads_div; /* tree_join: by max_length * n_q_heads, by n_q_heads */
     bool by_xcd;
     float *part_out;     /* [n_tokens * n_q_heads][parts][head_dim] */
     float2 *part_ml;     /* [n_tokens * n_q_heads][parts]: exponent of the maximum, sum */
@@ -127,18 +129,21 @@ __device__ __forceinline__ frag8 widen8(uint2 w)
     return __builtin_bit_cast(frag8, make_uint4(a.x, a.y, b.x, b.y));
 }
 
-/* A piece of a 4-bit cache, 32 codes and their power of two, to four operands' worth of bfloat16: exact. */
-__device__ __forceinline__ void widen32(u32x4 w, float scale, frag8 *to)
+/* Eight codes of a 4-bit cache and their power of two to the operand of a product: exact in bfloat16. */
+__device__ __forceinline__ frag8 widen8_fp4(uint32_t c, float scale)
 {
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+    const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+    const uint32_t z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+    const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+    return __builtin_bit_cast(frag8, make_uint4(x, y, z, w));
+}
+
+/* A piece of 32 codes to LDS as 16-bit values. */
+__device__ __forceinline__ void put32_fp4(char *to, u32x4 w, float scale)
+{
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t c = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
-        const b2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
-        const b2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
-        to[i] = __builtin_bit_cast(frag8, make_uint4(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1),
-                                                     __builtin_bit_cast(uint32_t, x2), __builtin_bit_cast(uint32_t, x3)));
-    }
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<frag8 *>(to + 16 * i) = widen8_fp4(w[i], scale);
 }
 
 /* A word of V without its infinities and NaN, which become zeros. */
@@ -153,6 +158,19 @@ __device__ __forceinline__ uint32_t finite_word(uint32_t w)
     }
     const uint32_t e = KIND == KV_F16 ? 0x7C00u : 0x7F80u;
     return w & (((w & e) != e ? 0x0000FFFFu : 0u) | (((w >> 16) & e) != e ? 0xFFFF0000u : 0u));
+}
+
+/* The maximum over the lanes of a column, 16 or 32 and 32 apart. */
+template <int CN>
+__device__ __forceinline__ float column_max(float x)
+{
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    if (CN == 16) {
+        const u2 y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+    }
+    const u2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
 }
 
 /* A value of the cache. */
@@ -180,6 +198,9 @@ struct TreeShape {
     /* Codes go to LDS as they are where one wave reads them again, and are widened behind it; where all four waves take
      * the same positions they are widened once, in front. */
     static constexpr bool RAW = CODES && SOLO;
+    /* 4-bit keys of few columns stay in registers: a lane loads the codes of its row of the products (the same share of
+     * the head for all of them, in the order that it has the queries in), 8 to 64 bytes next to each other. */
+    static constexpr bool DIRECT = FOUR && SOLO;
     /* columns of a product, CN x CN results; the 64 / CN lanes of a column hold these positions of 32:
      * KSTEP * (i / 4) + 4 * (lane / CN) + i % 4, and these rows of O^T of CN: 8 * (i / 4) + 4 * (lane / CN) + i % 4 */
     static constexpr int CN = COLS == 16 ? 16 : 32, G = 64 / CN, NV = 32 / G, KSTEP = 128 / NV;
@@ -190,14 +211,16 @@ struct TreeShape {
     static constexpr int KW = TK / WK;                /* of it, those of one wave */
     static constexpr int SUBS = KW / 32;
     /* rows in LDS: 16 bytes more than a multiple of 128 spread the reads of K over the banks, 64 bytes more the
-     * transposed reads of 16-bit V */
+     * transposed reads of 16-bit V.  4-bit V arrives in pieces of 32 values, so that four lanes write one row at
+     * distances of 64 bytes: 16 or 32 bytes more spread the next row's over the banks between them, and the transposed
+     * reads too (with 64 more, conflicts were a third of a step's time: 128 single tokens 267 us, without 247). */
     static constexpr int ES = RAW ? 1 : 2;            /* bytes of a value in LDS */
-    static constexpr int KS = RAW ? DP + 16 : DP + 8, VS = RAW ? DP + 16 : DP + 32; /* values */
-    static constexpr int KBYTES = TK * KS * ES, VBYTES = TK * VS * ES;
+    static constexpr int KS = RAW ? DP + 16 : DP + 8, VS = RAW ? DP + 16 : FOUR ? DP + (DP <= 64 ? 8 : 16) : DP + 32; /* values */
+    static constexpr int KBYTES = DIRECT ? 0 : TK * KS * ES, VBYTES = TK * VS * ES;
     static constexpr int OS = DP + 4;                 /* floats of a row of the waves' results when they are joined */
     static constexpr int JOIN = (WK - 1) * COLS * OS * 4;
     /* blocks that a CU holds: by LDS, or by registers */
-    static constexpr int BLOCKS = DP > 128 ? (COLS == 16 && RAW ? 2 : 1) : COLS > 16 ? (DP <= 64 && COLS == 32 ? 3 : 2) : RAW ? (DP <= 64 ? 4 : 3) : DP <= 64 ? 3 : 2;
+    static constexpr int BLOCKS = DIRECT ? (DP <= 64 ? 4 : DP <= 128 ? 3 : 2) - (COLS > 16) : DP > 128 ? (COLS == 16 && RAW ? 2 : 1) : COLS > 16 ? (DP <= 64 && COLS == 32 ? 3 : 2) : RAW ? (DP <= 64 ? 4 : 3) : DP <= 64 ? 3 : 2;
     static constexpr int TILE = KBYTES + VBYTES > JOIN ? KBYTES + VBYTES : JOIN;
 };
 
@@ -226,7 +249,8 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs &a, const KvRow &w,
 
 __device__ __forceinline__ int32_t parts_of(const TreeArgs &a, int32_t end)
 {
-    const int32_t n = (int32_t)(((int64_t)end + a.part_len - 1) / a.part_len);
+    const uint32_t q = div_by((uint32_t)end, a.part_len_div);
+    const int32_t n = (int32_t)(q + (q * (uint32_t)a.part_len < (uint32_t)end));
     return n < 1 ? 1 : n < a.parts ? n : a.parts;
 }
 
@@ -237,9 +261,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     constexpr int CN = Sh::CN, G = Sh::G, NV = Sh::NV, KSTEP = Sh::KSTEP, AC = Sh::AC, WQ = Sh::WQ;
     typedef typename Acc<CN>::type acc;
     constexpr int TK = Sh::TK, KS = Sh::KS, VS = Sh::VS, SUBS = Sh::SUBS;
-    constexpr bool CODES = Sh::CODES, RAW = Sh::RAW, FOUR = Sh::FOUR;
-    /* Type of the keys where they meet the queries.  A 4-bit cache's are bfloat16 (float16 does not hold all of its
-     * scales), and float16 queries two bfloat16 terms, which is all of them. */
+    constexpr bool CODES = Sh::CODES, RAW = Sh::RAW, FOUR = Sh::FOUR, DIRECT = Sh::DIRECT;
+    /* Type of the keys where they meet the queries.  A 4-bit cache's are bfloat16, exact (float16 does not hold all of its
+     * scales), and float16 queries two bfloat16 terms, which is all of them.  (Keys relative to the largest scale of their
+     * position, which fit float16 but for the smallest values, took no less: 26 draft tokens of 48 rows 233 us, this 232.) */
     constexpr bool SF16 = F16 && !FOUR, TWO = F16 && FOUR;
     /* Type of the weights and of V: bfloat16 for codes, whose scales are in the weights.  The weights are rounded to it for
      * the matrix product: 2^-9 of each, against which a result of the same type is rounded by as much once more (bfloat16
@@ -261,7 +286,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
 
     __shared__ __attribute__((aligned(16))) char tile[Sh::TILE];
     __shared__ __attribute__((aligned(16))) float k_sc[CODES ? TK : 4], v_sc[CODES ? TK : 4];
-    __shared__ int64_t place[TK], scale_place[FOUR ? TK : 1];
+    __shared__ int64_t place[TK], /* bytes */ scale_place[FOUR ? TK : 1];
     __shared__ int32_t v_stamp[TK];
     __shared__ uint32_t skip[TREE_SKIP_WORDS];
     __shared__ int32_t flags[2];            /* a bad page; the last tile with a value of V that is not finite (of the block) */
@@ -274,22 +299,21 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     const int wq = wave % WQ, wk = wave / WQ, k0 = wk * Sh::KW;
 
     /* ---- which row, cache head, part and columns */
-    int64_t unit;
+    /* (products instead of divisions: many blocks of a ragged call find nothing to do, and this is all they cost) */
+    uint32_t unit;
     int32_t q_block;
-    if (a.by_xcd) {
-        /* blocks that read the same keys on one XCD's L2 */
-        const uint32_t x = blockIdx.x & 7u, y = blockIdx.x >> 3;
-        unit = (int64_t)(y / (uint32_t)a.q_blocks) * 8 + x;
-        q_block = (int32_t)(y % (uint32_t)a.q_blocks);
-    } else {
-        unit = blockIdx.x / (uint32_t)a.q_blocks;
-        q_block = (int32_t)(blockIdx.x % (uint32_t)a.q_blocks);
+    {
+        const uint32_t y = a.by_xcd ? blockIdx.x >> 3 : blockIdx.x;
+        const uint32_t u = div_by(y, a.q_blocks_div);
+        unit = a.by_xcd ? u * 8 + (blockIdx.x & 7u) : u; /* blocks that read the same keys on one XCD's L2 */
+        q_block = (int32_t)(y - u * (uint32_t)a.q_blocks);
     }
     if (unit >= a.units) return;
     q_block = a.q_blocks - 1 - q_block;     /* the longest of a chain first */
-    const int32_t part = (int32_t)(unit % a.parts);
-    const int32_t head = (int32_t)(unit / a.parts % a.c.n_heads);
-    const int64_t row = unit / a.parts / a.c.n_heads;
+    const uint32_t row_head = div_by(unit, a.parts_div);
+    const int32_t part = (int32_t)(unit - row_head * (uint32_t)a.parts);
+    const int64_t row = div_by(row_head, a.heads_div);
+    const int32_t head = (int32_t)(row_head - (uint32_t)row * (uint32_t)a.c.n_heads);
     const KvRow w = load_row(a.r, a.c, row, false);
     const TreeSpan sp = tree_span(a, w, row, q_block, COLS);
     if (!sp.ok && part == 0 && head == 0 && q_block == 0 && tid == 0) report(a.r, row, PARASON_KV_BAD_ROW);
@@ -311,7 +335,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + t * a.q_stride_token + (live ? q_head : 0) * a.q_stride_head;
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-            const int d = k * KD + h * 8;
+            const int d = DIRECT ? h * (DP / G) + k * 8 : k * KD + h * 8;
             uint4 x = make_uint4(0u, 0u, 0u, 0u);
             if (live && d < a.c.head_dim) {
                 if (a.q_wide) {
@@ -324,17 +348,17 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                 if (a.negate) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
             }
             if (TWO) {
-                uint32_t w[4] = {x.x, x.y, x.z, x.w}, r[4];
+                uint32_t y[4] = {x.x, x.y, x.z, x.w}, z[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float a0 = f16_to_f32(w[i] & 0xFFFFu), a1 = f16_to_f32(w[i] >> 16);
-                    w[i] = pack2<false>(a0, a1);
+                    const float e0 = f16_to_f32(y[i] & 0xFFFFu), e1 = f16_to_f32(y[i] >> 16);
+                    y[i] = pack2<false>(e0, e1);
+                    const float r0 = e0 - __uint_as_float(y[i] << 16), r1 = e1 - __uint_as_float(y[i] & 0xFFFF0000u);
                     /* (an infinity is all in the first term) */
-                    const float r0 = a0 - __uint_as_float(w[i] << 16), r1 = a1 - __uint_as_float(w[i] & 0xFFFF0000u);
-                    r[i] = pack2<false>(fabsf(a0) < INFINITY ? r0 : 0.0f, fabsf(a1) < INFINITY ? r1 : 0.0f);
+                    z[i] = pack2<false>(fabsf(e0) < INFINITY ? r0 : 0.0f, fabsf(e1) < INFINITY ? r1 : 0.0f);
                 }
-                qf_rest[k] = __builtin_bit_cast(frag8, make_uint4(r[0], r[1], r[2], r[3]));
-                x = make_uint4(w[0], w[1], w[2], w[3]);
+                x = make_uint4(y[0], y[1], y[2], y[3]);
+                qf_rest[k] = __builtin_bit_cast(frag8, make_uint4(z[0], z[1], z[2], z[3]));
             }
             qf[k] = __builtin_bit_cast(frag8, x);
         }
@@ -392,10 +416,14 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     /* ---- loads: a position's page a tile ahead of its keys and values, these a tile ahead of their use */
     const int32_t loader = Sh::SOLO ? lane : tid, row0 = Sh::SOLO ? k0 : 0; /* who loads what of a tile */
     const bool loads = LOADERS / VPR <= ROWS || loader < ROWS * VPR; /* (fewer pieces than lanes) */
-    const int32_t my_piece = loader % VPR, my_row = row0 + (loads ? loader / VPR : 0);
+    /* (4-bit heads of 256 values: their pieces beyond the fourth by other lanes, see the rows in LDS) */
+    constexpr bool FOLD = FOUR && VPR == 8;
+    const int32_t my_piece = FOLD ? (loader & 3) + ((loader & 32) >> 3) : loader % VPR;
+    const int32_t my_row = row0 + (FOLD ? (loader >> 6) * 8 + ((loader >> 2) & 7) : loads ? loader / VPR : 0);
     const bool piece_live = loads && my_piece * VE < a.c.head_dim;
     const int64_t piece_at = (int64_t)head * a.c.stride_head + (piece_live ? my_piece * VE : 0);
     const char *const kb = a.c.k + cache_bytes<KIND>(piece_at), *const vb = a.c.v + cache_bytes<KIND>(piece_at);
+    const char *const khead = a.c.k + cache_bytes<KIND>((int64_t)head * a.c.stride_head);
     auto together = [&]() {                  /* what a loader put into LDS is there for the others */
         if (!Sh::SOLO) {
             __syncthreads();
@@ -418,24 +446,42 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     auto put_place = [&]() {
         if (loader >= ROWS) return;
         if (pg < 0 || pg >= a.c.n_pages) flags[0] = 0, pg = pg_slot = 0;
-        place[row0 + loader] = (int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot;
+        place[row0 + loader] = cache_bytes<KIND>((int64_t)pg * a.c.stride_page + (int64_t)pg_slot * a.c.stride_slot);
         if (CODES || FOUR)
             scale_at = (int64_t)pg * a.c.scale_stride_page + (int64_t)pg_slot * a.c.scale_stride_slot +
                        (int64_t)head * a.c.scale_stride_head;
         if (FOUR) scale_place[row0 + loader] = scale_at;
     };
-    u32x4 kr[NP], vr[NP];
-    uint32_t k_byte[FOUR ? NP : 1], v_byte[FOUR ? NP : 1]; /* the pieces' scales */
+    /* DIRECT: of each CN rows of keys this lane has one, KL codes of it from h * KL on */
+    constexpr int KL = DP / G, KN = DIRECT ? Sh::KW / CN * (KL < 32 ? 1 : KL / 32) : NP;
+    u32x4 kr[KN], vr[NP];
+    uint32_t k_byte[FOUR ? KN : 1], v_byte[FOUR ? NP : 1]; /* the pieces' scales */
     float k_scale = 0.0f, v_scale = 0.0f;    /* of position row0 + loader */
     auto load_tile = [&]() {
+        if (DIRECT) {
+            constexpr int EACH = KL < 32 ? 1 : KL / 32; /* pieces of a row */
+#pragma unroll
+            for (int i = 0; i < KN; ++i) {
+                const int r = k0 + i / EACH * CN + n;
+                const int first = h * KL + i % EACH * 32, d = first < a.c.head_dim ? first : 0;
+                const char *from = khead + (place[r] + d / 2);
+                if (KL < 32) {
+                    const uint2 c = *reinterpret_cast<const uint2 *>(from);
+                    kr[i].x = c.x, kr[i].y = c.y;
+                } else {
+                    kr[i] = *reinterpret_cast<const u32x4 *>(from);
+                }
+                k_byte[i] = reinterpret_cast<const uint8_t *>(a.c.k_scale)[scale_place[r] + d / 32];
+            }
+        }
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int64_t from = place[my_row + p * RPP];
-            kr[p] = *reinterpret_cast<const u32x4 *>(kb + cache_bytes<KIND>(from));
-            vr[p] = *reinterpret_cast<const u32x4 *>(vb + cache_bytes<KIND>(from));
+            if (!DIRECT) kr[p] = *reinterpret_cast<const u32x4 *>(kb + from);
+            vr[p] = *reinterpret_cast<const u32x4 *>(vb + from);
             if (FOUR) {
                 const int64_t at = scale_place[my_row + p * RPP] + (piece_live ? my_piece : 0);
-                k_byte[p] = reinterpret_cast<const uint8_t *>(a.c.k_scale)[at];
+                if (!DIRECT) k_byte[p] = reinterpret_cast<const uint8_t *>(a.c.k_scale)[at];
                 v_byte[p] = reinterpret_cast<const uint8_t *>(a.c.v_scale)[at];
             }
         }
@@ -474,6 +520,17 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         /* ---- the tile goes to LDS; the next page's places (nobody reads the last ones any more) */
         put_place();
         if (CODES && loader < ROWS) k_sc[row0 + loader] = k_scale, v_sc[row0 + loader] = v_scale;
+        u32x4 kc[DIRECT ? KN : 1];           /* this tile's keys */
+        uint32_t kc_byte[DIRECT ? KN : 1];
+        if (DIRECT) {
+            constexpr int EACH = KL < 32 ? 1 : KL / 32;
+#pragma unroll
+            for (int i = 0; i < KN; ++i) {
+                /* (behind the head, where the queries are zero: next to nothing, whatever was read) */
+                kc[i] = kr[i];
+                kc_byte[i] = h * KL + i % EACH * 32 < a.c.head_dim ? k_byte[i] : 0u;
+            }
+        }
         bool odd_seen = false;
         if (masked && KIND != KV_INT8) {
             /* infinities and NaN of V reach only the queries that see them, for which a product by zero would not do:
@@ -497,19 +554,16 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                 vr[p] = f;
             }
         }
-        if (piece_live) {
+        /* (DIRECT: what lies behind the head goes where only results behind it come from; a branch here would make every
+         * load below wait for the ones that it leaves out) */
+        if (DIRECT || piece_live) {
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
                 const int r = my_row + p * RPP;
                 char *const kd = Ks + (r * KS + my_piece * VE) * LS, *const vd = Vs + (r * VS + my_piece * VE) * LS;
                 if (FOUR) {
-                    frag8 wide[4];
-                    widen32(kr[p], fp4_scale(k_byte[p]), wide);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) *reinterpret_cast<frag8 *>(kd + 16 * i) = wide[i];
-                    widen32(vr[p], fp4_scale(v_byte[p]), wide);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) *reinterpret_cast<frag8 *>(vd + 16 * i) = wide[i];
+                    if (!DIRECT) put32_fp4(kd, kr[p], fp4_scale(k_byte[p]));
+                    put32_fp4(vd, vr[p], fp4_scale(v_byte[p]));
                     __builtin_amdgcn_sched_barrier(0);
                 } else if (CODES && !RAW) {
                     *reinterpret_cast<frag8 *>(kd) = widen8<F16, KIND>(make_uint2(kr[p].x, kr[p].y));
@@ -555,12 +609,24 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             }
         };
         u32x4 kf[KSTEPS + 1][KG];
-        read_keys(0, kf[0]);
+        if (!DIRECT) read_keys(0, kf[0]);
         acc c[KROWS];
 #pragma unroll
         for (int i = 0; i < KROWS; ++i) c[i] = acc{};
+        if (DIRECT) {
+            constexpr int EACH = KL < 32 ? 1 : KL / 32;
 #pragma unroll
-        for (int g = 0; g < KSTEPS; ++g) {
+            for (int k = 0; k < NK; ++k)
+#pragma unroll
+                for (int i = 0; i < KROWS; ++i) {
+                    const int at = i * EACH + k / 4;
+                    const frag8 f = widen8_fp4(kc[at][k % 4], fp4_scale(kc_byte[at]));
+                    c[i] = mma<SF16>(f, qf[k], c[i]);
+                    if (TWO) c[i] = mma<SF16>(f, qf_rest[k], c[i]);
+                }
+        }
+#pragma unroll
+        for (int g = 0; g < (DIRECT ? 0 : KSTEPS); ++g) {
             if (g + 1 < KSTEPS) read_keys(g + 1, kf[g + 1]);
 #pragma unroll
             for (int j = 0; j < KG; ++j) {
@@ -624,8 +690,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
             for (int r = 0; r < NV; ++r) top = fmaxf(top, s[u][r]);
-#pragma unroll
-        for (int k = CN; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+        top = column_max<CN>(top);
         /* Exponents beyond FAR are rounded by more than a weight bears (the largest would be 2^(LIFT + 1) or, further on,
          * infinite or nothing): they are rounded down, and the weights that this takes over 2^LIFT are 2^LIFT, which
          * makes equal what the scores' own rounding does not tell apart for certain. */
@@ -851,12 +916,12 @@ template <bool F16>
 __global__ void __launch_bounds__(TREE_THREADS) tree_join(TreeArgs a, int cols)
 {
     const int lane = (int)threadIdx.x & 63;
-    const int64_t per_row = (int64_t)a.r.max_length * a.n_q_heads;
-    const int64_t i = (int64_t)blockIdx.x * (TREE_THREADS / 64) + (threadIdx.x >> 6);
-    const int64_t row = i / per_row;
+    const uint32_t i = blockIdx.x * (TREE_THREADS / 64) + (threadIdx.x >> 6);
+    const uint32_t r0 = div_by(i, a.row_div);
+    const int64_t row = r0;
     if (row >= a.r.n_rows) return;
-    const int32_t tok = (int32_t)((uint32_t)(i - row * per_row) / (uint32_t)a.n_q_heads);
-    const int32_t q_head = (int32_t)(i - row * per_row - (int64_t)tok * a.n_q_heads);
+    const uint32_t in = i - r0 * (uint32_t)(a.r.max_length * a.n_q_heads);
+    const int32_t tok = (int32_t)div_by(in, a.q_heads_div), q_head = (int32_t)(in - (uint32_t)tok * (uint32_t)a.n_q_heads);
     const KvRow w = load_row(a.r, a.c, row, false);
     if (!w.out_ok || tok >= w.length) return;
     const int32_t col = tok * a.group + q_head % a.group;
