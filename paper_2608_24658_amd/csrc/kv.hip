@@ -67,7 +67,7 @@ int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void 
     a.group = 1, a.group_log = 0;
     while (a.group * pk::KV_PER_LANE < cache->head_dim) a.group <<= 1, ++a.group_log;
     a.heads_div = pk::fast_div((uint32_t)cache->n_heads);
-    const int64_t per_block = pk::KV_THREADS / a.group * (write ? pk::KV_WRITES : pk::KV_READS);
+    const int64_t per_block = pk::KV_THREADS / a.group * (write ? pk::KV_WRITES : kind == pk::KV_FP4 ? pk::KV_READS4 : pk::KV_READS);
     int64_t blocks = (units + per_block - 1) / per_block, most = MOVE_BLOCKS / rows->n_rows;
     if (most < 1) most = 1; /* (as many blocks as rows) */
     if (blocks > most) blocks = most;

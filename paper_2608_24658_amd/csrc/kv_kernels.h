@@ -21,6 +21,9 @@ constexpr int KV_PER_LANE = 8;  /* values */
 /* Units of a lane on their way at once: a unit's page is a load that its values wait for, so one at a time leaves the
  * memory idle.  48 rows of 1 to 36,000 positions read from FP8: 390 us with one, 260 with these. */
 constexpr int KV_WRITES = 2, KV_READS = 4;
+constexpr int KV_READS4 = 4; /* of a 4-bit cache, whose loads are a quarter of its stores */
+template <int KIND>
+constexpr int kv_reads() { return KIND == KV_FP4 ? KV_READS4 : KV_READS; }
 
 struct KvMoveArgs {
     KvCache c;
@@ -227,20 +230,21 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
+    constexpr int READS = kv_reads<KIND>();
     constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8 || KIND == KV_FP4;
     const int lane = (int)threadIdx.x & (a.group - 1);
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.c.n_heads;
     const int lo = piece_lo<T, KIND>(lane), hi = piece_hi<T, KIND>(lane, a.group);
     if (lo >= a.c.head_dim) return;
     const bool hi_live = hi < a.c.head_dim;
-    for (int64_t u0 = part * step * KV_READS; u0 < units; u0 += a.blocks_per_row * step * KV_READS) {
-        KvUnit x[KV_READS];
-        uint4 raw[KV_READS];
-        float scale[KV_READS];
+    for (int64_t u0 = part * step * READS; u0 < units; u0 += a.blocks_per_row * step * READS) {
+        KvUnit x[READS];
+        uint4 raw[READS];
+        float scale[READS];
 #pragma unroll
-        for (int i = 0; i < KV_READS; ++i) x[i] = kv_unit(a, row, w, u0 + i * step + (threadIdx.x >> a.group_log), units);
+        for (int i = 0; i < READS; ++i) x[i] = kv_unit(a, row, w, u0 + i * step + (threadIdx.x >> a.group_log), units);
 #pragma unroll
-        for (int i = 0; i < KV_READS; ++i) {
+        for (int i = 0; i < READS; ++i) {
             raw[i] = make_uint4(0u, 0u, 0u, 0u);
             scale[i] = __uint_as_float(0x7FC00000u);
             if (x[i].page < 0) {
@@ -280,7 +284,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
             }
         }
 #pragma unroll
-        for (int i = 0; i < KV_READS; ++i) {
+        for (int i = 0; i < READS; ++i) {
             if (u0 + i * step + (threadIdx.x >> a.group_log) >= units) continue;
             float f[8];
             if (!CODES) {

@@ -70,12 +70,27 @@ int check(const parason_rotate *r, pk::RotArgs *a)
     a->eps = r->eps, a->inv_dim = 1.0f / (float)a->dim;
     a->positions = r->positions, a->freqs = r->freqs;
     a->q_weight = (const char *)r->q_weight, a->k_weight = (const char *)r->k_weight;
-    /* as many tokens as give each thread an angle, but enough blocks */
-    int64_t n = a->half > 0 ? pk::ROT_TURNS / a->half : pk::ROT_TOKENS;
-    if (n > pk::ROT_TOKENS) n = pk::ROT_TOKENS;
-    if (n > a->n_tokens / 1024) n = a->n_tokens / 1024;
-    a->at_once = n > 1 ? (int32_t)n : 1;
     return PARASON_OK;
+}
+
+/* Tokens of a block at a time, at most as many as the block's table of angles holds.  Forward: as many as give each
+ * thread an angle, but enough blocks.  Backward: all blocks get the same number, in as few rounds as that takes, but
+ * at least a head for each group of lanes. */
+int32_t tokens_at_once(const pk::RotArgs &a, bool grad)
+{
+    int64_t most = a.half > 0 ? pk::ROT_TURNS / a.half : pk::ROT_TOKENS;
+    if (most > pk::ROT_TOKENS) most = pk::ROT_TOKENS;
+    int64_t n = a.n_tokens / 1024;
+    if (grad) {
+        const int64_t blocks = pk::ROT_GRAD_BLOCKS, rounds = (a.n_tokens + blocks * most - 1) / (blocks * most);
+        n = rounds > 0 ? (a.n_tokens + blocks * rounds - 1) / (blocks * rounds) : 1;
+        const int64_t groups = pk::ROT_THREADS >> a.group_log, heads = a.q_heads + a.k_heads;
+        if (n * heads < groups) n = heads > 0 ? (groups + heads - 1) / heads : most;
+    } else if (a.half > 0 && most > (pk::ROT_THREADS + a.half - 1) / a.half) {
+        most = (pk::ROT_THREADS + a.half - 1) / a.half;
+    }
+    if (n > most) n = most;
+    return n > 1 ? (int32_t)n : 1;
 }
 
 int64_t grad_blocks(int64_t n_tokens) { return n_tokens < pk::ROT_GRAD_BLOCKS ? n_tokens : pk::ROT_GRAD_BLOCKS; }
@@ -99,6 +114,7 @@ int parason_qk_norm_rotate(const parason_rotate *r, const parason_heads *x, cons
     if (rc == PARASON_OK) rc = check_heads(r, x, &a.x);
     if (rc == PARASON_OK) rc = check_heads(r, y, &a.y);
     if (rc != PARASON_OK) return rc;
+    a.at_once = tokens_at_once(a, false);
     const int64_t blocks = (a.n_tokens + a.at_once - 1) / a.at_once;
     if (blocks > abi::MAX_BLOCKS) return PARASON_ERR_SIZE;
     if (blocks == 0 || a.q_heads + a.k_heads == 0) return PARASON_OK;
@@ -134,6 +150,7 @@ int parason_qk_norm_rotate_grad(const parason_rotate *r, const parason_heads *x,
     if (abi::cu_count() <= 0) return PARASON_ERR_DEVICE;
     a.sums = (float *)workspace;
     hipStream_t stream = (hipStream_t)stream_ptr;
+    a.at_once = tokens_at_once(a, true);
     int64_t blocks = (a.n_tokens + a.at_once - 1) / a.at_once;
     blocks = blocks < grad_blocks(a.n_tokens) ? blocks : grad_blocks(a.n_tokens);
     if (blocks > 0) hipLaunchKernelGGL(pick(r, true), dim3((unsigned)blocks), dim3(pk::ROT_THREADS), 0, stream, a);

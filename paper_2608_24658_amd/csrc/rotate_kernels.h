@@ -2,13 +2,13 @@
  * rotate_kernels.h -- norm and rotation of query and key heads for gfx950, and
  * its backward pass.
  *
- * A group of lanes takes one head of one token, 16 values a lane as two pieces
- * of eight: the two halves of its pairs (or eight neighbouring pairs), so that a
- * lane rotates what it holds and only the sum of squares (backward: and the sum
- * that takes the norm's share out of the gradient) crosses lanes.  All heads of
- * a token turn by the same angles: a block takes a few tokens, whose sines and
- * cosines it works out once, and then all their heads.  Bound by memory: each
- * value is read once and written once (backward: read twice, written once).
+ * A group of lanes takes one head of one token, 16 values a lane, eight pairs or
+ * what is not rotated, so that a lane rotates what it holds and only the sum of
+ * squares (backward: and the sum that takes the norm's share out of the
+ * gradient) crosses lanes.  All heads of a token turn by the same angles: a
+ * block takes a few tokens, whose sines and cosines it works out once, and then
+ * all their heads.  Bound by memory: each value is read once and written once
+ * (backward: read twice, written once).
  */
 #pragma once
 #include "kv_kernels.h"
@@ -16,8 +16,8 @@
 namespace pk {
 
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_TOKENS = 8;        /* most tokens of a block at a time */
-constexpr int ROT_TURNS = 256;       /* most sines and cosines of these; one token has at most 128 */
+constexpr int ROT_TOKENS = 16;       /* most tokens of a block at a time */
+constexpr int ROT_TURNS = 1024;      /* most sines and cosines of these; one token has at most 128 */
 constexpr int ROT_GRAD_BLOCKS = 1024; /* most blocks of the backward pass, each with a share of the weights' gradients */
 
 struct RotHeads {
@@ -39,28 +39,6 @@ struct RotArgs {
     float *sums;                 /* [blocks][2][dim] */
 };
 
-template <int T>
-__device__ __forceinline__ void rot_load(const char *head, int at, bool wide, float *x)
-{
-    const char *p = head + at * type_bytes<T>();
-    if (T == PARASON_DTYPE_F32) {
-        load8<T>(p, 0, 4, true, wide, x);
-    } else {
-        load8<T>(p, 0, 0, true, wide, x);
-    }
-}
-
-template <int T>
-__device__ __forceinline__ void rot_store(char *head, int at, bool wide, const float *x)
-{
-    char *p = head + at * type_bytes<T>();
-    if (T == PARASON_DTYPE_F32) {
-        store8<T>(p, 0, 4, true, wide, x);
-    } else {
-        store8<T>(p, 0, 0, true, wide, x);
-    }
-}
-
 /* cos and sin of position * freq.  The angle is reduced to half turns in [-1, 1]
  * in double and goes on as two floats, so that the float functions see all of
  * it: the second, below 2^-25, turns what the first gave by its own small angle. */
@@ -75,8 +53,8 @@ __device__ __forceinline__ float2 turn_of(int32_t position, double freq)
 }
 
 struct RotLds {
-    float2 turns[ROT_TURNS];
-    float w[2][PARASON_KV_MAX_DIM];
+    __attribute__((aligned(16))) float2 turns[ROT_TURNS];
+    __attribute__((aligned(16))) float w[2][PARASON_KV_MAX_DIM];
 };
 
 template <int T>
@@ -104,29 +82,67 @@ __device__ __forceinline__ void rot_turns(const RotArgs &a, RotLds &s, int64_t t
     }
 }
 
-/* A lane's two pieces of a head: values [lo, lo + 8) and [hi, hi + 8), pair e of
- * its eight being values e of both, or 2e and 2e + 1 of the 16. */
-template <bool INTER>
+/* A lane's 16 values of a head: four fours, at values q[0] .. q[3].  Neighbouring lanes have neighbouring 16 bytes (two
+ * fours of a 16-bit type), so that every access of a group is whole lines (with 32 bytes of float32 a lane, 16 at a time,
+ * 16,000 tokens of 14 heads of 80 values took 81 us forward, this 31).  Halves: pair e of the lane is value e of the first
+ * two fours and value e of the last two; neighbours: the pairs are within the fours. */
+template <int T, bool INTER>
 struct RotPiece {
-    int lo, hi;
+    int q[4];
     bool live, turned;
 
     __device__ __forceinline__ RotPiece(const RotArgs &a, int lane)
     {
         turned = lane * 8 < a.half;
         live = lane * 16 < a.dim;
-        if (INTER || !turned) lo = lane * 16, hi = lo + 8;
-        else lo = lane * 8, hi = a.half + lane * 8;
+        const int n = turned ? a.half / 8 : (a.dim - 2 * a.half) / 16; /* lanes of its region */
+        const int at = turned ? lane : lane - a.half / 8, base = turned ? 0 : 2 * a.half;
+        constexpr bool F32 = T == PARASON_DTYPE_F32;
+        if (!INTER && turned) {
+            q[0] = F32 ? 4 * at : 8 * at, q[1] = F32 ? 4 * (at + n) : q[0] + 4;
+            q[2] = a.half + q[0], q[3] = a.half + q[1];
+        } else if (F32) {
+            for (int i = 0; i < 4; ++i) q[i] = base + 4 * (at + i * n);
+        } else {
+            q[0] = base + 8 * at, q[1] = q[0] + 4, q[2] = base + 8 * (at + n), q[3] = q[2] + 4;
+        }
     }
 };
 
-/* x: 16 values; DIRECTION 1: by the angles, -1: back */
-template <bool INTER, int DIRECTION>
-__device__ __forceinline__ void rot_turn(float *x, const float2 *turns)
+template <int T, bool INTER>
+__device__ __forceinline__ void rot_load(const char *head, const RotPiece<T, INTER> &p, bool wide, float *x)
+{
+    const char *const first = head + p.q[0] * type_bytes<T>(), *const last = head + p.q[2] * type_bytes<T>();
+    load8<T>(first, 0, p.q[1] - p.q[0], true, wide, x);
+    load8<T>(last, 0, p.q[3] - p.q[2], true, wide, x + 8);
+}
+
+template <int T, bool INTER>
+__device__ __forceinline__ void rot_store(char *head, const RotPiece<T, INTER> &p, bool wide, const float *x)
+{
+    char *const first = head + p.q[0] * type_bytes<T>(), *const last = head + p.q[2] * type_bytes<T>();
+    store8<T>(first, 0, p.q[1] - p.q[0], true, wide, x);
+    store8<T>(last, 0, p.q[3] - p.q[2], true, wide, x + 8);
+}
+
+/* 16 values of LDS at the lane's places. */
+template <class P>
+__device__ __forceinline__ void rot_gather(const float *from, const P &p, float *x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 v = *reinterpret_cast<const float4 *>(from + p.q[i]);
+        x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+    }
+}
+
+/* DIRECTION 1: by the token's angles, -1: back */
+template <int DIRECTION, int T, bool INTER>
+__device__ __forceinline__ void rot_turn(float *x, const RotPiece<T, INTER> &p, const float2 *turns)
 {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float2 cs = turns[e];
+        const float2 cs = turns[INTER ? p.q[e / 2] / 2 + (e & 1) : p.q[e / 4] + (e & 3)];
         const float s = DIRECTION > 0 ? cs.y : -cs.y;
         float &a = x[INTER ? 2 * e : e], &b = x[INTER ? 2 * e + 1 : 8 + e];
         const float na = __builtin_fmaf(a, cs.x, -(b * s)), nb = __builtin_fmaf(b, cs.x, a * s);
@@ -173,47 +189,43 @@ __global__ void __launch_bounds__(ROT_THREADS) qk_norm_rotate(RotArgs a)
     rot_turns(a, s, t0, n);
     __syncthreads();
     const int lane = (int)threadIdx.x & ((1 << a.group_log) - 1);
-    const RotPiece<INTER> p(a, lane);
+    const RotPiece<T, INTER> p(a, lane);
     const int q_units = n * a.q_heads, units = q_units + n * a.k_heads, step = ROT_THREADS >> a.group_log;
     for (int u = (int)threadIdx.x >> a.group_log; u < units; u += step) {
         const RotUnit v = rot_unit(a, u, q_units);
         const int64_t t = t0 + v.token;
         float x[16] = {};
         if (p.live) {
-            const char *h = rot_head<T>(a.x, v, t);
-            rot_load<T>(h, p.lo, a.x.wide, x);
-            rot_load<T>(h, p.hi, a.x.wide, x + 8);
+            rot_load<T>(rot_head<T>(a.x, v, t), p, a.x.wide, x);
         }
         float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
         const float r = rsqrtf(__builtin_fmaf(group_sum(sum, a.group_log), a.inv_dim, a.eps));
         if (!p.live) continue;
-        const float *w = s.w[v.is_k];
+        float w[16];
+        rot_gather(s.w[v.is_k], p, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= r * w[p.lo + e], x[8 + e] *= r * w[p.hi + e];
-        if (p.turned) rot_turn<INTER, 1>(x, s.turns + v.token * a.half + lane * 8);
+        for (int e = 0; e < 16; ++e) x[e] *= r * w[e];
+        if (p.turned) rot_turn<1>(x, p, s.turns + v.token * a.half);
         if (a.positions[t] < 0) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = 0.0f;
         }
-        char *y = rot_head<T>(a.y, v, t);
-        rot_store<T>(y, p.lo, a.y.wide, x);
-        rot_store<T>(y, p.hi, a.y.wide, x + 8);
+        rot_store<T>(rot_head<T>(a.y, v, t), p, a.y.wide, x);
     }
 }
 
 /* The same with the gradient turned back; a lane always has the same values of
- * its heads and keeps its sums of the weights' gradients in registers.  The
- * block's groups of lanes are added at the end, in their order. */
+ * its heads and keeps its sums of the weights' gradients in registers. */
 template <int T, bool INTER>
-__global__ void __launch_bounds__(ROT_THREADS) qk_norm_rotate_grad(RotArgs a)
+__global__ void __launch_bounds__(ROT_THREADS, 4) qk_norm_rotate_grad(RotArgs a)
 {
     __shared__ RotLds s;
-    __shared__ float sums[ROT_THREADS * 16];
+    __shared__ __attribute__((aligned(16))) float sums[ROT_THREADS * 16];
     const int lane = (int)threadIdx.x & ((1 << a.group_log) - 1), groups = ROT_THREADS >> a.group_log;
     const int mine = (int)threadIdx.x >> a.group_log;
-    const RotPiece<INTER> p(a, lane);
+    const RotPiece<T, INTER> p(a, lane);
     float acc[2][16] = {};
     rot_weights<T>(a, s);
     for (int64_t t0 = (int64_t)blockIdx.x * a.at_once; t0 < a.n_tokens; t0 += (int64_t)gridDim.x * a.at_once) {
@@ -228,18 +240,15 @@ __global__ void __launch_bounds__(ROT_THREADS) qk_norm_rotate_grad(RotArgs a)
             const bool there = a.positions[t] >= 0;
             float x[16] = {}, g[16] = {};
             if (p.live && there) {
-                const char *h = rot_head<T>(a.x, v, t), *d = rot_head<T>(a.g, v, t);
-                rot_load<T>(h, p.lo, a.x.wide, x);
-                rot_load<T>(h, p.hi, a.x.wide, x + 8);
-                rot_load<T>(d, p.lo, a.g.wide, g);
-                rot_load<T>(d, p.hi, a.g.wide, g + 8);
-                if (p.turned) rot_turn<INTER, -1>(g, s.turns + v.token * a.half + lane * 8);
+                rot_load<T>(rot_head<T>(a.x, v, t), p, a.x.wide, x);
+                rot_load<T>(rot_head<T>(a.g, v, t), p, a.g.wide, g);
+                if (p.turned) rot_turn<-1>(g, p, s.turns + v.token * a.half);
             }
-            const float *w = s.w[v.is_k];
             float sum = 0.0f, dot = 0.0f, gw[16];
+            if (p.live) rot_gather(s.w[v.is_k], p, gw);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                gw[e] = g[e] * w[e < 8 ? p.lo + e : p.hi + e - 8];
+                gw[e] = p.live ? gw[e] * g[e] : 0.0f;
                 sum = __builtin_fmaf(x[e], x[e], sum);
                 dot = __builtin_fmaf(gw[e], x[e], dot);
             }
@@ -257,24 +266,23 @@ __global__ void __launch_bounds__(ROT_THREADS) qk_norm_rotate_grad(RotArgs a)
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = r * __builtin_fmaf(-x[e], dot, gw[e]);
-            char *y = rot_head<T>(a.y, v, t);
-            rot_store<T>(y, p.lo, a.y.wide, x);
-            rot_store<T>(y, p.hi, a.y.wide, x + 8);
+            rot_store<T>(rot_head<T>(a.y, v, t), p, a.y.wide, x);
         }
     }
+    /* the block's groups of lanes, added in their order */
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
         if (p.live) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sums[mine * a.dim + p.lo + e] = acc[which][e];
-                sums[mine * a.dim + p.hi + e] = acc[which][8 + e];
-            }
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4 *>(&sums[mine * a.dim + p.q[i]]) =
+                    make_float4(acc[which][4 * i], acc[which][4 * i + 1], acc[which][4 * i + 2], acc[which][4 * i + 3]);
         }
         __syncthreads();
         for (int d = (int)threadIdx.x; d < a.dim; d += ROT_THREADS) {
             float x = 0.0f;
+#pragma unroll 16
             for (int i = 0; i < groups; ++i) x += sums[i * a.dim + d];
             a.sums[((int64_t)blockIdx.x * 2 + which) * a.dim + d] = x;
         }

@@ -1041,8 +1041,8 @@ def kv_extend(pool: KVPool, lengths, kv_lens, pages, page_size: int, n_tokens: i
         raise ValueError("n_tokens must not be negative")
     # one allocation for the 64-bit results, one for the 32-bit ones
     wide, narrow = T.empty(n + n_tokens, dtype=T.i64, device=dev), T.empty(2 * (n + n_tokens), dtype=T.i32, device=dev)
-    starts, slots = wide.split((n, n_tokens))
-    taken, status, positions, rows = narrow.split((n, n, n_tokens, n_tokens))
+    starts, slots = wide.split_with_sizes((n, n_tokens))
+    taken, status, positions, rows = narrow.split_with_sizes((n, n, n_tokens, n_tokens))
     at, to = wide.data_ptr(), narrow.data_ptr()
     step = KvStepArgs(to, at, to + 4 * n, to + 8 * n, at + 8 * n, to + 8 * n + 4 * n_tokens)
     rc = (_lib or lib()).parason_kv_extend(pa, ta, lengths.data_ptr(), n_tokens, step, workspace.data_ptr(), workspace.numel(),

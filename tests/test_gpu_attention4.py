@@ -141,6 +141,83 @@ def test_long_rows(dev):  # noqa: F811
 
 
 @GIVEN
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_ragged_rows(dev, dim, given):  # noqa: F811
+    """Rows of all lengths: some without tokens or positions, long ones that several blocks share, trees, and several
+    blocks of columns."""
+    log("case 4 bits ragged dim %d %s" % (dim, given))
+    kv = [3000, 0, 1, 128, 129, 5000, 40, 700, 0, 513, 4096, 77]
+    run_case(dev, 16, 2, 4, dim, kv, [1, 1, 1, 0, 1, 1, 0, 1, 0, 1, 1, 1], seed=3, given=given)
+    run_case(dev, 24, 1, 4, dim, kv, [3, 2, 1, 0, 5, 4, 0, 12, 0, 1, 3, 2], seed=4, given=given)
+    run_case(dev, 24, 1, 4, dim, [max(k, 9) for k in kv], [9, 2, 1, 0, 5, 4, 0, 9, 0, 1, 3, 2], shape="tree", seed=5, given=given)
+    run_case(dev, 64, 8, 4, dim, [600] * 40, [1] * 40, seed=6, given=given)
+
+
+def test_long_rows_that_are_bad(dev):  # noqa: F811
+    """Bad rows, pages and trees among rows that are cut into parts."""
+    log("case 4 bits long bad rows")
+    P = Paged4(dev, [3000] * 6, 8, 2, 64, "fp4", seed=3)
+    rng = np.random.default_rng(0)
+    P.fill(lambda i, n: rng.standard_normal((2, n, 2, 64)))
+    rows, total, _ = P.rows([2] * 6)
+    kv, pages, st = rows.kv_lens.clone(), rows.pages.clone(), rows.starts.clone()
+    kv[1], st[3], pages[4, 200] = 3001, -1, P.n_pages
+    rows = rows._replace(kv_lens=kv, pages=pages, starts=st)
+    q = torch.randn(total, 4, 64, device=dev, dtype=torch.bfloat16)
+    status, out = torch.zeros(6, dtype=torch.int32, device=dev), torch.full_like(q, 3.0)
+    PX.tree_attention(q, P.cache, rows, out=out, status=status)
+    assert status.cpu().tolist() == [0, PX.KV_BAD_ROW, 0, PX.KV_BAD_ROW, PX.KV_BAD_PAGE, 0]
+    got = out.cpu().double()
+    assert torch.isnan(got[2:4]).all() and (got[6:8] == 3.0).all() and torch.isnan(got[8:10]).all()
+    for i in (0, 2, 5):
+        o, _, tol, _ = D.attention(q[2 * i: 2 * i + 2].cpu().double().numpy(), *P.held[i], D.visible(3000, 2), 0.125, 7, 7)
+        assert np.all(np.abs(got[2 * i: 2 * i + 2].numpy() - o) <= tol)
+    # trees that their masks do not hold, and none of whose words are read
+    rows, total, _ = P.rows([2] * 6)
+    mask = torch.full((total, 1), -1, dtype=torch.int64, device=dev)
+    trees = torch.tensor([2, 40, 65, -1, 2 ** 31 - 1, 0], dtype=torch.int32, device=dev)
+    status.zero_()
+    got, lse = PX.tree_attention(q, P.cache, rows, mask=mask, tree_lens=trees, status=status, lse=True)
+    b = PX.KV_BAD_ROW
+    assert status.cpu().tolist() == [0, 0, b, b, b, 0]
+    assert torch.isnan(got[4:10]).all() and torch.isnan(lse[4:10]).all() and torch.isfinite(got[:4]).all() and torch.isfinite(got[10:]).all()
+    # a pool without pages
+    none = PX.KVCache(*(t[:0] for t in P.cache))
+    got = PX.tree_attention(q, none, rows)
+    assert torch.isnan(got).all()
+
+
+def test_growing_rows_in_a_graph(dev):  # noqa: F811
+    """Captured, and replayed over rows that have grown meanwhile; two graphs with workspaces of their own."""
+    log("case 4 bits graph")
+    P = Paged4(dev, [3000, 900, 2000], 16, 2, 64, "fp4", seed=3)
+    rng = np.random.default_rng(0)
+    P.fill(lambda i, n: rng.standard_normal((2, n, 2, 64)))
+    rows, total, _ = P.rows([1] * 3)
+    q = torch.randn(total, 8, 64, device=dev, dtype=torch.bfloat16)
+    ws = [torch.empty(PX.tree_attention_workspace_size(P.cache, rows, total, 8), dtype=torch.uint8, device=dev) for _ in range(2)]
+    outs, graphs = [torch.empty_like(q) for _ in range(2)], []
+    torch.cuda.synchronize()
+    for w, o in zip(ws, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            PX.tree_attention(q, P.cache, rows, out=o, workspace=w)
+        graphs.append(g)
+    for lens in ([3000, 900, 2000], [1, 900, 0], [2500, 17, 1999]):
+        rows.kv_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        want = PX.tree_attention(q, P.cache, rows)
+        for g, o, w in zip(graphs, outs, ws):
+            o.fill_(7), w.fill_(0xFF)
+            (torch.randn(1000, device=dev) * 2).sum().item()
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in outs)
+        for i, n in enumerate(lens):
+            o, _, tol, _ = D.attention(q[i: i + 1].cpu().double().numpy(), *(x[:n] for x in P.held[i]), D.visible(n, 1), 0.125, 7, 7)
+            assert np.all(np.abs(want[i: i + 1].cpu().double().numpy() - o) <= tol)
+
+
+@GIVEN
 @pytest.mark.parametrize("kv_lens,lengths,group", [([9000, 4001, 513, 63], [1, 1, 1, 1], 4), ([9100, 2049, 31], [3, 4, 3], 8),
                                                    ([9100, 5000, 1, 4097], [150, 40, 1, 2], 2), ([33000], [1], 4)])
 def test_every_position_counts_once(dev, given, kv_lens, lengths, group):  # noqa: F811
