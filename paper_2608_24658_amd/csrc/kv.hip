@@ -19,7 +19,6 @@ MoveKernel pick(int dtype, int kind)
     case pk::KV_BF16: return dtype == F32 ? K<F32, pk::KV_BF16>::f : dtype == BF16 ? K<BF16, pk::KV_BF16>::f : K<F16, pk::KV_BF16>::f;
     case pk::KV_F16: return dtype == F32 ? K<F32, pk::KV_F16>::f : dtype == BF16 ? K<BF16, pk::KV_F16>::f : K<F16, pk::KV_F16>::f;
     case pk::KV_FP8: return dtype == F32 ? K<F32, pk::KV_FP8>::f : dtype == BF16 ? K<BF16, pk::KV_FP8>::f : K<F16, pk::KV_FP8>::f;
-    case pk::KV_FP4: return dtype == F32 ? K<F32, pk::KV_FP4>::f : dtype == BF16 ? K<BF16, pk::KV_FP4>::f : K<F16, pk::KV_FP4>::f;
     default: return dtype == F32 ? K<F32, pk::KV_INT8>::f : dtype == BF16 ? K<BF16, pk::KV_INT8>::f : K<F16, pk::KV_INT8>::f;
     }
 }
@@ -32,6 +31,23 @@ template <int T, int KIND>
 struct Read {
     static constexpr MoveKernel f = pk::kv_read<T, KIND>;
 };
+
+template <int HEADS>
+MoveKernel pick_read4(int dtype)
+{
+    return dtype == PARASON_DTYPE_F32    ? pk::kv_read4<PARASON_DTYPE_F32, HEADS>
+           : dtype == PARASON_DTYPE_BF16 ? pk::kv_read4<PARASON_DTYPE_BF16, HEADS>
+                                         : pk::kv_read4<PARASON_DTYPE_F16, HEADS>;
+}
+
+MoveKernel pick4(int dtype, bool write, int heads)
+{
+    if (write)
+        return dtype == PARASON_DTYPE_F32    ? pk::kv_write4<PARASON_DTYPE_F32>
+               : dtype == PARASON_DTYPE_BF16 ? pk::kv_write4<PARASON_DTYPE_BF16>
+                                             : pk::kv_write4<PARASON_DTYPE_F16>;
+    return heads == pk::KV4_MORE ? pick_read4<pk::KV4_MORE>(dtype) : pick_read4<pk::KV4_HEADS>(dtype);
+}
 
 /* Most blocks of a launch.  Rows are cut for the longest one, so many blocks of a ragged call find nothing to do, and
  * the few long rows need enough of theirs to fill the device: 48 rows of 1 to 36,000 positions, FP8 read as bfloat16,
@@ -66,13 +82,16 @@ int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void 
     a.wide = aligned(k, 16) && aligned(v, 16) && stride_token * elem % 16 == 0 && stride_head * elem % 16 == 0;
     a.group = 1, a.group_log = 0;
     while (a.group * pk::KV_PER_LANE < cache->head_dim) a.group <<= 1, ++a.group_log;
-    a.heads_div = pk::fast_div((uint32_t)cache->n_heads);
-    const int64_t per_block = pk::KV_THREADS / a.group * (write ? pk::KV_WRITES : kind == pk::KV_FP4 ? pk::KV_READS4 : pk::KV_READS);
-    int64_t blocks = (units + per_block - 1) / per_block, most = MOVE_BLOCKS / rows->n_rows;
+    const bool four = kind == pk::KV_FP4;
+    const int heads = !write && rows->n_tokens >= pk::KV4_MANY && cache->n_heads > pk::KV4_HEADS ? pk::KV4_MORE : pk::KV4_HEADS;
+    const int64_t chunks = four ? (cache->n_heads + heads - 1) / heads : cache->n_heads;
+    a.heads_div = pk::fast_div((uint32_t)chunks);
+    const int64_t per_block = pk::KV_THREADS / a.group * (four ? 1 : write ? pk::KV_WRITES : pk::KV_READS);
+    int64_t blocks = (units / cache->n_heads * chunks + per_block - 1) / per_block, most = MOVE_BLOCKS / rows->n_rows;
     if (most < 1) most = 1; /* (as many blocks as rows) */
     if (blocks > most) blocks = most;
     a.blocks_per_row = (int32_t)blocks;
-    const MoveKernel f = write ? pick<Write>(dtype, kind) : pick<Read>(dtype, kind);
+    const MoveKernel f = four ? pick4(dtype, write, heads) : write ? pick<Write>(dtype, kind) : pick<Read>(dtype, kind);
     hipLaunchKernelGGL(f, dim3((unsigned)(rows->n_rows * blocks)), dim3(pk::KV_THREADS), 0, (hipStream_t)stream_ptr, a);
     return hipGetLastError() == hipSuccess ? PARASON_OK : PARASON_ERR_HIP;
 }

@@ -21,9 +21,6 @@ constexpr int KV_PER_LANE = 8;  /* values */
 /* Units of a lane on their way at once: a unit's page is a load that its values wait for, so one at a time leaves the
  * memory idle.  48 rows of 1 to 36,000 positions read from FP8: 390 us with one, 260 with these. */
 constexpr int KV_WRITES = 2, KV_READS = 4;
-constexpr int KV_READS4 = 4; /* of a 4-bit cache, whose loads are a quarter of its stores */
-template <int KIND>
-constexpr int kv_reads() { return KIND == KV_FP4 ? KV_READS4 : KV_READS; }
 
 struct KvMoveArgs {
     KvCache c;
@@ -38,15 +35,11 @@ struct KvMoveArgs {
 };
 
 /* A lane's eight values are two fours, at value lo and hi of the head: neighbours for 16-bit token arrays, 16 bytes in
- * all; for float32 ones half the group's lanes apart, so that neighbouring lanes read neighbouring 16 bytes (but for
- * 4-bit caches, where eight neighbours are one word of codes and four lanes' share a scale). */
-template <int T, int KIND>
-__device__ __forceinline__ int piece_lo(int lane) { return lane * (T == PARASON_DTYPE_F32 && KIND != KV_FP4 ? 4 : 8); }
-template <int T, int KIND>
-__device__ __forceinline__ int piece_hi(int lane, int group)
-{
-    return T == PARASON_DTYPE_F32 && KIND != KV_FP4 ? (group + lane) * 4 : lane * 8 + 4;
-}
+ * all; for float32 ones half the group's lanes apart, so that neighbouring lanes read neighbouring 16 bytes. */
+template <int T>
+__device__ __forceinline__ int piece_lo(int lane) { return lane * (T == PARASON_DTYPE_F32 ? 4 : 8); }
+template <int T>
+__device__ __forceinline__ int piece_hi(int lane, int group) { return T == PARASON_DTYPE_F32 ? (group + lane) * 4 : lane * 8 + 4; }
 
 /* T: type of the token arrays, PARASON_DTYPE_F32, _BF16 or _F16; p: the head */
 template <int T>
@@ -141,10 +134,10 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
-    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8 || KIND == KV_FP4;
+    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
     const int lane = (int)threadIdx.x & (a.group - 1);
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.c.n_heads;
-    const int lo = piece_lo<T, KIND>(lane), hi = piece_hi<T, KIND>(lane, a.group);
+    const int lo = piece_lo<T>(lane), hi = piece_hi<T>(lane, a.group);
     const bool live = lo < a.c.head_dim, hi_live = hi < a.c.head_dim;
     for (int64_t u0 = part * step * KV_WRITES; u0 < units; u0 += a.blocks_per_row * step * KV_WRITES) {
         KvUnit x[KV_WRITES];
@@ -185,20 +178,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write(KvMoveArgs a)
             uint32_t top = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7FFFFFFFu);
-            for (int o = KIND == KV_FP4 ? 2 : a.group >> 1; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+            for (int o = a.group >> 1; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
             const bool finite = top < 0x7F800000u;
-            if (KIND == KV_FP4) {
-                /* (top of the four lanes that share a scale: the loop above ends early) */
-                const uint32_t byte = finite ? fp4_scale_byte(top) : 255u;
-                if (!mine[i]) continue;
-                *reinterpret_cast<uint32_t *>(cache + (at + lo) / 2) = finite ? f32_to_fp4x8(f[i], fp4_scale(byte)) : 0u;
-                if ((lane & 3) == 0)
-                    reinterpret_cast<uint8_t *>(x[i].is_v ? a.c.v_scale : a.c.k_scale)[(int64_t)x[i].page * a.c.scale_stride_page +
-                                                                                       (int64_t)x[i].slot * a.c.scale_stride_slot +
-                                                                                       x[i].head * a.c.scale_stride_head + (lane >> 2)] =
-                        (uint8_t)byte;
-                continue;
-            }
             float scale = fmaxf(__uint_as_float(top) * (KIND == KV_FP8 ? 1.0f / 448.0f : 1.0f / 127.0f), 0x1p-126f);
             if (!finite) scale = __uint_as_float(0x7FC00000u);
 #pragma unroll
@@ -230,21 +211,20 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
-    constexpr int READS = kv_reads<KIND>();
-    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8 || KIND == KV_FP4;
+    constexpr bool CODES = KIND == KV_FP8 || KIND == KV_INT8;
     const int lane = (int)threadIdx.x & (a.group - 1);
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.c.n_heads;
-    const int lo = piece_lo<T, KIND>(lane), hi = piece_hi<T, KIND>(lane, a.group);
+    const int lo = piece_lo<T>(lane), hi = piece_hi<T>(lane, a.group);
     if (lo >= a.c.head_dim) return;
     const bool hi_live = hi < a.c.head_dim;
-    for (int64_t u0 = part * step * READS; u0 < units; u0 += a.blocks_per_row * step * READS) {
-        KvUnit x[READS];
-        uint4 raw[READS];
-        float scale[READS];
+    for (int64_t u0 = part * step * KV_READS; u0 < units; u0 += a.blocks_per_row * step * KV_READS) {
+        KvUnit x[KV_READS];
+        uint4 raw[KV_READS];
+        float scale[KV_READS];
 #pragma unroll
-        for (int i = 0; i < READS; ++i) x[i] = kv_unit(a, row, w, u0 + i * step + (threadIdx.x >> a.group_log), units);
+        for (int i = 0; i < KV_READS; ++i) x[i] = kv_unit(a, row, w, u0 + i * step + (threadIdx.x >> a.group_log), units);
 #pragma unroll
-        for (int i = 0; i < READS; ++i) {
+        for (int i = 0; i < KV_READS; ++i) {
             raw[i] = make_uint4(0u, 0u, 0u, 0u);
             scale[i] = __uint_as_float(0x7FC00000u);
             if (x[i].page < 0) {
@@ -264,12 +244,6 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
                     raw[i] = *reinterpret_cast<const uint4 *>(cache + (at + lo) * 2);
                 }
                 scale[i] = 1.0f;
-            } else if (KIND == KV_FP4) {
-                raw[i].x = *reinterpret_cast<const uint32_t *>(cache + (at + lo) / 2);
-                scale[i] = fp4_scale(
-                    reinterpret_cast<const uint8_t *>(x[i].is_v ? a.c.v_scale : a.c.k_scale)[(int64_t)x[i].page * a.c.scale_stride_page +
-                                                                                             (int64_t)x[i].slot * a.c.scale_stride_slot +
-                                                                                             x[i].head * a.c.scale_stride_head + (lane >> 2)]);
             } else {
                 if (T == PARASON_DTYPE_F32) {
                     raw[i].x = *reinterpret_cast<const uint32_t *>(cache + at + lo);
@@ -284,7 +258,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
             }
         }
 #pragma unroll
-        for (int i = 0; i < READS; ++i) {
+        for (int i = 0; i < KV_READS; ++i) {
             if (u0 + i * step + (threadIdx.x >> a.group_log) >= units) continue;
             float f[8];
             if (!CODES) {
@@ -294,8 +268,6 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
                     const uint32_t b = (h[e / 2] >> (16 * (e & 1))) & 0xFFFFu;
                     f[e] = x[i].page < 0 ? scale[i] : KIND == KV_BF16 ? bf16_to_f32(b) : f16_to_f32(b);
                 }
-            } else if (KIND == KV_FP4) {
-                fp4x8_to_f32(raw[i].x, scale[i], f);
             } else {
                 if (KIND == KV_FP8) fp8x4_to_f32(raw[i].x, f), fp8x4_to_f32(raw[i].y, f + 4);
                 else int8x4_to_f32(raw[i].x, f), int8x4_to_f32(raw[i].y, f + 4);
@@ -308,6 +280,119 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
             }
             store8<T>((x[i].is_v ? a.v : a.k) + ((w.start + x[i].token) * a.stride_token + x[i].head * a.stride_head) * type_bytes<T>(),
                       lo, hi, hi_live, a.wide, f);
+        }
+    }
+}
+
+/* ---- 4-bit caches ---------------------------------------------------------
+ * A lane has eight neighbouring values, one word of codes, and four lanes share
+ * a scale.  So little a head and lane that finding its place is most of the
+ * work: a group takes HEADS heads of a token's keys or values, whose places are
+ * one stride apart.  165,000 positions of 8 heads of 128 values read as bfloat16,
+ * 0.94 GB, take 204 us with 8 heads, 222 with 4 and 266 with one; the tokens of
+ * 64 rows, where there are too few groups otherwise, 5.0 with 8 and 3.9 with 4. */
+constexpr int KV4_HEADS = 4, KV4_MORE = 8;
+constexpr int64_t KV4_MANY = 16384; /* tokens that are read KV4_MORE heads at a time */
+
+struct Kv4Unit {
+    int32_t page, token, head, heads; /* its first head, and how many */
+    bool is_v;
+    char *codes;
+    uint8_t *scales;
+};
+
+/* Unit u of a row (token, k or v, HEADS heads; these fastest), for the lane whose values begin at lo. */
+template <int HEADS>
+__device__ __forceinline__ Kv4Unit kv4_unit(const KvMoveArgs &a, int64_t row, const KvRow &w, uint32_t u, int lo)
+{
+    Kv4Unit x;
+    const uint32_t th = div_by(u, a.heads_div);
+    x.head = (int32_t)(u - th * a.heads_div.d) * HEADS;
+    x.heads = a.c.n_heads - x.head < HEADS ? a.c.n_heads - x.head : HEADS;
+    x.token = (int32_t)(th >> 1);
+    x.is_v = th & 1;
+    int32_t slot;
+    x.page = page_of(a.r, a.c, row, w.kv_len - w.length + x.token, &slot);
+    const int64_t page = x.page < 0 ? 0 : x.page;
+    x.codes = (x.is_v ? a.c.v : a.c.k) + ((page * a.c.stride_page + slot * a.c.stride_slot + x.head * a.c.stride_head + lo) >> 1);
+    x.scales = reinterpret_cast<uint8_t *>(x.is_v ? a.c.v_scale : a.c.k_scale) +
+               (page * a.c.scale_stride_page + slot * a.c.scale_stride_slot + x.head * a.c.scale_stride_head + lo / PARASON_KV_SCALE_GROUP);
+    return x;
+}
+
+template <int T>
+__global__ void __launch_bounds__(KV_THREADS) kv_write4(KvMoveArgs a)
+{
+    const int64_t row = blockIdx.x / (uint32_t)a.blocks_per_row;
+    const uint32_t part = blockIdx.x % (uint32_t)a.blocks_per_row;
+    const KvRow w = load_row(a.r, a.c, row, true);
+    if (!w.ok) {
+        if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
+        return;
+    }
+    const int lane = (int)threadIdx.x & (a.group - 1), lo = lane * KV_PER_LANE;
+    const bool live = lo < a.c.head_dim;
+    const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.heads_div.d;
+    for (int64_t u = part * step + (threadIdx.x >> a.group_log); u < units; u += a.blocks_per_row * step) {
+        const Kv4Unit x = kv4_unit<KV4_HEADS>(a, row, w, (uint32_t)u, live ? lo : 0);
+        if (x.page < 0 && lane == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
+        const char *from = (x.is_v ? a.v : a.k) + ((w.start + x.token) * a.stride_token + x.head * a.stride_head) * type_bytes<T>();
+        const bool mine = live && x.page >= 0;
+        float f[KV4_HEADS][8];
+#pragma unroll
+        for (int i = 0; i < KV4_HEADS; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[i][e] = 0.0f;
+            if (mine && i < x.heads) load8<T>(from + i * a.stride_head * type_bytes<T>(), lo, lo + 4, true, a.wide, f[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < KV4_HEADS; ++i) {
+            /* the largest magnitude as bits: in that order infinities and NaN come last */
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7FFFFFFFu);
+            top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+            if (!mine || i >= x.heads) continue;
+            const bool finite = top < 0x7F800000u;
+            const uint32_t byte = finite ? fp4_scale_byte(top) : 255u;
+            *reinterpret_cast<uint32_t *>(x.codes + ((i * a.c.stride_head) >> 1)) = finite ? f32_to_fp4x8(f[i], fp4_scale(byte)) : 0u;
+            if ((lane & 3) == 0) x.scales[i * a.c.scale_stride_head] = (uint8_t)byte;
+        }
+    }
+}
+
+template <int T, int HEADS>
+__global__ void __launch_bounds__(KV_THREADS) kv_read4(KvMoveArgs a)
+{
+    const int64_t row = blockIdx.x / (uint32_t)a.blocks_per_row;
+    const uint32_t part = blockIdx.x % (uint32_t)a.blocks_per_row;
+    const KvRow w = load_row(a.r, a.c, row, true);
+    if (!w.ok) {
+        if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
+        return;
+    }
+    const int lane = (int)threadIdx.x & (a.group - 1), lo = lane * KV_PER_LANE;
+    if (lo >= a.c.head_dim) return;
+    const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.heads_div.d;
+    for (int64_t u = part * step + (threadIdx.x >> a.group_log); u < units; u += a.blocks_per_row * step) {
+        const Kv4Unit x = kv4_unit<HEADS>(a, row, w, (uint32_t)u, lo);
+        uint32_t codes[HEADS], byte[HEADS];
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            codes[i] = 0u, byte[i] = 255u;    /* (of a bad page: NaN) */
+            if (x.page >= 0 && i < x.heads) {
+                codes[i] = *reinterpret_cast<const uint32_t *>(x.codes + ((i * a.c.stride_head) >> 1));
+                byte[i] = x.scales[i * a.c.scale_stride_head];
+            }
+        }
+        if (x.page < 0 && lane == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
+        char *to = (x.is_v ? a.v : a.k) + ((w.start + x.token) * a.stride_token + x.head * a.stride_head) * type_bytes<T>();
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            float f[8];
+            fp4x8_to_f32(codes[i], fp4_scale(byte[i]), f);
+            if (i < x.heads) store8<T>(to + i * a.stride_head * type_bytes<T>(), lo, lo + 4, true, a.wide, f);
         }
     }
 }

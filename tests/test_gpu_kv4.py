@@ -83,6 +83,25 @@ def test_write_then_read(dev, shape, given):
     assert status.cpu().tolist() == [0] * len(lengths)
 
 
+@pytest.mark.parametrize("heads", [1, 5, 8, 11])
+def test_many_tokens(dev, heads):
+    """Enough tokens that more heads are read at a time, and some of the last ones are not there."""
+    log("case kv4 many tokens of %d heads" % heads)
+    n, dim = 16500, 64
+    cache = PX.kv_alloc(-(-n // 16) + 1, 16, heads, dim, torch.float4_e2m1fn_x2, dev)
+    one = lambda v, dt: torch.tensor([v], dtype=dt, device=dev)  # noqa: E731
+    pages = torch.randperm(cache.k.shape[0], device=dev, dtype=torch.int32)[None]
+    rows = PX.KVRows(one(0, torch.int64), one(n, torch.int32), one(n, torch.int32), pages, n, n)
+    x = torch.randn(2, n, heads, dim, device=dev)
+    PX.kv_write(x[0], x[1], cache, rows)
+    wide = torch.full((2, n, heads + 1, dim), 5.0, device=dev, dtype=torch.bfloat16)
+    k, v = PX.kv_read(cache, rows, n, torch.bfloat16, out=(wide[0, :, :heads], wide[1, :, :heads]))
+    for g, w in ((k, x[0]), (v, x[1])):
+        want = torch.from_numpy(S.values4(*S.quantise4(w.cpu().numpy()))).bfloat16()
+        assert torch.equal(g.cpu(), want)
+    assert (wide[:, :, heads] == 5.0).all()
+
+
 def test_every_code_and_scale(dev):
     """All 16 codes under every scale byte that a write makes, and 255, read back as float32."""
     log("case every code")
