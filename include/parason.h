@@ -555,7 +555,7 @@ typedef struct parason_kv_table {
  * per token (each of the three arrays may be NULL) where it belongs; -1 for
  * tokens of no row and of rows that were not served. */
 typedef struct parason_kv_step {
-    int32_t *lengths;         /* [n_rows] the row's tokens, 0 if it was not served; not the array of the wished lengths */
+    int32_t *lengths;         /* [n_rows] the row's tokens, 0 if it was not served; may be the array of the wished lengths */
     int64_t *starts;          /* [n_rows] their first one: the sum of the wished lengths before it, at most n_tokens */
     uint32_t *row_status;     /* [n_rows] 0, PARASON_KV_BAD_ROW or PARASON_KV_NO_PAGES (set, not ORed); NULL: not reported */
     int32_t *positions;       /* [n_tokens] position in the row */
@@ -590,7 +590,8 @@ int parason_kv_extend(const parason_kv_pool *pool, const parason_kv_table *table
  * entries that are negative go onto the pool too, and pages for which the pool
  * has no room are lost: both set PARASON_KV_BAD_PAGE.  Pages that several rows
  * share are the caller's to keep: the rows that do not own them give back what
- * is behind the shared prefix. */
+ * is behind the shared prefix.  (PARASON_ERR_SIZE when the rows times their 512s
+ * of pages are 2^26 or more.) */
 int parason_kv_shrink(const parason_kv_pool *pool, const parason_kv_table *table, const int32_t *new_lens,
                       uint32_t *row_status, void *workspace, size_t workspace_bytes, void *stream);
 
@@ -629,7 +630,8 @@ typedef struct parason_heads {
 } parason_heads;
 
 /* y of every head of x, asynchronously on `stream`.  y may be x itself (the same
- * addresses and strides); other overlaps give wrong results. */
+ * addresses and strides); other overlaps give wrong results.  Up to 2^24 tokens
+ * at least (PARASON_ERR_SIZE). */
 int parason_qk_norm_rotate(const parason_rotate *r, const parason_heads *x, const parason_heads *y, void *stream);
 
 /* The backward pass: dx of every head from x and dy = d loss / d y, and d loss /

@@ -34,7 +34,8 @@ def values4(codes, scales):
     """The float32 values that codes and scale bytes stand for: exact."""
     x = np.where(codes & 8, -1.0, 1.0) * GRID4[codes & 7]
     s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
-    return (x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32)) * s[..., None]).reshape(x.shape).astype(np.float32)
+    with np.errstate(over="ignore"):
+        return (x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32)) * s[..., None]).reshape(x.shape).astype(np.float32)
 
 
 def pack4(codes):

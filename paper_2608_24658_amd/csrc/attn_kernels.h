@@ -160,6 +160,17 @@ __device__ __forceinline__ uint32_t finite_word(uint32_t w)
     return w & (((w & e) != e ? 0x0000FFFFu : 0u) | (((w >> 16) & e) != e ? 0xFFFF0000u : 0u));
 }
 
+/* Scales of a 4-bit cache from here on may make values that are not finite: 253 and 254 infinities (which a write
+ * does not), 255 NaN. */
+constexpr uint32_t FP4_FAR = 253;
+
+/* Value d of a head of a 4-bit cache. */
+__device__ __forceinline__ float fp4_value(const char *codes, int d, uint32_t byte)
+{
+    const uint32_t c = ((uint32_t)(uint8_t)codes[d >> 1] >> (4 * (d & 1))) & 15u;
+    return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, fp4_scale(byte), 0)[0];
+}
+
 /* The maximum over the lanes of a column, 16 or 32 and 32 apart. */
 template <int CN>
 __device__ __forceinline__ float column_max(float x)
@@ -538,9 +549,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
                 if (FOUR) {
-                    if (piece_live && v_byte[p] == 255u) {
+                    if (piece_live && v_byte[p] >= FP4_FAR) {
                         v_stamp[my_row + p * RPP] = x;
                         odd_seen = true;
+                        vr[p] = u32x4{0u, 0u, 0u, 0u};
                         v_byte[p] = 127u;
                     }
                     continue;
@@ -812,17 +824,21 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                     asm volatile("" : "+v"(h4));
                     const char *v = a.c.v + cache_bytes<KIND>((int64_t)page * a.c.stride_page + (int64_t)slot * a.c.stride_slot +
                                                               (int64_t)head * a.c.stride_head);
-                    if (FOUR)                /* what is NaN in a 4-bit cache is so by its scale */
-                        v = (const char *)a.c.v_scale + (int64_t)page * a.c.scale_stride_page + (int64_t)slot * a.c.scale_stride_slot +
-                            (int64_t)head * a.c.scale_stride_head;
+                    const uint8_t *const scales = FOUR ? reinterpret_cast<const uint8_t *>(a.c.v_scale) + (int64_t)page * a.c.scale_stride_page +
+                                                             (int64_t)slot * a.c.scale_stride_slot + (int64_t)head * a.c.scale_stride_head
+                                                       : nullptr;
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
 #pragma unroll
                         for (int i = 0; i < AC; ++i) {
                             const int at_d = d * CN + 8 * (i / 4) + h4 + (i & 3);
                             if (at_d >= a.c.head_dim) continue;
-                            const float e = FOUR ? ((uint8_t)v[at_d / 32] == 255u ? __uint_as_float(0x7FC00000u) : 0.0f)
-                                                 : cached_value<KIND>(v + cache_bytes<KIND>(at_d));
+                            if (FOUR) {      /* 32 values were left out together */
+                                const uint32_t byte = scales[at_d / 32];
+                                if (byte >= FP4_FAR) o[d][i] += p * fp4_value(v, at_d, byte);
+                                continue;
+                            }
+                            const float e = cached_value<KIND>(v + cache_bytes<KIND>(at_d));
                             if (!(e > -INFINITY && e < INFINITY)) o[d][i] += p * e;
                         }
                         __builtin_amdgcn_sched_barrier(0);

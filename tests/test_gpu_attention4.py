@@ -30,6 +30,8 @@ def in_4_bits(monkeypatch):
         group, u = q.shape[1] // k.shape[1], np.nan_to_num(np.abs(v))
         size = np.einsum("np,phd->nhd", seen.astype(np.float64), u)
         out_tol = out_tol + 2.0 ** -126 * np.repeat(size, group, 1)
+        if bits == 10:  # 65,504 is float16's largest, and from 65,520, half a step further, on results round to infinity
+            out = np.where(np.abs(out) >= 65520, np.copysign(np.inf, out), out)
         return out, lse, out_tol, lse_tol
 
     monkeypatch.setattr(D, "attention", attention)
@@ -118,6 +120,28 @@ def test_what_is_not_seen_changes_nothing(dev, lengths, bad, given):  # noqa: F8
 
     for shape in (None, "tree", "empty"):
         run_case(dev, 16, 2, 4, 64, [lengths[0] + 37, lengths[1]], lengths, shape=shape, seed=11, values=values, given=given)
+
+
+@GIVEN
+@pytest.mark.parametrize("lengths", [[4, 9], [40, 60]])
+def test_scales_that_a_write_does_not_make(dev, lengths, given):  # noqa: F811
+    """Scale bytes of 253 and 254, whose larger values are infinities, and 255, in values of positions that some tokens
+    see and others do not: the smaller values of the same 32 count as they are, those of other 32s too."""
+    log("case 4 bits infinite scales %s %s" % (lengths, given))
+    rng = np.random.default_rng(2)
+
+    def spoil(P, seens):
+        for i, n in enumerate(lengths):
+            for byte, back, at in ((253, 1, 0), (254, 2, 1), (255, 3, 0)):
+                pos = int(P.kv_lens[i]) - back
+                pg, slot = (int(v) for v in P.place(i, pos))
+                codes = rng.integers(0, 16, 32).astype(np.uint8)
+                P.cache.v.view(torch.uint8)[pg, slot, 1, 16 * at: 16 * at + 16] = torch.from_numpy(S.pack4(codes)).to(dev)
+                P.cache.v_scale.view(torch.uint8)[pg, slot, 1, at] = byte
+                P.held[i][1][pos, 1, 32 * at: 32 * at + 32] = S.values4(codes, np.array([byte], np.uint8))
+
+    for shape in (None, "tree"):
+        run_case(dev, 16, 2, 4, 64, [lengths[0] + 37, lengths[1]], lengths, shape=shape, seed=12, given=given, spoil=spoil)
 
 
 @GIVEN

@@ -103,12 +103,11 @@ def test_many_tokens(dev, heads):
 
 
 def test_every_code_and_scale(dev):
-    """All 16 codes under every scale byte that a write makes, and 255, read back as float32."""
+    """All 16 codes under every scale byte, those that a write does not make too, read back as float32."""
     log("case every code")
     cache = PX.kv_alloc(16, 16, 1, 32, torch.float4_e2m1fn_x2, dev)
     codes = np.tile(np.arange(16, dtype=np.uint8), (256, 2))
     scale = np.arange(256, dtype=np.uint8)
-    scale[(scale < 7) | ((scale > 252) & (scale < 255))] = 127
     for t in (cache.k, cache.v):
         t.view(torch.uint8).copy_(torch.from_numpy(S.pack4(codes)).view(16, 16, 1, 16))
     for t in (cache.k_scale, cache.v_scale):
