@@ -32,21 +32,23 @@ struct Read {
     static constexpr MoveKernel f = pk::kv_read<T, KIND>;
 };
 
-template <int HEADS>
-MoveKernel pick_read4(int dtype)
+template <int T, int HEADS>
+MoveKernel pick4(bool write)
 {
-    return dtype == PARASON_DTYPE_F32    ? pk::kv_read4<PARASON_DTYPE_F32, HEADS>
-           : dtype == PARASON_DTYPE_BF16 ? pk::kv_read4<PARASON_DTYPE_BF16, HEADS>
-                                         : pk::kv_read4<PARASON_DTYPE_F16, HEADS>;
+    return write ? pk::kv_write4<T, HEADS> : pk::kv_read4<T, HEADS>;
+}
+
+template <int T>
+MoveKernel pick4(bool write, int heads)
+{
+    return heads == 1 ? pick4<T, 1>(write) : heads == 2 ? pick4<T, 2>(write) : heads == pk::KV4_MORE ? pk::kv_read4<T, pk::KV4_MORE> : pick4<T, pk::KV4_HEADS>(write);
 }
 
 MoveKernel pick4(int dtype, bool write, int heads)
 {
-    if (write)
-        return dtype == PARASON_DTYPE_F32    ? pk::kv_write4<PARASON_DTYPE_F32>
-               : dtype == PARASON_DTYPE_BF16 ? pk::kv_write4<PARASON_DTYPE_BF16>
-                                             : pk::kv_write4<PARASON_DTYPE_F16>;
-    return heads == pk::KV4_MORE ? pick_read4<pk::KV4_MORE>(dtype) : pick_read4<pk::KV4_HEADS>(dtype);
+    return dtype == PARASON_DTYPE_F32    ? pick4<PARASON_DTYPE_F32>(write, heads)
+           : dtype == PARASON_DTYPE_BF16 ? pick4<PARASON_DTYPE_BF16>(write, heads)
+                                         : pick4<PARASON_DTYPE_F16>(write, heads);
 }
 
 /* Most blocks of a launch.  Rows are cut for the longest one, so many blocks of a ragged call find nothing to do, and
@@ -83,10 +85,13 @@ int move(const parason_kv_cache *cache, const parason_kv_rows *rows, const void 
     a.group = 1, a.group_log = 0;
     while (a.group * pk::KV_PER_LANE < cache->head_dim) a.group <<= 1, ++a.group_log;
     const bool four = kind == pk::KV_FP4;
-    const int heads = !write && rows->n_tokens >= pk::KV4_MANY && cache->n_heads > pk::KV4_HEADS ? pk::KV4_MORE : pk::KV4_HEADS;
+    /* (only reads take KV4_MORE) */
+    const int heads = !write && rows->n_tokens >= pk::KV4_MANY && cache->n_heads > pk::KV4_HEADS ? pk::KV4_MORE
+                      : cache->n_heads < 3                                                       ? cache->n_heads
+                                                                                                 : pk::KV4_HEADS;
     const int64_t chunks = four ? (cache->n_heads + heads - 1) / heads : cache->n_heads;
     a.heads_div = pk::fast_div((uint32_t)chunks);
-    const int64_t per_block = pk::KV_THREADS / a.group * (four ? 1 : write ? pk::KV_WRITES : pk::KV_READS);
+    const int64_t per_block = pk::KV_THREADS / a.group * (four ? (heads < pk::KV4_HEADS ? pk::KV4_HEADS / heads : 1) : write ? pk::KV_WRITES : pk::KV_READS);
     int64_t blocks = (units / cache->n_heads * chunks + per_block - 1) / per_block, most = MOVE_BLOCKS / rows->n_rows;
     if (most < 1) most = 1; /* (as many blocks as rows) */
     if (blocks > most) blocks = most;

@@ -285,42 +285,45 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
 }
 
 /* ---- 4-bit caches ---------------------------------------------------------
- * A lane has eight neighbouring values, one word of codes, and four lanes share
- * a scale.  So little a head and lane that finding its place is most of the
- * work: a group takes HEADS heads of a token's keys or values, whose places are
- * one stride apart.  165,000 positions of 8 heads of 128 values read as bfloat16,
- * 0.94 GB, take 204 us with 8 heads, 222 with 4 and 266 with one; the tokens of
- * 64 rows, where there are too few groups otherwise, 5.0 with 8 and 3.9 with 4. */
+ * A lane has eight values, and four lanes share a scale.  So little a head and
+ * lane that finding its place and waiting for its page is most of the work: a
+ * group takes HEADS heads of a token's keys or values, whose places are one
+ * stride apart, and where these are fewer than four, several tokens at a time.
+ * 165,000 positions of 8 heads of 128 values read as bfloat16, 0.94 GB, take 204
+ * us with 8 heads, 222 with 4 and 266 with one (and four tokens); the tokens of
+ * 64 rows, where there are too few groups otherwise, 5.0 with 8 and 3.9 with 4.
+ * 256,000 tokens of one head of 128 values: written in 46 us four at a time,
+ * read in 38; 63 and 49 one by one. */
 constexpr int KV4_HEADS = 4, KV4_MORE = 8;
 constexpr int64_t KV4_MANY = 16384; /* tokens that are read KV4_MORE heads at a time */
 
 struct Kv4Unit {
-    int32_t page, token, head, heads; /* its first head, and how many */
+    int32_t page, token, head, heads; /* its first head, and how many (0: no unit) */
     bool is_v;
-    char *codes;
+    char *codes;                      /* of the first head */
     uint8_t *scales;
 };
 
-/* Unit u of a row (token, k or v, HEADS heads; these fastest), for the lane whose values begin at lo. */
+/* Unit u of a row (token, k or v, HEADS heads; these fastest). */
 template <int HEADS>
-__device__ __forceinline__ Kv4Unit kv4_unit(const KvMoveArgs &a, int64_t row, const KvRow &w, uint32_t u, int lo)
+__device__ __forceinline__ Kv4Unit kv4_unit(const KvMoveArgs &a, int64_t row, const KvRow &w, int64_t u, int64_t units)
 {
     Kv4Unit x;
-    const uint32_t th = div_by(u, a.heads_div);
-    x.head = (int32_t)(u - th * a.heads_div.d) * HEADS;
-    x.heads = a.c.n_heads - x.head < HEADS ? a.c.n_heads - x.head : HEADS;
+    const uint32_t v = (uint32_t)(u < units ? u : units - 1), th = div_by(v, a.heads_div);
+    x.head = (int32_t)(v - th * a.heads_div.d) * HEADS;
+    x.heads = u >= units ? 0 : a.c.n_heads - x.head < HEADS ? a.c.n_heads - x.head : HEADS;
     x.token = (int32_t)(th >> 1);
     x.is_v = th & 1;
     int32_t slot;
     x.page = page_of(a.r, a.c, row, w.kv_len - w.length + x.token, &slot);
     const int64_t page = x.page < 0 ? 0 : x.page;
-    x.codes = (x.is_v ? a.c.v : a.c.k) + ((page * a.c.stride_page + slot * a.c.stride_slot + x.head * a.c.stride_head + lo) >> 1);
+    x.codes = (x.is_v ? a.c.v : a.c.k) + ((page * a.c.stride_page + slot * a.c.stride_slot + x.head * a.c.stride_head) >> 1);
     x.scales = reinterpret_cast<uint8_t *>(x.is_v ? a.c.v_scale : a.c.k_scale) +
-               (page * a.c.scale_stride_page + slot * a.c.scale_stride_slot + x.head * a.c.scale_stride_head + lo / PARASON_KV_SCALE_GROUP);
+               (page * a.c.scale_stride_page + slot * a.c.scale_stride_slot + x.head * a.c.scale_stride_head);
     return x;
 }
 
-template <int T>
+template <int T, int HEADS>
 __global__ void __launch_bounds__(KV_THREADS) kv_write4(KvMoveArgs a)
 {
     const int64_t row = blockIdx.x / (uint32_t)a.blocks_per_row;
@@ -330,38 +333,50 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write4(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
+    constexpr int TOKENS = HEADS < KV4_HEADS ? KV4_HEADS / HEADS : 1;
     const int lane = (int)threadIdx.x & (a.group - 1), lo = lane * KV_PER_LANE;
     const bool live = lo < a.c.head_dim;
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.heads_div.d;
-    for (int64_t u = part * step + (threadIdx.x >> a.group_log); u < units; u += a.blocks_per_row * step) {
-        const Kv4Unit x = kv4_unit<KV4_HEADS>(a, row, w, (uint32_t)u, live ? lo : 0);
-        if (x.page < 0 && lane == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
-        const char *from = (x.is_v ? a.v : a.k) + ((w.start + x.token) * a.stride_token + x.head * a.stride_head) * type_bytes<T>();
-        const bool mine = live && x.page >= 0;
-        float f[KV4_HEADS][8];
+    for (int64_t u0 = part * step * TOKENS; u0 < units; u0 += a.blocks_per_row * step * TOKENS) {
+        Kv4Unit x[TOKENS];
+        float f[TOKENS][HEADS][8];
 #pragma unroll
-        for (int i = 0; i < KV4_HEADS; ++i) {
+        for (int k = 0; k < TOKENS; ++k) x[k] = kv4_unit<HEADS>(a, row, w, u0 + k * step + (threadIdx.x >> a.group_log), units);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[i][e] = 0.0f;
-            if (mine && i < x.heads) load8<T>(from + i * a.stride_head * type_bytes<T>(), lo, lo + 4, true, a.wide, f[i]);
+        for (int k = 0; k < TOKENS; ++k) {
+            if (x[k].page < 0 && x[k].heads > 0 && lane == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
+            const char *from =
+                (x[k].is_v ? a.v : a.k) + ((w.start + x[k].token) * a.stride_token + x[k].head * a.stride_head) * type_bytes<T>();
+#pragma unroll
+            for (int i = 0; i < HEADS; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[k][i][e] = 0.0f;
+                if (live && x[k].page >= 0 && i < x[k].heads)
+                    load8<T>(from + i * a.stride_head * type_bytes<T>(), lo, lo + 4, true, a.wide, f[k][i]);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < KV4_HEADS; ++i) {
-            /* the largest magnitude as bits: in that order infinities and NaN come last */
-            uint32_t top = 0;
+        for (int k = 0; k < TOKENS; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7FFFFFFFu);
-            top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-            if (!mine || i >= x.heads) continue;
-            const bool finite = top < 0x7F800000u;
-            const uint32_t byte = finite ? fp4_scale_byte(top) : 255u;
-            *reinterpret_cast<uint32_t *>(x.codes + ((i * a.c.stride_head) >> 1)) = finite ? f32_to_fp4x8(f[i], fp4_scale(byte)) : 0u;
-            if ((lane & 3) == 0) x.scales[i * a.c.scale_stride_head] = (uint8_t)byte;
-        }
+            for (int i = 0; i < HEADS; ++i) {
+                /* the largest magnitude as bits: in that order infinities and NaN come last */
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[k][i][e]) & 0x7FFFFFFFu);
+                top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+                if (!live || x[k].page < 0 || i >= x[k].heads) continue;
+                const bool finite = top < 0x7F800000u;
+                const uint32_t byte = finite ? fp4_scale_byte(top) : 255u;
+                *reinterpret_cast<uint32_t *>(x[k].codes + ((i * a.c.stride_head + lo) >> 1)) =
+                    finite ? f32_to_fp4x8(f[k][i], fp4_scale(byte)) : 0u;
+                if ((lane & 3) == 0) x[k].scales[i * a.c.scale_stride_head + lo / PARASON_KV_SCALE_GROUP] = (uint8_t)byte;
+            }
     }
 }
 
+/* float32 results: a lane's two fours are half the head apart, so that neighbouring lanes write neighbouring 16 bytes
+ * (64,000 tokens of 8 heads of 128 values 165 us, 213 with 32 bytes a lane). */
 template <int T, int HEADS>
 __global__ void __launch_bounds__(KV_THREADS) kv_read4(KvMoveArgs a)
 {
@@ -372,27 +387,49 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read4(KvMoveArgs a)
         if (part == 0 && threadIdx.x == 0) report(a.r, row, PARASON_KV_BAD_ROW);
         return;
     }
-    const int lane = (int)threadIdx.x & (a.group - 1), lo = lane * KV_PER_LANE;
-    if (lo >= a.c.head_dim) return;
+    constexpr int TOKENS = HEADS < KV4_HEADS ? KV4_HEADS / HEADS : 1;
+    constexpr bool F32 = T == PARASON_DTYPE_F32;
+    const int lane = (int)threadIdx.x & (a.group - 1);
+    if (lane * KV_PER_LANE >= a.c.head_dim) return;
+    const int lo = F32 ? lane * 4 : lane * 8, hi = F32 ? a.c.head_dim / 2 + lane * 4 : lo + 4;
     const int64_t step = KV_THREADS >> a.group_log, units = (int64_t)w.length * 2 * a.heads_div.d;
-    for (int64_t u = part * step + (threadIdx.x >> a.group_log); u < units; u += a.blocks_per_row * step) {
-        const Kv4Unit x = kv4_unit<HEADS>(a, row, w, (uint32_t)u, lo);
-        uint32_t codes[HEADS], byte[HEADS];
+    for (int64_t u0 = part * step * TOKENS; u0 < units; u0 += a.blocks_per_row * step * TOKENS) {
+        Kv4Unit x[TOKENS];
+        uint32_t codes[TOKENS][HEADS], byte[TOKENS][HEADS], last[TOKENS][HEADS]; /* last: the second four's scale */
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            codes[i] = 0u, byte[i] = 255u;    /* (of a bad page: NaN) */
-            if (x.page >= 0 && i < x.heads) {
-                codes[i] = *reinterpret_cast<const uint32_t *>(x.codes + ((i * a.c.stride_head) >> 1));
-                byte[i] = x.scales[i * a.c.scale_stride_head];
+        for (int k = 0; k < TOKENS; ++k) x[k] = kv4_unit<HEADS>(a, row, w, u0 + k * step + (threadIdx.x >> a.group_log), units);
+#pragma unroll
+        for (int k = 0; k < TOKENS; ++k) {
+#pragma unroll
+            for (int i = 0; i < HEADS; ++i) {
+                codes[k][i] = 0u, byte[k][i] = last[k][i] = 255u; /* (of a bad page: NaN) */
+                if (x[k].page < 0 || i >= x[k].heads) continue;
+                const char *c = x[k].codes + ((i * a.c.stride_head) >> 1);
+                const uint8_t *s = x[k].scales + i * a.c.scale_stride_head;
+                if (F32) {
+                    codes[k][i] = *reinterpret_cast<const uint16_t *>(c + lo / 2) | (uint32_t) * reinterpret_cast<const uint16_t *>(c + hi / 2) << 16;
+                    last[k][i] = s[hi / PARASON_KV_SCALE_GROUP];
+                } else {
+                    codes[k][i] = *reinterpret_cast<const uint32_t *>(c + lo / 2);
+                }
+                byte[k][i] = s[lo / PARASON_KV_SCALE_GROUP];
             }
+            if (x[k].page < 0 && x[k].heads > 0 && lane == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
         }
-        if (x.page < 0 && lane == 0) report(a.r, row, PARASON_KV_BAD_PAGE);
-        char *to = (x.is_v ? a.v : a.k) + ((w.start + x.token) * a.stride_token + x.head * a.stride_head) * type_bytes<T>();
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            float f[8];
-            fp4x8_to_f32(codes[i], fp4_scale(byte[i]), f);
-            if (i < x.heads) store8<T>(to + i * a.stride_head * type_bytes<T>(), lo, lo + 4, true, a.wide, f);
+        for (int k = 0; k < TOKENS; ++k) {
+            char *to = (x[k].is_v ? a.v : a.k) + ((w.start + x[k].token) * a.stride_token + x[k].head * a.stride_head) * type_bytes<T>();
+#pragma unroll
+            for (int i = 0; i < HEADS; ++i) {
+                float f[8], g[8];
+                fp4x8_to_f32(codes[k][i], fp4_scale(byte[k][i]), f);
+                if (F32) {
+                    fp4x8_to_f32(codes[k][i], fp4_scale(last[k][i]), g);
+#pragma unroll
+                    for (int e = 4; e < 8; ++e) f[e] = g[e];
+                }
+                if (i < x[k].heads) store8<T>(to + i * a.stride_head * type_bytes<T>(), lo, hi, true, a.wide, f);
+            }
         }
     }
 }

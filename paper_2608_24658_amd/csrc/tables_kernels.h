@@ -244,7 +244,7 @@ __device__ __forceinline__ int64_t wave_row_of(const int64_t *starts, int64_t lo
 __global__ void __launch_bounds__(FILL_THREADS) table_fill(TableArgs a)
 {
     __shared__ int64_t ends[2];
-    __shared__ int32_t first[FILL_TOKENS + 1];
+    __shared__ int32_t first[FILL_TOKENS], takes[FILL_TOKENS], olds[FILL_TOKENS], offs[FILL_TOKENS];
     const int64_t t0 = (int64_t)blockIdx.x * FILL_TOKENS;
     const int64_t t1 = t0 + FILL_TOKENS < a.n_tokens ? t0 + FILL_TOKENS : a.n_tokens; /* behind the last one */
     const int wave = (int)threadIdx.x >> 6;
@@ -261,8 +261,12 @@ __global__ void __launch_bounds__(FILL_THREADS) table_fill(TableArgs a)
     const bool held = n <= FILL_TOKENS; /* (more rows: most of them empty) */
     if (held)
         for (int i = (int)threadIdx.x; i < n; i += FILL_THREADS) {
-            const int64_t d = a.starts[r0 + i] - t0;
-            first[i] = d < 0 ? -1 : (int32_t)d;
+            const int64_t d = a.starts[r0 + i] - t0, off = a.off[r0 + i];
+            const int32_t n_taken = a.out_lengths[r0 + i];
+            /* (the first row may begin before this block: -2^31 where that is further than 31 bits say, which a row that is
+             * served never is) */
+            first[i] = d < INT32_MIN ? INT32_MIN : (int32_t)d;
+            takes[i] = n_taken, olds[i] = a.kv_lens[r0 + i] - n_taken, offs[i] = (int32_t)(off < INT32_MAX ? off : INT32_MAX);
         }
     __syncthreads();
     const int64_t have = a.head[0];
@@ -270,26 +274,27 @@ __global__ void __launch_bounds__(FILL_THREADS) table_fill(TableArgs a)
     for (int k = 0; k < FILL_PER; ++k) {
         const int32_t j = k * FILL_THREADS + (int32_t)threadIdx.x;
         const int64_t t = t0 + j;
-        if (t >= t1) break;
-        int64_t lo = 0, hi = n;
+        if (t >= t1) continue;
         if (held) {
-            int32_t l = 0, h = (int32_t)n;
-            while (h - l > 1) {
-                const int32_t mid = (l + h) >> 1;
-                if (first[mid] <= j) l = mid;
-                else h = mid;
+            int32_t lo = 0, hi = (int32_t)n;
+            while (hi - lo > 1) {
+                const int32_t mid = (lo + hi) >> 1;
+                if (first[mid] <= j) lo = mid;
+                else hi = mid;
             }
-            lo = l;
+            const int64_t in = (int64_t)j - first[lo];
+            place_token(a, t, in < takes[lo], r0 + lo, in, olds[lo], offs[lo], have);
         } else {
+            int64_t lo = 0, hi = n;
             while (hi - lo > 1) {
                 const int64_t mid = (lo + hi) >> 1;
                 if (a.starts[r0 + mid] <= t) lo = mid;
                 else hi = mid;
             }
+            const int64_t row = r0 + lo, in = t - a.starts[row];
+            const int32_t taken = a.out_lengths[row];
+            place_token(a, t, in < taken, row, in, a.kv_lens[row] - taken, a.off[row], have);
         }
-        const int64_t row = r0 + lo, in = t - a.starts[row];
-        const int32_t taken = a.out_lengths[row];
-        place_token(a, t, in < taken, row, in, a.kv_lens[row] - taken, a.off[row], have);
     }
 }
 

@@ -83,7 +83,7 @@ def test_write_then_read(dev, shape, given):
     assert status.cpu().tolist() == [0] * len(lengths)
 
 
-@pytest.mark.parametrize("heads", [1, 5, 8, 11])
+@pytest.mark.parametrize("heads", [1, 2, 5, 8, 11])
 def test_many_tokens(dev, heads):
     """Enough tokens that more heads are read at a time, and some of the last ones are not there."""
     log("case kv4 many tokens of %d heads" % heads)
