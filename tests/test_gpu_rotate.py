@@ -172,6 +172,37 @@ def test_values_that_are_not_finite(dev):
     assert all((t == 0).all() for t in res.values())
 
 
+def test_offsets_beyond_32_bits(dev):
+    """Tokens whose values lie behind 2^32 of the first one's, in and out."""
+    log("case rotation long offsets")
+    n, q_heads, k_heads, dim, stride = 4, 3, 2, 64, 1_500_000_016
+    q, k, w, at, freqs, _, _, call = make(dev, "bf16", n, q_heads, k_heads, dim, dim, 5, packed=False, padding=False)
+    dq, dk = (torch.randn(x.shape, generator=torch.Generator().manual_seed(i)).bfloat16().double().numpy() for i, x in enumerate((q, k)))
+    wide = [torch.empty((n - 1) * stride + (q_heads + k_heads) * dim, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    heads = [(b.as_strided((n, q_heads, dim), (stride, dim, 1)), b.as_strided((n, k_heads, dim), (stride, dim, 1), q_heads * dim)) for b in wide]
+    for views, values in zip(heads, ((q, k), (dq, dk))):
+        for v, x in zip(views, values):
+            v.copy_(torch.as_tensor(x))
+    grads = PX.qk_norm_rotate_grad(*heads[1], *heads[0], out=heads[1], **call)
+    got = PX.qk_norm_rotate(*heads[0], out=heads[0], **call)
+    for i, (x, dy, name) in enumerate(((q, dq, "q"), (k, dk, "k"))):
+        near(got[i], *S.rotate(x, w[i], at, freqs, 1e-6, False), "bf16", name)
+        dx, dw, dx_tol, dw_tol = S.rotate_grad(x, dy, w[i], at, freqs, 1e-6, False)
+        near(grads[name], dx, dx_tol, "bf16", "gradient of " + name)
+        assert (np.abs(grads[name + "_weight"].cpu().double().numpy() - dw) <= dw_tol).all()
+
+
+def test_the_smallest_eps(dev):
+    """Heads of zeros, and padding, with an eps that is no normal number: zeros, and no gradient that is not finite."""
+    log("case smallest eps")
+    x, at = torch.zeros(3, 2, 64, device=dev), torch.tensor([0, 5, -1], dtype=torch.int32, device=dev)
+    x[2] = float("nan")
+    f = torch.rand(32, device=dev, dtype=torch.float64)
+    assert all((t == 0).all() for t in PX.qk_norm_rotate(x, x, at, f, eps=1e-44))
+    res = PX.qk_norm_rotate_grad(x, x, x, x, at, f, eps=1e-44)
+    assert all((t == 0).all() for t in res.values())
+
+
 def test_no_tokens(dev):
     log("case no tokens")
     x = torch.empty(0, 3, 64, device=dev, dtype=torch.bfloat16)

@@ -140,6 +140,21 @@ def test_calls_without_rows_or_tokens(dev):
     T.shrink([0, 0])
 
 
+def test_offsets_beyond_32_bits(dev):
+    """Rows of the table that lie behind 2^32 bytes of the first one."""
+    log("case tables long offsets")
+    stride = 1_100_000_003
+    pages = torch.empty(2 * stride + 4, dtype=torch.int32, device=dev).as_strided((3, 4), (stride, 1))
+    pages.fill_(-1)
+    pool, i32 = PX.kv_pool(20, dev), lambda *v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+    lens = i32(0, 0, 0)
+    got = PX.kv_extend(pool, i32(5, 0, 7), lens, pages, 2, 12)
+    assert pages.tolist() == [[0, 1, 2, -1], [-1] * 4, [3, 4, 5, 6]] and lens.tolist() == [5, 0, 7]
+    assert got["slots"].tolist() == [0, 1, 2, 3, 4] + list(range(6, 13)) and pool.count.tolist() == [13]
+    PX.kv_shrink(pool, i32(1, 0, 2), lens, pages, 2)
+    assert pages.tolist() == [[0, -1, -1, -1], [-1] * 4, [3, -1, -1, -1]] and pool.free[:18].tolist() == list(range(19, 6, -1)) + [6, 5, 4, 2, 1]
+
+
 def test_tokens_that_nobody_asks_for(dev):
     """Through the C call: token arrays that are NULL are not written, and the status neither."""
     log("case no token arrays")
