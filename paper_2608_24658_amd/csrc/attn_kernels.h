@@ -543,7 +543,14 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             }
         }
         bool odd_seen = false;
-        if (masked && KIND != KV_INT8) {
+        /* (4-bit values in products with two terms: an infinity times the second, which is zero or negative as often as
+         * not, would be NaN, whoever sees it) */
+        bool far = false;
+        if (FOUR && SPLIT) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) far |= v_byte[p] >= FP4_FAR;
+        }
+        if (KIND != KV_INT8 && (masked || (FOUR && SPLIT && __ballot(far) != 0))) {
             /* infinities and NaN of V reach only the queries that see them, for which a product by zero would not do:
              * they are left out here and added one position at a time below */
 #pragma unroll
@@ -590,13 +597,13 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
             }
         }
         bool odd_values = false;             /* of the wave's positions, or of the block's */
-        if (masked && KIND != KV_INT8) {
+        if ((masked || (FOUR && SPLIT)) && KIND != KV_INT8) {
             if (Sh::SOLO) odd_values = __ballot(odd_seen) != 0;
             else if (odd_seen) flags[1] = x;
         }
         const uint64_t lo = m_lo, hi = m_hi;
         together();
-        if (masked && KIND != KV_INT8 && !Sh::SOLO) odd_values = flags[1] == x;
+        if ((masked || (FOUR && SPLIT)) && KIND != KV_INT8 && !Sh::SOLO) odd_values = flags[1] == x;
         /* ---- the next one is on its way (loads come back in order, so what is needed first goes first) */
         const int32_t x2 = x1 < t_end ? next_tile(x1 + 1) : t_end;
         load_page(x2);
