@@ -359,14 +359,21 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
                 if (a.negate) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
             }
             if (TWO) {
+                /* The first term is cut off, not rounded, so that what is left over has its sign, and where nothing is left
+                 * it is 2^-126 of that sign: an infinite key times either is the same infinity, and 2^-102 of the smallest
+                 * float16 is nothing beside it. */
                 uint32_t y[4] = {x.x, x.y, x.z, x.w}, z[4];
+                auto rest = [](float e) {    /* (bits; three are the most that are left) */
+                    const uint32_t b = __float_as_uint(e);
+                    const float r = e - __uint_as_float(b & 0xFFFF0000u);
+                    /* nothing of a zero; the maximum passes over the NaN that an infinity leaves */
+                    return __float_as_uint(fmaxf(fabsf(r), fminf(fabsf(e), 0x1p-126f))) | (b & 0x80000000u);
+                };
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float e0 = f16_to_f32(y[i] & 0xFFFFu), e1 = f16_to_f32(y[i] >> 16);
-                    y[i] = pack2<false>(e0, e1);
-                    const float r0 = e0 - __uint_as_float(y[i] << 16), r1 = e1 - __uint_as_float(y[i] & 0xFFFF0000u);
-                    /* (an infinity is all in the first term) */
-                    z[i] = pack2<false>(fabsf(e0) < INFINITY ? r0 : 0.0f, fabsf(e1) < INFINITY ? r1 : 0.0f);
+                    y[i] = (__float_as_uint(e0) >> 16) | (__float_as_uint(e1) & 0xFFFF0000u);
+                    z[i] = (rest(e0) >> 16) | (rest(e1) & 0xFFFF0000u);
                 }
                 x = make_uint4(y[0], y[1], y[2], y[3]);
                 qf_rest[k] = __builtin_bit_cast(frag8, make_uint4(z[0], z[1], z[2], z[3]));
