@@ -683,12 +683,14 @@ int parason_kv_read(const parason_kv_cache *cache, const parason_kv_rows *rows, 
  * holds.  Scores, maxima, sums and the accumulation are float32; for the matrix
  * product with v the weights exp(s_p - max), an 8-bit cache's scales of v
  * among them, are rounded to 16 bits (float16 over an F16 cache, else bfloat16;
- * F16 results over an 8- or 4-bit cache: to two bfloat16 terms).  Weights below
- * 2^-126 of a token's largest, and values of a 4-bit cache below 2^-126 (scales
- * that parason_kv_write does not make), may count as zero.  Weights below 2^-39
- * of a token's largest are nothing over an F16 cache: an infinity of v behind
- * such a weight gives NaN.  Bad rows get NaN (nothing, where starts[i] and
- * lengths[i] themselves are bad), and so do tokens that see a position on a bad
+ * F16 results over an 8- or 4-bit cache, and BF16 ones over a 4-bit cache in
+ * calls of at most 64 columns, max_length (at most n_tokens) times the query
+ * heads of a cache head: to two bfloat16 terms).  Weights below 2^-126 of a
+ * token's largest, and values of a 4-bit cache below 2^-126 (scales that
+ * parason_kv_write does not make), may count as zero.  Weights below 2^-39 of a
+ * token's largest are nothing over an F16 cache: an infinity of v behind such a
+ * weight gives NaN.  Bad rows get NaN (nothing, where starts[i] and lengths[i]
+ * themselves are bad), and so do tokens that see a position on a bad
  * page (others of their row may). */
 typedef struct parason_tree_args {
     const void *q;            /* value d of head h of token t: element t * q_stride_token + h * q_stride_head + d */

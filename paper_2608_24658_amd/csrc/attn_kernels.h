@@ -284,8 +284,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
     constexpr bool PF16 = KIND == KV_F16;
     /* float16 results over codes: the weights go in as two bfloat16 terms, so that they are not the coarsest step of
      * the whole.  (float16 weights would lose all precision where the positions with nearly all of the weight hold a
-     * code of zero.) */
-    constexpr bool SPLIT = (CODES || FOUR) && F16;
+     * code of zero.)  So do bfloat16 ones over a 4-bit cache for few columns, which the matrix units have time for: 128
+     * single tokens over 4,000 positions each 124.5 us, 121.9 with one term, 48 trees of 8 tokens 73.3 and 67.4.  A prompt
+     * of 8,192 tokens, which they bound, would take 745 us, 584 with one. */
+    constexpr bool SPLIT = CODES ? F16 : FOUR && (F16 || Sh::SOLO);
     /* The largest weight is 2^LIFT: of float16's 30 binades of full precision 29 are then below it. */
     constexpr int LIFT = PF16 ? 15 : 0;
     constexpr int VE = FOUR ? 32 : CODES ? 16 : 8; /* values of a 16-byte piece of the cache */
