@@ -603,8 +603,8 @@ int parason_kv_shrink(const parason_kv_pool *pool, const parason_kv_table *table
  *   y_a = n_a cos(p f_j) - n_b sin(p f_j),   y_b = n_b cos(p f_j) + n_a sin(p f_j),
  * (a, b) = (j, j + n_turned / 2), or (2j, 2j + 1) with
  * PARASON_ROTATE_INTERLEAVED; values from n_turned on are not rotated.  The
- * angle p f_j is reduced to a turn in double; all else is float32, rounded once
- * at the end.  (Squares that float32 does not hold are infinite: the head is
+ * angle p f_j is reduced to a turn in two doubles, as exact at 2^31 as at 1; all
+ * else is float32, rounded once at the end.  (Squares that float32 does not hold are infinite: the head is
  * zero then.)  A token with a negative position is padding: its results and
  * gradients are zero, whatever its values are. */
 #define PARASON_ROTATE_INTERLEAVED (1u << 0)

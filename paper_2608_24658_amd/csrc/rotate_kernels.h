@@ -39,13 +39,18 @@ struct RotArgs {
     float *sums;                 /* [blocks][2][dim] */
 };
 
-/* cos and sin of position * freq.  The angle is reduced to half turns in [-1, 1]
- * in double and goes on as two floats, so that the float functions see all of
- * it: the second, below 2^-25, turns what the first gave by its own small angle. */
+/* cos and sin of position * freq.  The product and its share of a turn are held
+ * as two doubles each, so that what is left of many turns is exact too: a double
+ * alone is off by 2^-53 of the whole angle, 2^-22 radians at 2^31.  The angle,
+ * in half turns in [-1, 1], goes on as two floats, so that the float functions
+ * see all of it: the second, below 2^-25, turns what the first gave by its own
+ * small angle. */
 __device__ __forceinline__ float2 turn_of(int32_t position, double freq)
 {
-    double t = (double)position * freq * 0.15915494309189535;
-    t = 2.0 * (t - __builtin_rint(t));
+    constexpr double PER_TURN = 0.15915494309189535, PER_TURN_LO = -9.839338337591243e-18; /* 1 / (2 pi) */
+    const double p = (double)position, x = p * freq, x_lo = __builtin_fma(p, freq, -x);
+    const double n = x * PER_TURN, n_lo = __builtin_fma(x, PER_TURN, -n) + __builtin_fma(x, PER_TURN_LO, x_lo * PER_TURN);
+    const double t = 2.0 * ((n - __builtin_rint(n)) + n_lo);
     const float hi = (float)t, lo = (float)(t - (double)hi) * 3.14159265358979f;
     float s, c;
     sincospif(hi, &s, &c);
