@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(ROT_THREADS, 4) qk_norm_rotate_grad(RotArgs a)
             if (p.live) rot_gather(s.w[v.is_k], p, gw);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                gw[e] = p.live ? gw[e] * g[e] : 0.0f;
+                gw[e] = p.live && there ? gw[e] * g[e] : 0.0f; /* (padding: whatever the weight is) */
                 sum = __builtin_fmaf(x[e], x[e], sum);
                 dot = __builtin_fmaf(gw[e], x[e], dot);
             }
