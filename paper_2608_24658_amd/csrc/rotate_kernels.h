@@ -259,6 +259,7 @@ __global__ void __launch_bounds__(ROT_THREADS, 4) qk_norm_rotate_grad(RotArgs a)
             }
             const float r = rsqrtf(__builtin_fmaf(group_sum(sum, a.group_log), a.inv_dim, a.eps));
             dot = group_sum(dot, a.group_log) * r * a.inv_dim;
+            dot = r == 0.0f ? 0.0f : dot; /* (a head without a length has no gradient, also where this sum is infinite) */
             if (!p.live) continue;
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] *= r;
