@@ -572,10 +572,15 @@ int parason_kv_tables_workspace_size(int64_t n_rows, size_t *bytes);
  * `out` is written.  n_tokens: the size of the call's token arrays, of which the
  * sum of the lengths may leave some over.  Not served, and left as they were:
  *   - bad rows: a negative length or kv_len, more positions than max_pages or
- *     PARASON_KV_MAX_LEN allow, tokens that reach beyond n_tokens;
+ *     PARASON_KV_MAX_LEN allow, tokens that reach beyond n_tokens, and all rows
+ *     behind such a one, those without tokens too;
  *   - rows that need a page when the pages that they and the rows before them
  *     (bad ones aside) need are more than the pool has.
- * Pages taken from the pool stay in free_pages, behind the new count. */
+ * Pages taken from the pool stay in free_pages, behind the new count.  New tokens
+ * go on in a row's last page where that has slots left: pages that rows share
+ * have to end with the shared prefix, or a row gets a copy of the last one
+ * first.  Two rows with the same such page get the same slots, and nothing
+ * reports it. */
 int parason_kv_extend(const parason_kv_pool *pool, const parason_kv_table *table, const int32_t *lengths,
                       int64_t n_tokens, const parason_kv_step *out, void *workspace, size_t workspace_bytes,
                       void *stream);

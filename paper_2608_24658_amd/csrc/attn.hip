@@ -64,7 +64,7 @@ int plan(const parason_kv_cache *c, const parason_kv_rows *r, int32_t n_q_heads,
     const int64_t tile = p->cols < 128 ? 128 : 64;
     /* Enough blocks to fill the device, and for few columns, whose partial results are small, parts short enough that
      * long rows among short ones do not finish last (4-bit positions are half as long as 8-bit ones, so that a part's
-     * beginning and end weigh more: 128 single tokens 247 us in parts of 4,096, 278 in parts of 1,024).  A part is
+     * beginning and end weigh more: 128 single tokens 231 us in parts of 4,096, 278 in parts of 1,024).  A part is
      * worth its results: 8 bytes a column and value, written and read, against 2 to 4 bytes a position and value.  24
      * parts of prompts of 2 to 300 tokens behind 1 to 18,000 positions, all blocks the longest row would need counted:
      * 247 us, which is the longest row's; those with columns: 147. */

@@ -5,9 +5,9 @@
  * keys or of values, eight values a lane.  The write needs the head's largest
  * magnitude before its first code, which the group finds by exchanges among
  * its lanes, so the values stay in registers between the two.  Bound by memory:
- * 165,000 positions of 8 heads of 128 values from FP8 pages of 24 slots to
+ * 182,000 positions of 8 heads of 128 values from FP8 pages of 24 slots to
  * bfloat16, 1.13 GB in all, take 256 us (4.4 TB/s, where a copy reaches 4.75);
- * 28,000 float16 tokens of 8 heads of 64 values to INT8 and back 44 us, two
+ * 23,500 float16 tokens of 8 heads of 64 values to INT8 and back 44 us, two
  * launches of 74 MB each.  A single token of 64 rows is two launches and the
  * host's checks, 23 us.
  */
@@ -289,13 +289,16 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read(KvMoveArgs a)
  * lane that finding its place and waiting for its page is most of the work: a
  * group takes HEADS heads of a token's keys or values, whose places are one
  * stride apart, and where these are fewer than four, several tokens at a time.
- * 165,000 positions of 8 heads of 128 values read as bfloat16, 0.94 GB, take 204
+ * 182,000 positions of 8 heads of 128 values read as bfloat16, 0.94 GB, take 204
  * us with 8 heads, 222 with 4 and 266 with one (and four tokens); the tokens of
  * 64 rows, where there are too few groups otherwise, 5.0 with 8 and 3.9 with 4.
  * 256,000 tokens of one head of 128 values: written in 46 us four at a time,
  * read in 38; 63 and 49 one by one. */
 constexpr int KV4_HEADS = 4, KV4_MORE = 8;
-constexpr int64_t KV4_MANY = 16384; /* tokens that are read KV4_MORE heads at a time */
+/* Tokens that are read KV4_MORE heads at a time.  Fewer leave too few groups, 2,048 of 8 heads of 128 values as bfloat16
+ * 5.3 us and 4.5 with four heads; from here on the two are within 3 % of each other or eight are faster, 131,072 tokens of
+ * 5 heads of 64 values 27.1 and 33.0 us, of 8 heads of 128 133.8 and 136.5 (float32 results up to 6 % either way). */
+constexpr int64_t KV4_MANY = 16384;
 
 struct Kv4Unit {
     int32_t page, token, head, heads; /* its first head, and how many (0: no unit) */

@@ -1138,8 +1138,9 @@ def qk_norm_rotate_grad(dq, dk, q, k, positions, freqs, q_weight=None, k_weight=
     """The backward pass of qk_norm_rotate: dict of the gradients q and k from
     those of its results, dq and dk (shapes and type of q and k), and q_weight
     and k_weight, float32 [head_dim] (weights=False: without these).  out: a pair
-    of tensors for q and k, which may be (dq, dk) or (q, k) themselves.
-    Asynchronous on the current stream."""
+    of tensors for q and k, which may be (dq, dk) or (q, k) themselves.  The
+    results are constants to autograd, also where an input requires a gradient:
+    there are no second derivatives.  Asynchronous on the current stream."""
     T = _types()
     xa, ga = _heads_args(T, q, k), _heads_args(T, dq, dk, like=(q, k))
     ra = _rotate_args(T, q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
