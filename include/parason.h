@@ -610,7 +610,8 @@ int parason_kv_shrink(const parason_kv_pool *pool, const parason_kv_table *table
  * PARASON_ROTATE_INTERLEAVED; values from n_turned on are not rotated.  The
  * angle p f_j is reduced to a turn in two doubles, as exact at 2^31 as at 1; all
  * else is float32, rounded once at the end.  (Squares that float32 does not hold
- * are infinite: the head is zero then, and its gradients.)  A token with a
+ * are infinite: the head is zero then, and its gradients.  Squares below 2^-126
+ * lose bits, which shows where eps does not outweigh them.)  A token with a
  * negative position is padding: its results and gradients are zero, whatever its
  * values and the weights are. */
 #define PARASON_ROTATE_INTERLEAVED (1u << 0)

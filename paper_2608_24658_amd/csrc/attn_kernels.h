@@ -730,7 +730,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeShape<DP, COLS, KIND>::BLOC
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
             for (int r = 0; r < NV; ++r) top = fmaxf(top, s[u][r]);
-        top = column_max<CN>(top);
+        /* (16-bit caches of more than 128 values a head and 32 columns, which have no registers left: a shuffle through LDS is
+         * faster there, 48 trees of 8 tokens over 4,000 positions of 256 values 829 us instead of 840) */
+        if constexpr (DP > 128 && COLS == 32 && !CODES && !FOUR) top = fmaxf(top, __shfl_xor(top, 32));
+        else top = column_max<CN>(top);
         /* Exponents beyond FAR are rounded by more than a weight bears (the largest would be 2^(LIFT + 1) or, further on,
          * infinite or nothing): they are rounded down, and the weights that this takes over 2^LIFT are 2^LIFT, which
          * makes equal what the scores' own rounding does not tell apart for certain. */
